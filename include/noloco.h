@@ -300,6 +300,145 @@ noloco_status noloco_replica_spread_noalloc(const noloco_launch_plan* plan, cons
                                             void* hip_stream);
 
 /*
+ * The inner step's operators (between two outer steps every worker trains its own row of the arena).
+ * Two parts of an inner step touch the arena itself: the update of the weight matrices, whose direction is
+ * the momentum orthogonalised by Newton-Schulz products, and the embedding table, which the forward pass
+ * looks tokens up in and whose gradient the backward pass adds up.  All take the W stacked rows at once.
+ */
+
+/* One matrix of every worker's row, row-major: element (i, j) is `offset + i * row_stride + j` elements into the row.
+ * Matrices may be columns of a larger tensor (queries, keys and values side by side: row_stride > cols); they must not
+ * share an element.  One with no rows or no columns is ignored. */
+typedef struct noloco_matrix {
+  int64_t offset;
+  int64_t rows, cols;
+  int64_t row_stride;      /* >= cols */
+  float scale;             /* noloco_muon_step: its learning rate is lr * scale */
+} noloco_matrix;
+
+/* How products take their operands (sums are always binary32).
+ *   F16    one binary16 a number: results to a few 2^-12 of their norm, what a bf16 result needs
+ *   PAIRS  a pair of binary16 (high and low half, 22 bits) and three products for each: a float result's last bits
+ *   AUTO   F16 for bf16 results, PAIRS for float ones */
+typedef enum noloco_products { NOLOCO_PRODUCTS_AUTO = 0, NOLOCO_PRODUCTS_F16 = 1, NOLOCO_PRODUCTS_PAIRS = 2 } noloco_products;
+
+/*
+ * Orthogonalisation by Newton-Schulz products: of a matrix U (X stands on its short side, X = U^T if U is tall)
+ *   X_0 = U / (|U|_F + eps);   step s:  A = X X^T,  X <- (a_s + b_s A + c_s A^2) X
+ * which takes every singular value x of X to x (a + b x^2 + c x^4), for suitable coefficients towards 1.
+ * A matrix of zeros gives zeros; a NaN or an infinity in U makes all of its result NaN (and of no other matrix).
+ *   steps         >= 1
+ *   coefficients  host, float[3 * steps]: a, b, c of every step.  Starting from singular values up to 1, every step
+ *                 must keep a + b x^2 + c x^4 within +-15.5 and its results within 2.79 (what binary16 has room
+ *                 for), else NOLOCO_ERR_UNSUPPORTED; NaN or infinite ones give NOLOCO_ERR_INVALID_ARG
+ *   eps           >= 0
+ *   products      noloco_products
+ */
+typedef struct noloco_newton_schulz {
+  int32_t steps;
+  const float* coefficients;
+  float eps;
+  int32_t products;
+} noloco_newton_schulz;
+
+/*
+ * Plan for the matrices of an arena's rows: validates them, uploads their table and allocates the workspace in which
+ * X, A and P are kept (one hipMalloc on the current device, freed by noloco_muon_plan_destroy).  Matrices go through the
+ * products in batches that fit the workspace.
+ *   matrices         host, [num_matrices], any order
+ *   worker_stride    elements between consecutive workers' rows, a multiple of NOLOCO_STRIDE_ALIGN_ELEMS
+ *   workspace_bytes  most bytes for the workspace; 0: 4 GiB.  Never more than all matrices need at once, and never less
+ *                    than the largest one needs by itself (about 16 bytes for each of its numbers when it is square)
+ * Errors: NOLOCO_ERR_SEGMENT_OVERLAP (two matrices share an element, or one leaves the row), NOLOCO_ERR_INVALID_ARG,
+ * NOLOCO_ERR_ALIGNMENT, NOLOCO_ERR_UNSUPPORTED (more than 2^28 numbers, or one of its sides above 2^22, in a matrix,
+ * or more than 2^24 copies of matrices), NOLOCO_ERR_DEVICE.  On error *out is null.
+ */
+typedef struct noloco_muon_plan noloco_muon_plan;
+noloco_status noloco_muon_plan_create(const noloco_matrix* matrices, int32_t num_matrices, int64_t worker_stride,
+                                      int32_t W, int64_t workspace_bytes, noloco_muon_plan** out);
+noloco_status noloco_muon_plan_destroy(noloco_muon_plan* plan);
+
+/* Facts about a plan: elements in matrices per worker, bytes of its workspace, and in how many batches bf16 and
+ * float results are made.  Any out pointer may be null. */
+noloco_status noloco_muon_plan_info(const noloco_muon_plan* plan, int64_t* elements_per_worker, int64_t* workspace_bytes,
+                                    int32_t* bf16_batches, int32_t* f32_batches);
+
+/*
+ * out = orthogonalised x, for every matrix of the plan in every worker's row (their `scale` is not used).
+ *   x, out   device, [W][worker_stride] float or bf16, NOLOCO_BASE_ALIGN_BYTES-aligned.  x may be out itself where the
+ *            types agree; otherwise the two must not overlap (NOLOCO_ERR_INVALID_ARG).  Elements of no matrix are
+ *            neither read nor written.
+ * Enqueued on hip_stream, not synchronised; allocates and copies nothing, so it may be captured into a HIP graph.
+ * The plan owns the workspace: calls sharing one plan must not overlap in time.  Results are bit-identical
+ * from run to run.  Every argument is checked before the first launch; after NOLOCO_ERR_DEVICE the output is undefined.
+ */
+noloco_status noloco_orthogonalize(const noloco_muon_plan* plan, const void* x, int32_t x_dtype, void* out,
+                                   int32_t out_dtype, const noloco_newton_schulz* method, void* hip_stream);
+
+typedef struct noloco_muon_hparams {
+  float lr;                /* learning rate */
+  float mu;                /* momentum */
+  float weight_decay;      /* decoupled: theta shrinks by lr * weight_decay a step */
+  int32_t nesterov;        /* 0: the momentum is orthogonalised, 1: grad + mu * momentum */
+} noloco_muon_hparams;
+
+/*
+ * One update of every matrix of the plan in every worker's row, in place:
+ *   momentum <- mu * momentum + grad
+ *   U = nesterov ? grad + mu * momentum : momentum
+ *   theta <- (1 - lr * weight_decay) * theta - lr * scale * NS(U)
+ *   theta, grad   device, [W][worker_stride] float or bf16
+ *   momentum      device, [W][worker_stride] float
+ * all NOLOCO_BASE_ALIGN_BYTES-aligned and none overlapping another.  bf16 weights are rounded to nearest once, after the
+ * update in float; AUTO takes products by theta's type.  As noloco_orthogonalize otherwise.
+ */
+noloco_status noloco_muon_step(const noloco_muon_plan* plan, void* theta, int32_t theta_dtype, const void* grad,
+                               int32_t grad_dtype, float* momentum, const noloco_muon_hparams* hparams,
+                               const noloco_newton_schulz* method, void* hip_stream);
+
+/* Types of token ids. */
+typedef enum noloco_token_type { NOLOCO_I32 = 2, NOLOCO_I64 = 3 } noloco_token_type;
+
+/*
+ * Plan for an embedding table in every worker's row: row v of worker w is the `width` elements from
+ * w * worker_stride + offset + v * width on.  Holds the scratch of noloco_embed_gradient for up to max_tokens tokens a worker
+ * (one hipMalloc: 16 bytes a token, and 8 bytes for each column of every 32 tokens).
+ * Errors: NOLOCO_ERR_SEGMENT_OVERLAP (the table leaves the row), NOLOCO_ERR_INVALID_ARG, NOLOCO_ERR_ALIGNMENT,
+ * NOLOCO_ERR_UNSUPPORTED (vocab above 2^29, width above 2^24, max_tokens above 2^27, W * max_tokens above 2^31 - 1),
+ * NOLOCO_ERR_DEVICE.  On error *out is null.
+ */
+typedef struct noloco_embedding_plan noloco_embedding_plan;
+noloco_status noloco_embedding_plan_create(int64_t offset, int64_t vocab, int64_t width, int64_t worker_stride, int32_t W,
+                                           int64_t max_tokens, noloco_embedding_plan** out);
+noloco_status noloco_embedding_plan_destroy(noloco_embedding_plan* plan);
+
+/*
+ * out[w][t] = scale * table_w[tokens[w][t]], a row of zeros where the token is negative or not below vocab (padding).
+ *   table       device, [W][worker_stride] float or bf16, NOLOCO_BASE_ALIGN_BYTES-aligned
+ *   tokens      device, [W][num_tokens] of token_type, aligned to its size
+ *   num_tokens  0 <= num_tokens <= max_tokens
+ *   out         device, [W][num_tokens][width] float or bf16, 16-byte-aligned
+ * One multiplication in binary32, rounded once to out's type.  Enqueued on hip_stream, not synchronised, nothing allocated.
+ */
+noloco_status noloco_embed_lookup(const noloco_embedding_plan* plan, const void* table, int32_t table_dtype,
+                                  const void* tokens, int32_t token_type, int64_t num_tokens, float scale, void* out,
+                                  int32_t out_dtype, void* hip_stream);
+
+/*
+ * The lookup's gradient: grad_w[v] = (accumulate ? grad_w[v] : 0) + scale * sum of dout[w][t] over the t with
+ * tokens[w][t] = v.  Positions whose token is negative or not below vocab are left out.
+ *   dout   device, [W][num_tokens][width] float or bf16, 16-byte-aligned
+ *   grad   device, [W][worker_stride] float or bf16, NOLOCO_BASE_ALIGN_BYTES-aligned; only the table's elements are
+ *          touched, with accumulate only the rows of tokens that come up
+ * Positions are sorted by token on the GPU (stable, so by token and position), sums are binary32 in an order that depends on the
+ * tokens alone: results are bit-identical from run to run.  Uses the plan's scratch: calls sharing one plan must not overlap
+ * in time.  Enqueued on hip_stream, not synchronised, nothing allocated.
+ */
+noloco_status noloco_embed_gradient(const noloco_embedding_plan* plan, const void* dout, int32_t dout_dtype,
+                                    const void* tokens, int32_t token_type, int64_t num_tokens, float scale, void* grad,
+                                    int32_t grad_dtype, int32_t accumulate, void* hip_stream);
+
+/*
  * Latency model (section "Latency results", appendix "Latency analysis").  Host only, seeded
  * Monte-Carlo; no GPU work.  Message and step times are LogNormal(mu, sigma^2), sigma >= 0.
  *

@@ -6,8 +6,10 @@ it libnoloco.so, is loaded on first use of any name below, so that
 `python -m paper_2506_10911_amd.build` can run before the library exists. There is no
 fallback: if the library is missing, that first use raises.
 """
-_NAMES = ("BF16", "F32", "LaunchPlan", "NolocoError", "copy_probe", "fill_probe", "read_probe",
-          "library_path", "merge_segments", "outer_step", "plan_groups", "plan_routes", "replica_spread", "replica_spread_noalloc", "sim_tree_vs_pair", "sim_barrier_penalty", "strerror",
+_NAMES = ("BF16", "EmbeddingPlan", "F32", "I32", "I64", "LaunchPlan", "MuonPlan", "NEWTON_SCHULZ", "NolocoError",
+          "PRODUCTS_AUTO", "PRODUCTS_F16", "PRODUCTS_PAIRS", "copy_probe", "embed_gradient", "embed_lookup", "fill_probe",
+          "library_path", "merge_segments", "muon_step", "orthogonalize", "outer_step", "plan_groups", "plan_routes",
+          "read_probe", "replica_spread", "replica_spread_noalloc", "sim_tree_vs_pair", "sim_barrier_penalty", "strerror",
           "binding")
 
 

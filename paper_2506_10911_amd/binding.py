@@ -12,6 +12,10 @@ import os
 import numpy as np
 
 F32, BF16 = 0, 1
+I32, I64 = 2, 3                                          # types of token ids
+PRODUCTS_AUTO, PRODUCTS_F16, PRODUCTS_PAIRS = 0, 1, 2
+# Five steps that take singular values from 0.003 to 1 to between 0.7 and 1.2.
+NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 MAX_GROUP = 256
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -41,6 +45,20 @@ class _HParams(C.Structure):
 class _Tuning(C.Structure):
     _fields_ = [("vectors_per_thread", C.c_int32), ("nontemporal", C.c_int32),
                 ("group_major", C.c_int32), ("xcd_map", C.c_int32)]
+
+
+class _Matrix(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64), ("row_stride", C.c_int64),
+                ("scale", C.c_float)]
+
+
+class _NewtonSchulz(C.Structure):
+    _fields_ = [("steps", C.c_int32), ("coefficients", C.POINTER(C.c_float)), ("eps", C.c_float),
+                ("products", C.c_int32)]
+
+
+class _MuonHParams(C.Structure):
+    _fields_ = [("lr", C.c_float), ("mu", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32)]
 
 
 def _load():
@@ -84,6 +102,27 @@ def _load():
     L.noloco_replica_spread.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
     L.noloco_replica_spread_noalloc.restype = C.c_int
     L.noloco_replica_spread_noalloc.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+    L.noloco_muon_plan_create.restype = C.c_int
+    L.noloco_muon_plan_create.argtypes = [C.POINTER(_Matrix), C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.POINTER(C.c_void_p)]
+    L.noloco_muon_plan_destroy.restype = C.c_int
+    L.noloco_muon_plan_destroy.argtypes = [C.c_void_p]
+    L.noloco_muon_plan_info.restype = C.c_int
+    L.noloco_muon_plan_info.argtypes = [C.c_void_p, C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+    L.noloco_orthogonalize.restype = C.c_int
+    L.noloco_orthogonalize.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.POINTER(_NewtonSchulz), C.c_void_p]
+    L.noloco_muon_step.restype = C.c_int
+    L.noloco_muon_step.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(_MuonHParams),
+                                   C.POINTER(_NewtonSchulz), C.c_void_p]
+    L.noloco_embedding_plan_create.restype = C.c_int
+    L.noloco_embedding_plan_create.argtypes = [C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int64, C.POINTER(C.c_void_p)]
+    L.noloco_embedding_plan_destroy.restype = C.c_int
+    L.noloco_embedding_plan_destroy.argtypes = [C.c_void_p]
+    L.noloco_embed_lookup.restype = C.c_int
+    L.noloco_embed_lookup.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_void_p,
+                                      C.c_int32, C.c_void_p]
+    L.noloco_embed_gradient.restype = C.c_int
+    L.noloco_embed_gradient.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_void_p,
+                                        C.c_int32, C.c_int32, C.c_void_p]
     L.noloco_copy_probe.restype = C.c_int
     L.noloco_copy_probe.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
     L.noloco_read_probe.restype = C.c_int
@@ -119,7 +158,9 @@ _calls = _load_calls()
 EXPORTS = ("noloco_plan_groups", "noloco_plan_routes", "noloco_merge_segments", "noloco_launch_plan_create",
            "noloco_launch_plan_destroy", "noloco_launch_plan_info", "noloco_launch_plan_tune",
            "noloco_outer_step", "noloco_replica_spread", "noloco_replica_spread_noalloc",
-           "noloco_sim_tree_vs_pair",
+           "noloco_muon_plan_create", "noloco_muon_plan_destroy", "noloco_muon_plan_info", "noloco_orthogonalize",
+           "noloco_muon_step", "noloco_embedding_plan_create", "noloco_embedding_plan_destroy", "noloco_embed_lookup",
+           "noloco_embed_gradient", "noloco_sim_tree_vs_pair",
            "noloco_sim_barrier_penalty", "noloco_copy_probe", "noloco_read_probe", "noloco_fill_probe",
            "noloco_strerror")
 
@@ -262,6 +303,101 @@ def replica_spread_noalloc(plan: LaunchPlan, x, x_dtype: int, out_std, stream=No
     status = _calls.replica_spread_noalloc(plan._layout, x, int(x_dtype), out_std, _stream(stream))
     if status != 0:
         raise NolocoError(status, "noloco_replica_spread_noalloc")
+
+
+class MuonPlan:
+    """noloco_muon_plan_create / _destroy / _info: the matrices of every worker's row, each (offset, rows, cols) or
+    (offset, rows, cols, row_stride) or (offset, rows, cols, row_stride, scale)."""
+
+    def __init__(self, matrices, worker_stride: int, W: int, workspace_bytes: int = 0):
+        self._handle = C.c_void_p(0)
+        self.worker_stride, self.W = int(worker_stride), int(W)
+        arr = (_Matrix * max(len(matrices), 1))()
+        for slot, m in zip(arr, matrices):
+            slot.offset, slot.rows, slot.cols = int(m[0]), int(m[1]), int(m[2])
+            slot.row_stride = int(m[3]) if len(m) > 3 else int(m[2])
+            slot.scale = float(m[4]) if len(m) > 4 else 1.0
+        _check(_lib.noloco_muon_plan_create(arr, len(matrices), self.worker_stride, self.W, int(workspace_bytes),
+                                            C.byref(self._handle)), "noloco_muon_plan_create")
+
+    def info(self):
+        e, b, one, two = C.c_int64(), C.c_int64(), C.c_int32(), C.c_int32()
+        _check(_lib.noloco_muon_plan_info(self._handle, C.byref(e), C.byref(b), C.byref(one), C.byref(two)),
+               "noloco_muon_plan_info")
+        return {"elements_per_worker": e.value, "workspace_bytes": b.value, "bf16_batches": one.value,
+                "f32_batches": two.value}
+
+    def destroy(self):
+        if self._handle:
+            handle, self._handle = self._handle, C.c_void_p(0)
+            _check(_lib.noloco_muon_plan_destroy(handle), "noloco_muon_plan_destroy")
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def _newton_schulz(coefficients, eps, products):
+    flat = [float(v) for step in coefficients for v in step]
+    if len(flat) != 3 * len(coefficients):
+        raise ValueError("coefficients: three numbers for every step")
+    return _NewtonSchulz(len(coefficients), (C.c_float * max(len(flat), 1))(*flat), float(eps), int(products))
+
+
+def orthogonalize(plan: MuonPlan, x, x_dtype: int, out, out_dtype: int, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
+                  products: int = PRODUCTS_AUTO, stream=None):
+    """noloco_orthogonalize: out <- Newton-Schulz of every matrix of the plan in x, one (a, b, c) for every step."""
+    method = _newton_schulz(coefficients, eps, products)
+    _check(_lib.noloco_orthogonalize(plan._handle, _ptr(x), int(x_dtype), _ptr(out), int(out_dtype), C.byref(method),
+                                     _stream(stream)), "noloco_orthogonalize")
+
+
+def muon_step(plan: MuonPlan, theta, theta_dtype: int, grad, grad_dtype: int, momentum, hparams, nesterov: bool = True,
+              coefficients=NEWTON_SCHULZ, eps: float = 1e-7, products: int = PRODUCTS_AUTO, stream=None):
+    """noloco_muon_step: one update of every matrix of the plan in place; hparams = (lr, mu, weight_decay)."""
+    method = _newton_schulz(coefficients, eps, products)
+    hp = _MuonHParams(float(hparams[0]), float(hparams[1]), float(hparams[2]), int(nesterov))
+    _check(_lib.noloco_muon_step(plan._handle, _ptr(theta), int(theta_dtype), _ptr(grad), int(grad_dtype), _ptr(momentum),
+                                 C.byref(hp), C.byref(method), _stream(stream)), "noloco_muon_step")
+
+
+class EmbeddingPlan:
+    """noloco_embedding_plan_create / _destroy: the table of `vocab` rows of `width` elements at `offset` of every worker's
+    row, for up to max_tokens tokens a worker."""
+
+    def __init__(self, offset: int, vocab: int, width: int, worker_stride: int, W: int, max_tokens: int):
+        self._handle = C.c_void_p(0)
+        _check(_lib.noloco_embedding_plan_create(int(offset), int(vocab), int(width), int(worker_stride), int(W),
+                                                 int(max_tokens), C.byref(self._handle)), "noloco_embedding_plan_create")
+
+    def destroy(self):
+        if self._handle:
+            handle, self._handle = self._handle, C.c_void_p(0)
+            _check(_lib.noloco_embedding_plan_destroy(handle), "noloco_embedding_plan_destroy")
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def embed_lookup(plan: EmbeddingPlan, table, table_dtype: int, tokens, token_type: int, num_tokens: int, scale: float, out,
+                 out_dtype: int, stream=None):
+    """noloco_embed_lookup: out[w, t] <- scale * table_w[tokens[w, t]], zeros where the token is no row of the table."""
+    _check(_lib.noloco_embed_lookup(plan._handle, _ptr(table), int(table_dtype), _ptr(tokens), int(token_type),
+                                    int(num_tokens), float(scale), _ptr(out), int(out_dtype), _stream(stream)),
+           "noloco_embed_lookup")
+
+
+def embed_gradient(plan: EmbeddingPlan, dout, dout_dtype: int, tokens, token_type: int, num_tokens: int, scale: float, grad,
+                   grad_dtype: int, accumulate: bool = False, stream=None):
+    """noloco_embed_gradient: grad_w[v] <- (grad_w[v] if accumulate) + scale * sum of dout[w, t] over tokens[w, t] = v."""
+    _check(_lib.noloco_embed_gradient(plan._handle, _ptr(dout), int(dout_dtype), _ptr(tokens), int(token_type),
+                                      int(num_tokens), float(scale), _ptr(grad), int(grad_dtype), int(accumulate),
+                                      _stream(stream)), "noloco_embed_gradient")
 
 
 def copy_probe(dst, src, nbytes: int, stream=None):

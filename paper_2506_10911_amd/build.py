@@ -21,8 +21,8 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libnoloco.so")
 CALLS = os.path.join(PKG, "_calls.so")       # CPython module of the binding
 OBJ = os.path.join(PKG, "_build")
-HOST_SOURCES = ["api.cpp", "planner.cpp", "launch_plan.cpp", "latency_model.cpp"]   # no device code
-DEVICE_SOURCES = ["kernels.hip"]
+HOST_SOURCES = ["api.cpp", "planner.cpp", "launch_plan.cpp", "latency_model.cpp", "inner_step.cpp"]   # no device code
+DEVICE_SOURCES = ["kernels.hip", "newton_schulz.hip", "embedding.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ROCM = os.path.dirname(os.path.dirname(os.path.realpath(HIPCC)))

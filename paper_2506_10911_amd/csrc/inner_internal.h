@@ -1,0 +1,105 @@
+// Types shared by the host side of the inner step's operators and their kernels (not part of the C ABI).
+#pragma once
+
+#include <cstdint>
+
+#include "noloco.h"
+
+namespace noloco {
+
+// ---------------------------------------------------------------------------
+// Orthogonalised updates of matrices
+// ---------------------------------------------------------------------------
+
+// Matrices of one shape that go through a launch together.  Everything that a product needs to know about them
+// travels in the kernel arguments; a launch serves at most kNsClasses shapes.
+constexpr int kNsClasses = 32;
+constexpr int kNsChunks = 256;          // partial sums of squares of one matrix
+constexpr int kNsChunkElems = 8192;     // elements that a workgroup sums, as long as kNsChunks of them are enough
+
+// X and A are held times 2^13, P times 2^12, so that binary16 has room for what they can be (A's eigenvalues up to
+// kNsMostA, P's up to kNsMostP) and the low halves of pairs are not subnormal.
+constexpr float kNsUnit = 8192.f, kNsUnitP = 4096.f;
+constexpr double kNsMostA = 7.8, kNsMostP = 15.5;
+
+// A worker's copy of a matrix.
+struct NsItem {
+  int64_t offset;       // first element in the array of all workers' rows
+  int64_t row_stride;
+  float scale;
+  int32_t pad;
+};
+
+struct NsClass {
+  uint64_t base;        // bytes from the workspace's start to the first item's buffers
+  uint64_t item_bytes;  // from one item's buffers to the next one's
+  uint32_t per_item;    // workgroups of one item in this launch
+  uint32_t first_item;  // in the plan's table of items
+  uint32_t first_sum;   // first item's place in the partial sums
+  uint32_t m, n;        // the short and the long side
+  uint32_t mp, np;      // and what they are padded to
+  uint32_t tall;        // the matrix has more rows than columns: X is its transpose
+};
+
+struct NsArgs {
+  uint32_t end[kNsClasses];     // workgroups of all classes up to and with this one; the rest 0xffffffff
+  NsClass cls[kNsClasses];
+  const NsItem* items;
+  char* workspace;
+  double* sums;                 // [item][kNsChunks]
+};
+
+// What an item's buffers hold, in bytes from their start: X and the next X [mp][np], A and P [mp][mp], each number
+// one binary16 or a pair of them ("planes").
+inline uint64_t ns_x_bytes(uint32_t mp, uint32_t np, int planes) { return uint64_t(mp) * np * 2 * planes; }
+inline uint64_t ns_item_bytes(uint32_t mp, uint32_t np, int planes) { return 2 * (ns_x_bytes(mp, np, planes) + ns_x_bytes(mp, mp, planes)); }
+
+enum NsKind { kNsGram = 0, kNsSquare = 1, kNsApply = 2, kNsLast = 3 };
+
+// The arrays that hold the matrices (device, all workers' rows).
+struct NsArrays {
+  const void* in;        // x, or the gradient
+  float* momentum;       // null: x is orthogonalised as it stands
+  void* out;             // out, or theta
+  int32_t in_bf16, out_bf16;
+  float mu;
+  int32_t nesterov;
+  float keep;            // 1 - lr * weight_decay
+  float lr;
+  int32_t update;        // out <- keep * out - lr * scale * result instead of out <- result
+  float eps;
+};
+
+int launch_ns_sums(const NsArgs& args, const NsArrays& arrays, uint32_t workgroups, void* stream);
+int launch_ns_start(const NsArgs& args, const NsArrays& arrays, int planes, uint32_t workgroups, void* stream);
+// Step `step` reads X number step & 1.
+int launch_ns_product(const NsArgs& args, const NsArrays& arrays, int kind, int tile, int planes, int step,
+                      float a, float b, float c, uint32_t workgroups, void* stream);
+
+// ---------------------------------------------------------------------------
+// Embedding lookup and its gradient
+// ---------------------------------------------------------------------------
+
+constexpr int kSortChunk = 2048;        // tokens that one workgroup sorts in its LDS
+constexpr int kMergeWays = 16;          // sorted lists that one merge joins
+constexpr int kSumChunk = 32;           // sorted positions that a workgroup sums
+
+struct EmbedArgs {
+  void* table;            // first element of worker 0's table (or of its gradient)
+  void* rows;             // out, or dout: [W][tokens][width]
+  const void* tokens;     // [W][tokens]
+  int64_t stride;         // between workers' tables
+  int64_t num_tokens;
+  uint32_t vocab, width;
+  int32_t W;
+  float scale;
+  int32_t table_bf16, rows_bf16, tokens_i64, accumulate;
+  int32_t vectors;        // four columns at a time: everything is aligned for it
+  uint64_t* sorted[2];    // [W][tokens] token << 32 | position
+  float* partial;         // [W][chunks][2][width]
+};
+
+int launch_embed_lookup(const EmbedArgs& args, void* stream);
+int launch_embed_gradient(const EmbedArgs& args, void* stream);
+
+}  // namespace noloco

@@ -1,0 +1,523 @@
+// C ABI of the inner step's operators: argument checking, plans, and the split of a call into kernel launches.  All
+// arithmetic is in newton_schulz.hip and embedding.hip.
+#include <hip/hip_runtime_api.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <limits>
+#include <memory>
+#include <new>
+#include <vector>
+
+#include "inner_internal.h"
+
+namespace {
+
+using noloco::NsArgs;
+using noloco::NsArrays;
+using noloco::NsClass;
+using noloco::NsItem;
+
+constexpr int64_t kDefaultWorkspace = 4ll << 30;
+constexpr int64_t kMostNumbers = 1ll << 28, kMostSide = 1ll << 22, kMostItems = 1ll << 24;
+constexpr uint64_t kMostGroups = 1u << 22;      // workgroups of a launch
+
+bool aligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+  return a0 < b0 + b_bytes && b0 < a0 + a_bytes;
+}
+
+bool is_dtype(int32_t t) { return t == NOLOCO_F32 || t == NOLOCO_BF16; }
+uint64_t bytes_of(int32_t dtype) { return dtype == NOLOCO_BF16 ? 2 : 4; }
+
+uint32_t padded(int64_t v, int tile) { return static_cast<uint32_t>((v + tile - 1) / tile * tile); }
+
+// Matrices of one shape.
+struct Shape {
+  uint32_t rows, cols;      // as stored
+  int tile;
+  uint32_t first_item, items;
+  uint32_t m() const { return std::min(rows, cols); }
+  uint32_t n() const { return std::max(rows, cols); }
+  uint32_t mp() const { return padded(m(), tile); }
+  uint32_t np() const { return padded(n(), tile); }
+  uint64_t item_bytes(int planes) const { return noloco::ns_item_bytes(mp(), np(), planes); }
+};
+
+// What goes through the products together, with its launches' arguments.
+struct Batch {
+  int tile;
+  NsArgs sums, start, symmetric, apply;
+  uint32_t sums_groups, start_groups, symmetric_groups, apply_groups;
+};
+
+// The tile that takes the least time by a rough model: a workgroup's share of the rate that products of this tile reach
+// with all its slots filled, for as many rounds as there are tiles.
+int tile_for(int64_t m, int64_t n, int64_t items) {
+  struct Kind { int tile; double slots, rate; };
+  constexpr Kind kinds[3] = {{256, 256, 1.0}, {128, 512, 0.9}, {64, 1024, 0.5}};
+  int best = 0;
+  double least = std::numeric_limits<double>::infinity();
+  for (const Kind& k : kinds) {
+    const double mp = padded(m, k.tile), np = padded(n, k.tile), mt = mp / k.tile, nt = np / k.tile;
+    if (noloco::ns_x_bytes(padded(m, k.tile), padded(n, k.tile), 2) >> 32 != 0) continue;      // a buffer's offsets have 32 bits
+    const double each = 2.0 * k.tile * k.tile * k.slots / k.rate;
+    auto rounds = [&](double tiles) { return std::max(1.0, tiles * items / k.slots); };
+    const double time = each * (rounds(mt * (mt + 1) / 2) * (n + m) + rounds(mt * nt) * m);
+    if (time < least) { least = time; best = k.tile; }
+  }
+  return best;
+}
+
+}  // namespace
+
+struct noloco_muon_plan {
+  int device = -1;
+  int32_t W = 0;
+  int64_t stride = 0;
+  int64_t elements = 0;
+  int64_t workspace_bytes = 0;
+  std::vector<Batch> batches[2];     // one binary16 a number, pairs
+  char* block = nullptr;             // the one device allocation: items, sums, workspace
+
+  noloco_muon_plan() = default;
+  noloco_muon_plan(const noloco_muon_plan&) = delete;
+  noloco_muon_plan& operator=(const noloco_muon_plan&) = delete;
+  ~noloco_muon_plan() {
+    if (block != nullptr) (void)hipFree(block);
+  }
+};
+
+struct noloco_embedding_plan {
+  int device = -1;
+  int64_t offset = 0, vocab = 0, width = 0, stride = 0, max_tokens = 0;
+  int32_t W = 0;
+  char* block = nullptr;
+  uint64_t* sorted[2] = {};
+  float* partial = nullptr;
+
+  noloco_embedding_plan() = default;
+  noloco_embedding_plan(const noloco_embedding_plan&) = delete;
+  noloco_embedding_plan& operator=(const noloco_embedding_plan&) = delete;
+  ~noloco_embedding_plan() {
+    if (block != nullptr) (void)hipFree(block);
+  }
+};
+
+namespace {
+
+// Do two matrices share an element?  Those whose rows touch each other are one run of elements, others a run for each row.
+noloco_status check_overlap(const std::vector<noloco_matrix>& matrices) {
+  std::vector<std::pair<int64_t, int64_t>> runs;
+  for (const noloco_matrix& m : matrices) {
+    if (m.row_stride == m.cols || m.rows == 1) {
+      runs.emplace_back(m.offset, m.offset + m.rows * m.cols);
+    } else {
+      for (int64_t r = 0; r < m.rows; ++r) runs.emplace_back(m.offset + r * m.row_stride, m.offset + r * m.row_stride + m.cols);
+    }
+  }
+  std::sort(runs.begin(), runs.end());
+  for (size_t i = 1; i < runs.size(); ++i)
+    if (runs[i].first < runs[i - 1].second) return NOLOCO_ERR_SEGMENT_OVERLAP;
+  return NOLOCO_OK;
+}
+
+// Splits the items of all shapes into batches that fit `room` bytes and a launch's table of classes.
+void make_batches(const std::vector<Shape>& shapes, int planes, uint64_t room, std::vector<Batch>* out) {
+  size_t shape = 0;
+  uint32_t done = 0;      // of that shape's items
+  while (shape < shapes.size()) {
+    Batch b;
+    b.tile = shapes[shape].tile;
+    b.sums_groups = b.start_groups = b.symmetric_groups = b.apply_groups = 0;
+    uint64_t used = 0;
+    uint32_t first_sum = 0;
+    int classes = 0;
+    for (NsArgs* a : {&b.sums, &b.start, &b.symmetric, &b.apply}) {
+      a->items = nullptr;
+      a->workspace = nullptr;
+      a->sums = nullptr;
+      for (int i = 0; i < noloco::kNsClasses; ++i) {
+        a->end[i] = 0xffffffffu;
+        a->cls[i] = NsClass{};
+      }
+    }
+    while (shape < shapes.size() && shapes[shape].tile == b.tile && classes < noloco::kNsClasses) {
+      const Shape& s = shapes[shape];
+      const uint64_t each = s.item_bytes(planes), elements = uint64_t(s.rows) * s.cols;
+      const uint32_t mt = s.mp() / b.tile, nt = s.np() / b.tile;
+      const uint32_t chunks = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>((elements + noloco::kNsChunkElems - 1) / noloco::kNsChunkElems, 1), noloco::kNsChunks));
+      const uint32_t per[4] = {chunks, s.mp() / 64 * (s.np() / 64), mt * (mt + 1) / 2, mt * nt};
+      uint32_t* groups[4] = {&b.sums_groups, &b.start_groups, &b.symmetric_groups, &b.apply_groups};
+      uint64_t fit = std::min<uint64_t>(s.items - done, (room - used) / each);
+      for (int k = 0; k < 4; ++k) {
+        const uint64_t left = *groups[k] < kMostGroups ? kMostGroups - *groups[k] : 0;
+        fit = std::min(fit, std::max<uint64_t>(left / per[k], used == 0 ? 1 : 0));
+      }
+      if (fit == 0) break;
+      NsClass c{};
+      c.base = used;
+      c.item_bytes = each;
+      c.first_item = s.first_item + done;
+      c.first_sum = first_sum;
+      c.m = s.m();
+      c.n = s.n();
+      c.mp = s.mp();
+      c.np = s.np();
+      c.tall = s.rows > s.cols ? 1 : 0;
+      NsArgs* args[4] = {&b.sums, &b.start, &b.symmetric, &b.apply};
+      for (int k = 0; k < 4; ++k) {
+        c.per_item = per[k];
+        *groups[k] += per[k] * static_cast<uint32_t>(fit);
+        args[k]->cls[classes] = c;
+        args[k]->end[classes] = *groups[k];
+      }
+      ++classes;
+      used += each * fit;
+      first_sum += static_cast<uint32_t>(fit);
+      done += static_cast<uint32_t>(fit);
+      if (done < s.items) break;
+      ++shape;
+      done = 0;
+    }
+    out->push_back(b);
+  }
+}
+
+uint32_t most_items(const std::vector<Batch>& batches) {
+  uint32_t most = 0;
+  for (const Batch& b : batches) {
+    uint32_t items = 0, last = 0;
+    for (int i = 0; i < noloco::kNsClasses && b.sums.end[i] != 0xffffffffu; ++i) {
+      items += (b.sums.end[i] - last) / b.sums.cls[i].per_item;
+      last = b.sums.end[i];
+    }
+    most = std::max(most, items);
+  }
+  return most;
+}
+
+noloco_status create_muon_plan(const noloco_matrix* given, int32_t num, int64_t stride, int32_t W, int64_t workspace,
+                               noloco_muon_plan** out) {
+  std::unique_ptr<noloco_muon_plan> plan(new noloco_muon_plan);
+  plan->W = W;
+  plan->stride = stride;
+  std::vector<noloco_matrix> matrices;
+  for (int32_t i = 0; i < num; ++i) {
+    const noloco_matrix& m = given[i];
+    if (m.offset < 0 || m.rows < 0 || m.cols < 0 || m.row_stride < m.cols || !std::isfinite(m.scale)) return NOLOCO_ERR_INVALID_ARG;
+    if (m.rows == 0 || m.cols == 0) continue;
+    if (m.rows > kMostSide || m.cols > kMostSide || m.rows * m.cols > kMostNumbers) return NOLOCO_ERR_UNSUPPORTED;
+    // the last element's place, without a product that could overflow
+    if (m.offset > stride || m.cols > stride - m.offset) return NOLOCO_ERR_SEGMENT_OVERLAP;
+    if (m.rows > 1 && m.row_stride > (stride - m.offset - m.cols) / (m.rows - 1)) return NOLOCO_ERR_SEGMENT_OVERLAP;
+    matrices.push_back(m);
+    plan->elements += m.rows * m.cols;
+  }
+  if (static_cast<int64_t>(matrices.size()) * W > kMostItems) return NOLOCO_ERR_UNSUPPORTED;
+  const noloco_status st = check_overlap(matrices);
+  if (st != NOLOCO_OK) return st;
+
+  // Those with the longest products first, so that a launch does not end with them.
+  std::stable_sort(matrices.begin(), matrices.end(), [](const noloco_matrix& a, const noloco_matrix& b) {
+    const int64_t an = std::max(a.rows, a.cols), bn = std::max(b.rows, b.cols);
+    if (an != bn) return an > bn;
+    if (a.rows * a.cols != b.rows * b.cols) return a.rows * a.cols > b.rows * b.cols;
+    return a.rows > b.rows;
+  });
+  std::vector<Shape> shapes;
+  std::vector<NsItem> items;
+  for (size_t i = 0; i < matrices.size();) {
+    size_t end = i;
+    Shape s{};
+    s.rows = static_cast<uint32_t>(matrices[i].rows);
+    s.cols = static_cast<uint32_t>(matrices[i].cols);
+    s.first_item = static_cast<uint32_t>(items.size());
+    while (end < matrices.size() && matrices[end].rows == matrices[i].rows && matrices[end].cols == matrices[i].cols) {
+      for (int32_t w = 0; w < W; ++w)
+        items.push_back(NsItem{w * stride + matrices[end].offset, matrices[end].row_stride, matrices[end].scale, 0});
+      ++end;
+    }
+    s.items = static_cast<uint32_t>(items.size()) - s.first_item;
+    s.tile = tile_for(s.m(), s.n(), s.items);
+    shapes.push_back(s);
+    i = end;
+  }
+  std::stable_sort(shapes.begin(), shapes.end(), [](const Shape& a, const Shape& b) { return a.tile > b.tile; });
+
+  uint64_t all = 0, largest = 0;
+  for (const Shape& s : shapes) {
+    all += s.item_bytes(2) * s.items;
+    largest = std::max(largest, s.item_bytes(2));
+  }
+  const uint64_t room = std::max(largest, std::min(all, static_cast<uint64_t>(workspace > 0 ? workspace : kDefaultWorkspace)));
+  plan->workspace_bytes = static_cast<int64_t>(room);
+  for (int planes = 1; planes <= 2; ++planes) make_batches(shapes, planes, room, &plan->batches[planes - 1]);
+  const uint64_t sums = std::max(most_items(plan->batches[0]), most_items(plan->batches[1]));
+  auto whole = [](uint64_t bytes) { return (bytes + 4095) / 4096 * 4096; };
+  const uint64_t item_bytes = whole(items.size() * sizeof(NsItem)), sum_bytes = whole(sums * noloco::kNsChunks * sizeof(double));
+  if (hipGetDevice(&plan->device) != hipSuccess ||
+      hipMalloc(reinterpret_cast<void**>(&plan->block), item_bytes + sum_bytes + room + 4096) != hipSuccess) {
+    plan->block = nullptr;
+    return NOLOCO_ERR_DEVICE;
+  }
+  if (!items.empty() && hipMemcpy(plan->block, items.data(), items.size() * sizeof(NsItem), hipMemcpyHostToDevice) != hipSuccess)
+    return NOLOCO_ERR_DEVICE;
+  for (std::vector<Batch>& batches : plan->batches)
+    for (Batch& b : batches)
+      for (NsArgs* a : {&b.sums, &b.start, &b.symmetric, &b.apply}) {
+        a->items = reinterpret_cast<const NsItem*>(plan->block);
+        a->sums = reinterpret_cast<double*>(plan->block + item_bytes);
+        a->workspace = plan->block + item_bytes + sum_bytes;
+      }
+  *out = plan.release();
+  return NOLOCO_OK;
+}
+
+// Do the coefficients keep what binary16 holds in its range?  Singular values start at most at 1.
+noloco_status check_method(const noloco_newton_schulz* method) {
+  if (method == nullptr || method->coefficients == nullptr) return NOLOCO_ERR_NULL;
+  if (method->steps < 1 || !(method->eps >= 0.f) || !std::isfinite(method->eps)) return NOLOCO_ERR_INVALID_ARG;
+  if (method->products < NOLOCO_PRODUCTS_AUTO || method->products > NOLOCO_PRODUCTS_PAIRS) return NOLOCO_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < 3 * method->steps; ++i)
+    if (!std::isfinite(method->coefficients[i])) return NOLOCO_ERR_INVALID_ARG;
+  double most = 1.002;      // of a singular value, with room for the rounding of X
+  for (int32_t s = 0; s < method->steps; ++s) {
+    const double a = method->coefficients[3 * s], b = method->coefficients[3 * s + 1], c = method->coefficients[3 * s + 2];
+    auto poly = [&](double square) { return a + square * (b + square * c); };
+    const double square = most * most;
+    // extremes of P on [0, square], and of x P(x^2) on [0, most]
+    double p = std::max(std::fabs(a), std::fabs(poly(square))), x = most * std::fabs(poly(square));
+    if (c != 0. && -b / (2 * c) > 0. && -b / (2 * c) < square) p = std::max(p, std::fabs(poly(-b / (2 * c))));
+    const double root = 9 * b * b - 20 * a * c;
+    double at[2] = {-1., -1.};
+    if (c == 0.) {
+      if (b != 0.) at[0] = -a / (3 * b);
+    } else if (root >= 0.) {
+      at[0] = (-3 * b + std::sqrt(root)) / (10 * c);
+      at[1] = (-3 * b - std::sqrt(root)) / (10 * c);
+    }
+    for (double v : at)
+      if (v > 0. && v < square) x = std::max(x, std::sqrt(v) * std::fabs(poly(v)));
+    most = x * 1.002;
+    if (!(p <= noloco::kNsMostP) || !(most * most <= noloco::kNsMostA)) return NOLOCO_ERR_UNSUPPORTED;
+  }
+  return NOLOCO_OK;
+}
+
+noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, const noloco_newton_schulz* method, void* stream) {
+  const int32_t products = method->products != NOLOCO_PRODUCTS_AUTO ? method->products
+                                                                    : (arrays.out_bf16 ? NOLOCO_PRODUCTS_F16 : NOLOCO_PRODUCTS_PAIRS);
+  const int planes = products == NOLOCO_PRODUCTS_F16 ? 1 : 2;
+  for (const Batch& b : plan->batches[planes - 1]) {
+    if (noloco::launch_ns_sums(b.sums, arrays, b.sums_groups, stream) != 0) return NOLOCO_ERR_DEVICE;
+    if (noloco::launch_ns_start(b.start, arrays, planes, b.start_groups, stream) != 0) return NOLOCO_ERR_DEVICE;
+    for (int32_t s = 0; s < method->steps; ++s) {
+      const float *k = method->coefficients + 3 * s;
+      const int last = s + 1 == method->steps ? noloco::kNsLast : noloco::kNsApply;
+      if (noloco::launch_ns_product(b.symmetric, arrays, noloco::kNsGram, b.tile, planes, s, k[0], k[1], k[2], b.symmetric_groups, stream) != 0 ||
+          noloco::launch_ns_product(b.symmetric, arrays, noloco::kNsSquare, b.tile, planes, s, k[0], k[1], k[2], b.symmetric_groups, stream) != 0 ||
+          noloco::launch_ns_product(b.apply, arrays, last, b.tile, planes, s, k[0], k[1], k[2], b.apply_groups, stream) != 0)
+        return NOLOCO_ERR_DEVICE;
+    }
+  }
+  return NOLOCO_OK;
+}
+
+}  // namespace
+
+extern "C" noloco_status noloco_muon_plan_create(const noloco_matrix* matrices, int32_t num_matrices, int64_t worker_stride,
+                                                 int32_t W, int64_t workspace_bytes, noloco_muon_plan** out) {
+  if (out == nullptr) return NOLOCO_ERR_NULL;
+  *out = nullptr;
+  if (num_matrices < 0 || worker_stride < 0 || W < 1 || workspace_bytes < 0) return NOLOCO_ERR_INVALID_ARG;
+  if (matrices == nullptr && num_matrices > 0) return NOLOCO_ERR_NULL;
+  if (W > NOLOCO_MAX_WORKERS) return NOLOCO_ERR_UNSUPPORTED;
+  if (worker_stride > std::numeric_limits<int64_t>::max() / 8 / W) return NOLOCO_ERR_UNSUPPORTED;
+  if (worker_stride % NOLOCO_STRIDE_ALIGN_ELEMS != 0) return NOLOCO_ERR_ALIGNMENT;
+  try {
+    return create_muon_plan(matrices, num_matrices, worker_stride, W, workspace_bytes, out);
+  } catch (const std::bad_alloc&) {
+    return NOLOCO_ERR_NO_MEMORY;
+  } catch (...) {
+    return NOLOCO_ERR_INVALID_ARG;
+  }
+}
+
+extern "C" noloco_status noloco_muon_plan_destroy(noloco_muon_plan* plan) {
+  if (plan == nullptr) return NOLOCO_OK;
+  noloco_status st = NOLOCO_OK;
+  if (plan->block != nullptr && hipFree(plan->block) != hipSuccess) st = NOLOCO_ERR_DEVICE;
+  plan->block = nullptr;
+  delete plan;
+  return st;
+}
+
+extern "C" noloco_status noloco_muon_plan_info(const noloco_muon_plan* plan, int64_t* elements_per_worker,
+                                               int64_t* workspace_bytes, int32_t* bf16_batches, int32_t* f32_batches) {
+  if (plan == nullptr) return NOLOCO_ERR_NULL;
+  if (elements_per_worker != nullptr) *elements_per_worker = plan->elements;
+  if (workspace_bytes != nullptr) *workspace_bytes = plan->workspace_bytes;
+  if (bf16_batches != nullptr) *bf16_batches = static_cast<int32_t>(plan->batches[0].size());
+  if (f32_batches != nullptr) *f32_batches = static_cast<int32_t>(plan->batches[1].size());
+  return NOLOCO_OK;
+}
+
+extern "C" noloco_status noloco_orthogonalize(const noloco_muon_plan* plan, const void* x, int32_t x_dtype, void* out,
+                                              int32_t out_dtype, const noloco_newton_schulz* method, void* hip_stream) {
+  if (plan == nullptr || x == nullptr || out == nullptr) return NOLOCO_ERR_NULL;
+  const noloco_status st = check_method(method);
+  if (st != NOLOCO_OK) return st;
+  if (!is_dtype(x_dtype) || !is_dtype(out_dtype)) return NOLOCO_ERR_INVALID_ARG;
+  if (!aligned(x, NOLOCO_BASE_ALIGN_BYTES) || !aligned(out, NOLOCO_BASE_ALIGN_BYTES)) return NOLOCO_ERR_ALIGNMENT;
+  const uint64_t numbers = static_cast<uint64_t>(plan->W) * static_cast<uint64_t>(plan->stride);
+  if (!(x == out && x_dtype == out_dtype) && overlap(x, numbers * bytes_of(x_dtype), out, numbers * bytes_of(out_dtype)))
+    return NOLOCO_ERR_INVALID_ARG;
+  NsArrays arrays{};
+  arrays.in = x;
+  arrays.out = out;
+  arrays.in_bf16 = x_dtype == NOLOCO_BF16;
+  arrays.out_bf16 = out_dtype == NOLOCO_BF16;
+  arrays.eps = method->eps;
+  return run_batches(plan, arrays, method, hip_stream);
+}
+
+extern "C" noloco_status noloco_muon_step(const noloco_muon_plan* plan, void* theta, int32_t theta_dtype, const void* grad,
+                                          int32_t grad_dtype, float* momentum, const noloco_muon_hparams* hparams,
+                                          const noloco_newton_schulz* method, void* hip_stream) {
+  if (plan == nullptr || theta == nullptr || grad == nullptr || momentum == nullptr || hparams == nullptr) return NOLOCO_ERR_NULL;
+  const noloco_status st = check_method(method);
+  if (st != NOLOCO_OK) return st;
+  if (!is_dtype(theta_dtype) || !is_dtype(grad_dtype) || (hparams->nesterov != 0 && hparams->nesterov != 1)) return NOLOCO_ERR_INVALID_ARG;
+  if (!aligned(theta, NOLOCO_BASE_ALIGN_BYTES) || !aligned(grad, NOLOCO_BASE_ALIGN_BYTES) || !aligned(momentum, NOLOCO_BASE_ALIGN_BYTES))
+    return NOLOCO_ERR_ALIGNMENT;
+  const uint64_t numbers = static_cast<uint64_t>(plan->W) * static_cast<uint64_t>(plan->stride);
+  const uint64_t tb = numbers * bytes_of(theta_dtype), gb = numbers * bytes_of(grad_dtype), mb = numbers * 4;
+  if (overlap(theta, tb, grad, gb) || overlap(theta, tb, momentum, mb) || overlap(grad, gb, momentum, mb)) return NOLOCO_ERR_INVALID_ARG;
+  NsArrays arrays{};
+  arrays.in = grad;
+  arrays.momentum = momentum;
+  arrays.out = theta;
+  arrays.in_bf16 = grad_dtype == NOLOCO_BF16;
+  arrays.out_bf16 = theta_dtype == NOLOCO_BF16;
+  arrays.mu = hparams->mu;
+  arrays.nesterov = hparams->nesterov;
+  arrays.keep = static_cast<float>(1.0 - static_cast<double>(hparams->lr) * hparams->weight_decay);
+  arrays.lr = hparams->lr;
+  arrays.update = 1;
+  arrays.eps = method->eps;
+  return run_batches(plan, arrays, method, hip_stream);
+}
+
+// ---------------------------------------------------------------------------
+// Embedding
+// ---------------------------------------------------------------------------
+
+extern "C" noloco_status noloco_embedding_plan_create(int64_t offset, int64_t vocab, int64_t width, int64_t worker_stride,
+                                                      int32_t W, int64_t max_tokens, noloco_embedding_plan** out) {
+  if (out == nullptr) return NOLOCO_ERR_NULL;
+  *out = nullptr;
+  if (offset < 0 || vocab < 1 || width < 1 || worker_stride < 0 || W < 1 || max_tokens < 0) return NOLOCO_ERR_INVALID_ARG;
+  if (W > NOLOCO_MAX_WORKERS || vocab > (1 << 29) || width > (1 << 24) || max_tokens > (1 << 27) ||
+      W * max_tokens > std::numeric_limits<int32_t>::max() || worker_stride > std::numeric_limits<int64_t>::max() / 8 / W)
+    return NOLOCO_ERR_UNSUPPORTED;
+  if (worker_stride % NOLOCO_STRIDE_ALIGN_ELEMS != 0) return NOLOCO_ERR_ALIGNMENT;
+  if (offset > worker_stride || vocab > (worker_stride - offset) / width) return NOLOCO_ERR_SEGMENT_OVERLAP;
+  std::unique_ptr<noloco_embedding_plan> plan(new (std::nothrow) noloco_embedding_plan);
+  if (plan == nullptr) return NOLOCO_ERR_NO_MEMORY;
+  plan->offset = offset;
+  plan->vocab = vocab;
+  plan->width = width;
+  plan->stride = worker_stride;
+  plan->W = W;
+  plan->max_tokens = max_tokens;
+  auto whole = [](uint64_t bytes) { return (bytes + 255) / 256 * 256; };
+  const uint64_t list = whole(static_cast<uint64_t>(W) * max_tokens * sizeof(uint64_t));
+  const uint64_t chunks = static_cast<uint64_t>(max_tokens + noloco::kSumChunk - 1) / noloco::kSumChunk;
+  const uint64_t partial = static_cast<uint64_t>(W) * chunks * 2 * width * sizeof(float);
+  if (hipGetDevice(&plan->device) != hipSuccess ||
+      hipMalloc(reinterpret_cast<void**>(&plan->block), 2 * list + partial + 256) != hipSuccess) {
+    plan->block = nullptr;
+    return NOLOCO_ERR_DEVICE;
+  }
+  plan->sorted[0] = reinterpret_cast<uint64_t*>(plan->block);
+  plan->sorted[1] = reinterpret_cast<uint64_t*>(plan->block + list);
+  plan->partial = reinterpret_cast<float*>(plan->block + 2 * list);
+  *out = plan.release();
+  return NOLOCO_OK;
+}
+
+extern "C" noloco_status noloco_embedding_plan_destroy(noloco_embedding_plan* plan) {
+  if (plan == nullptr) return NOLOCO_OK;
+  noloco_status st = NOLOCO_OK;
+  if (plan->block != nullptr && hipFree(plan->block) != hipSuccess) st = NOLOCO_ERR_DEVICE;
+  plan->block = nullptr;
+  delete plan;
+  return st;
+}
+
+namespace {
+
+// Checks what lookup and gradient share; fills the kernels' arguments.
+noloco_status embed_args(const noloco_embedding_plan* plan, const void* table, int32_t table_dtype, const void* rows,
+                         int32_t rows_dtype, const void* tokens, int32_t token_type, int64_t num_tokens, float scale,
+                         noloco::EmbedArgs* out) {
+  if (plan == nullptr || table == nullptr) return NOLOCO_ERR_NULL;
+  if (num_tokens < 0 || num_tokens > plan->max_tokens) return NOLOCO_ERR_INVALID_ARG;
+  if (num_tokens > 0 && (rows == nullptr || tokens == nullptr)) return NOLOCO_ERR_NULL;
+  if (!is_dtype(table_dtype) || !is_dtype(rows_dtype) || (token_type != NOLOCO_I32 && token_type != NOLOCO_I64))
+    return NOLOCO_ERR_INVALID_ARG;
+  const uint64_t token_bytes = token_type == NOLOCO_I64 ? 8 : 4;
+  if (!aligned(table, NOLOCO_BASE_ALIGN_BYTES) || !aligned(rows, 16) || !aligned(tokens, token_bytes)) return NOLOCO_ERR_ALIGNMENT;
+  const uint64_t tokens_all = static_cast<uint64_t>(plan->W) * num_tokens;
+  const uint64_t table_all = static_cast<uint64_t>(plan->W) * plan->stride * bytes_of(table_dtype);
+  const uint64_t rows_all = tokens_all * plan->width * bytes_of(rows_dtype);
+  if (overlap(table, table_all, rows, rows_all) || overlap(tokens, tokens_all * token_bytes, rows, rows_all) ||
+      overlap(table, table_all, tokens, tokens_all * token_bytes))
+    return NOLOCO_ERR_INVALID_ARG;
+  *out = noloco::EmbedArgs{};
+  out->table = static_cast<char*>(const_cast<void*>(table)) + plan->offset * static_cast<int64_t>(bytes_of(table_dtype));
+  out->rows = const_cast<void*>(rows);
+  out->tokens = tokens;
+  out->stride = plan->stride;
+  out->num_tokens = num_tokens;
+  out->vocab = static_cast<uint32_t>(plan->vocab);
+  out->width = static_cast<uint32_t>(plan->width);
+  out->W = plan->W;
+  out->scale = scale;
+  out->table_bf16 = table_dtype == NOLOCO_BF16;
+  out->rows_bf16 = rows_dtype == NOLOCO_BF16;
+  out->tokens_i64 = token_type == NOLOCO_I64;
+  out->vectors = plan->width % 4 == 0 && plan->offset % 4 == 0;
+  out->sorted[0] = plan->sorted[0];
+  out->sorted[1] = plan->sorted[1];
+  out->partial = plan->partial;
+  return NOLOCO_OK;
+}
+
+}  // namespace
+
+extern "C" noloco_status noloco_embed_lookup(const noloco_embedding_plan* plan, const void* table, int32_t table_dtype,
+                                             const void* tokens, int32_t token_type, int64_t num_tokens, float scale,
+                                             void* out, int32_t out_dtype, void* hip_stream) {
+  noloco::EmbedArgs args;
+  const noloco_status st = embed_args(plan, table, table_dtype, out, out_dtype, tokens, token_type, num_tokens, scale, &args);
+  if (st != NOLOCO_OK) return st;
+  if (num_tokens == 0) return NOLOCO_OK;
+  return noloco::launch_embed_lookup(args, hip_stream) == 0 ? NOLOCO_OK : NOLOCO_ERR_DEVICE;
+}
+
+extern "C" noloco_status noloco_embed_gradient(const noloco_embedding_plan* plan, const void* dout, int32_t dout_dtype,
+                                               const void* tokens, int32_t token_type, int64_t num_tokens, float scale,
+                                               void* grad, int32_t grad_dtype, int32_t accumulate, void* hip_stream) {
+  if (accumulate != 0 && accumulate != 1) return NOLOCO_ERR_INVALID_ARG;
+  noloco::EmbedArgs args;
+  const noloco_status st = embed_args(plan, grad, grad_dtype, dout, dout_dtype, tokens, token_type, num_tokens, scale, &args);
+  if (st != NOLOCO_OK) return st;
+  args.accumulate = accumulate;
+  if (num_tokens == 0 && accumulate) return NOLOCO_OK;
+  return noloco::launch_embed_gradient(args, hip_stream) == 0 ? NOLOCO_OK : NOLOCO_ERR_DEVICE;
+}

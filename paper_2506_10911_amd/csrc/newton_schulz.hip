@@ -1,0 +1,602 @@
+// Newton-Schulz orthogonalisation of many matrices at once (kernels and their launchers).
+//
+// X_0 = U / (|U|_F + eps), transposed if U is tall, so that X is m x n with m <= n; a step is
+//   A = X X^T          m x m, symmetric
+//   P = a + b A + c A^2   m x m, symmetric
+//   X <- P X
+// which takes every singular value s of X to s (a + b s^2 + c s^4).  All three are matrix products with both
+// operands in binary16 and sums in binary32.  |X_0| <= 1 and the polynomial keeps X small, so binary16's range is
+// enough and its eleven bits beat bf16's eight at the same rate.  One binary16 a number is exact enough for bf16
+// results (a few 2^-12 of the result's norm); for float results a number is a pair of binary16, high and low half, of
+// which three products are taken (high high, high low, low high): 22 bits.
+//
+// A and P are symmetric: only tiles on and below the diagonal are computed, each written to both its places.
+// X stays row-major throughout: X X^T reads rows along their length, and P X reads X through the LDS's
+// transposing reads, so that no transposed copy of X is ever stored.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "inner_internal.h"
+
+namespace noloco {
+namespace {
+
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint16_t ushort4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+
+#define lds_memory __attribute__((address_space(3)))
+
+// 16 bytes a lane from a buffer to the LDS, at `to` + 16 times the lane, past the registers.  The compiler does not count
+// these loads (it would wait for all of them in front of every transposing read): who reads what they bring waits for
+// vmcnt itself.
+__device__ __forceinline__ uint4v buffer_words(const void* p, uint32_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  return uint4v{static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+__device__ __forceinline__ void load_to_lds(uint4v buffer, uint32_t lane_offset, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+               :: "v"(lane_offset), "s"(buffer), "s"(offset), "s"(to) : "memory");
+}
+
+// Enqueue a kernel and return the launch status itself.
+template <typename T> struct same { typedef T type; };
+template <typename... KArgs>
+int enqueue(void (*kernel)(KArgs...), uint32_t grid, uint32_t block, void* stream, typename same<KArgs>::type... args) {
+  void* argv[] = {static_cast<void*>(&args)...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(grid), dim3(block), argv, 0, static_cast<hipStream_t>(stream));
+}
+
+__device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+__device__ __forceinline__ uint16_t narrow(float v) {   // to bf16, nearest, ties to even; NaN stays NaN
+  const uint32_t u = __float_as_uint(v);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return static_cast<uint16_t>((u >> 16) | 0x40u);
+  return static_cast<uint16_t>((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+}
+
+// Which class and item workgroup `group` works on, and which workgroup of the item it is.
+struct Place { uint32_t cls, item, part; };
+__device__ __forceinline__ Place locate(const NsArgs& args, uint32_t group) {
+  uint32_t cls = 0, begin = 0;
+#pragma unroll
+  for (int i = 0; i < kNsClasses - 1; ++i) {
+    const bool past = args.end[i] <= group;
+    cls += past ? 1u : 0u;
+    begin = past ? args.end[i] : begin;
+  }
+  const uint32_t at = group - begin, per = args.cls[cls].per_item;
+  const uint32_t item = at / per;
+  return {cls, item, at - item * per};
+}
+
+// ---------------------------------------------------------------------------
+// Momentum, and the sum of squares of what is orthogonalised
+// ---------------------------------------------------------------------------
+
+template <bool BF16> __device__ __forceinline__ float load_one(const void* p, int64_t i) {
+  if constexpr (BF16) return widen(static_cast<const uint16_t*>(p)[i]);
+  else return static_cast<const float*>(p)[i];
+}
+
+// What is orthogonalised: x, the momentum, or the gradient that looks one step ahead.
+__device__ __forceinline__ float direction(float g, float moved, float mu, bool nesterov) {
+  return nesterov ? g + mu * moved : moved;
+}
+
+// One workgroup sums one chunk of an item: elements chunk * size .. of the matrix in row-major order.
+// Squares are summed in binary64: gradients are small enough for their squares to leave binary32's range.
+template <bool BF16, bool MOMENTUM>
+__global__ __launch_bounds__(256) void ns_sums(NsArgs args, NsArrays arrays) {
+  const Place place = locate(args, blockIdx.x);
+  const NsClass& cls = args.cls[place.cls];
+  const NsItem item = args.items[cls.first_item + place.item];
+  const uint32_t cols = cls.tall ? cls.m : cls.n;
+  const uint64_t total = uint64_t(cls.m) * cls.n;
+  const uint64_t size = (total + cls.per_item - 1) / cls.per_item;
+  const uint64_t begin = place.part * size, end = begin + size < total ? begin + size : total;
+  double sum = 0.;
+  if (begin + threadIdx.x < end) {
+    const uint64_t first = begin + threadIdx.x;
+    uint64_t row = first / cols, col = first - row * cols;
+    const uint32_t step_rows = 256 / cols, step_cols = 256 - step_rows * cols;
+    for (uint64_t e = first; e < end; e += 256) {
+      const int64_t at = item.offset + static_cast<int64_t>(row) * item.row_stride + static_cast<int64_t>(col);
+      float u = load_one<BF16>(arrays.in, at);
+      if constexpr (MOMENTUM) {
+        const float moved = arrays.mu * arrays.momentum[at] + u;
+        arrays.momentum[at] = moved;
+        u = direction(u, moved, arrays.mu, arrays.nesterov != 0);
+      }
+      sum += static_cast<double>(u) * u;
+      row += step_rows;
+      col += step_cols;
+      if (col >= cols) { col -= cols; ++row; }
+    }
+  }
+  __shared__ double part[4];
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    args.sums[uint64_t(cls.first_sum + place.item) * kNsChunks + place.part] = part[0] + part[1] + part[2] + part[3];
+}
+
+// ---------------------------------------------------------------------------
+// X_0
+// ---------------------------------------------------------------------------
+
+// chunks of an item in ns_sums; the same on the host
+__host__ __device__ inline uint32_t chunks_of(uint64_t elements) {
+  const uint64_t c = (elements + kNsChunkElems - 1) / kNsChunkElems;
+  return c < 1 ? 1 : (c > kNsChunks ? kNsChunks : static_cast<uint32_t>(c));
+}
+
+// A workgroup writes a 64 x 64 tile of X_0, zeros where it is padded.
+template <bool BF16, bool MOMENTUM, int PLANES>
+__global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
+  __shared__ float tile[64][65];
+  __shared__ double part[4];
+  const Place place = locate(args, blockIdx.x);
+  const NsClass& cls = args.cls[place.cls];
+  const NsItem item = args.items[cls.first_item + place.item];
+  const uint32_t chunks = chunks_of(uint64_t(cls.m) * cls.n);
+  double sum = threadIdx.x < chunks ? args.sums[uint64_t(cls.first_sum + place.item) * kNsChunks + threadIdx.x] : 0.;
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+
+  const uint32_t across = cls.np / 64;
+  const uint32_t i0 = place.part / across * 64, j0 = place.part % across * 64;     // of X
+  const bool tall = cls.tall != 0;
+  const uint32_t rows = tall ? cls.n : cls.m, cols = tall ? cls.m : cls.n;
+  const uint32_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;                         // of the matrix
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (uint32_t r = wave; r < 64; r += 4) {
+    float u = 0.f;
+    if (r0 + r < rows && c0 + lane < cols) {
+      const int64_t at = item.offset + static_cast<int64_t>(r0 + r) * item.row_stride + c0 + lane;
+      if constexpr (MOMENTUM) {
+        const float moved = arrays.momentum[at];
+        u = arrays.nesterov ? direction(load_one<BF16>(arrays.in, at), moved, arrays.mu, true) : moved;
+      } else {
+        u = load_one<BF16>(arrays.in, at);
+      }
+    }
+    if (tall) tile[lane][r] = u; else tile[r][lane] = u;
+  }
+  __syncthreads();
+  const double norm = sqrt(part[0] + part[1] + part[2] + part[3]) + static_cast<double>(arrays.eps);
+  // A matrix of zeros stays one.
+  const double unit = norm == 0. ? 0. : static_cast<double>(kNsUnit) / norm;
+  char* x = args.workspace + cls.base + place.item * cls.item_bytes;
+  const uint64_t ld = uint64_t(cls.np) * 2 * PLANES;
+  // eight numbers of a row a thread: two rounds
+  for (uint32_t v = threadIdx.x; v < 64 * 8; v += 256) {
+    const uint32_t r = v >> 3, c = (v & 7) * 8;
+    half8 high, low;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float f = static_cast<float>(static_cast<double>(tile[r][c + e]) * unit);
+      high[e] = static_cast<_Float16>(f);
+      low[e] = static_cast<_Float16>(f - static_cast<float>(high[e]));
+    }
+    const uint32_t j = j0 + c;
+    char* at = x + (i0 + r) * ld + (PLANES == 1 ? j * 2 : (j / 32) * 128 + (j % 32) * 2);
+    *reinterpret_cast<half8*>(at) = high;
+    if constexpr (PLANES == 2) *reinterpret_cast<half8*>(at + 64) = low;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The products
+// ---------------------------------------------------------------------------
+
+// Workgroups are dealt to the 8 XCDs in turn; each XCD takes runs of `run` consecutive tiles, which share rows and
+// columns in its L2.
+__device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t blocks, uint32_t run) {
+  const uint32_t whole = blocks / (8 * run) * (8 * run);
+  if (block >= whole) return block;
+  const uint32_t xcd = block & 7u, slot = block >> 3, k = slot / run;
+  return (k * 8 + xcd) * run + (slot - k * run);
+}
+
+// D[r][c] = sum over k of F[r][k] S[c][k], a T x T tile of it.  For A and P F and S are rows of X or A; for P X
+// the second operand is rows of P and the first is columns of X, whose rows lie in the LDS as in memory and are
+// turned by the LDS's transposing reads.  With pairs a row holds 32 high halves, their 32 low halves, the next 32 high
+// ones and so on, so that a stage of 128 bytes of every row is 64 numbers, or 32 pairs.
+//
+// A wave owns a (T / WR) x (T / WC) part in 32 x 32 blocks.  The operands come to the LDS by loads that bypass the
+// registers, two stages deep; fragments are read one slice of 16 k ahead of the products that use them, across the
+// stage's end too: the barrier in front of the last slice's products tells that the next stage has come and that
+// this one's buffer is free.
+//
+// Rows of 128 bytes: 16-byte chunk q of row r lies at q ^ (r >> 1 & 7), so that the 16 lanes that read at once meet
+// 16 different quarters of the 64 banks.  Rows of X in the transposed operand: chunk q of row k at q ^ (k & 3) << 2
+// (shorter rows: q ^ (k >> 1 & 1) << 2), since four lanes of a group of 16 read each of four rows.
+template <int T, int WR, int WC, int KIND, int PLANES, typename Out>
+__global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays arrays, int32_t step, float ca, float cb, float cc, uint32_t run) {
+  constexpr bool kApplies = KIND == kNsApply || KIND == kNsLast;
+  constexpr int kWaves = WR * WC, kThreads = kWaves * 64;
+  constexpr int kDepth = 64 / PLANES;                       // k of a stage
+  constexpr int kSlices = kDepth / 16;
+  constexpr int kOperand = T * 128;                         // bytes of one operand's stage
+  constexpr int kStage = 2 * kOperand;
+  constexpr int MB = T / WR / 32, NB = T / WC / 32;         // a wave's blocks
+  constexpr int kLoads = T / 8 / kWaves;                    // of 1 KiB, of a wave, operand and stage
+  constexpr int kTurned = T * 2 * PLANES;                   // bytes of a row of the transposed operand
+  constexpr int kTurnedRows = 1024 / kTurned > 0 ? 1024 / kTurned : 1;   // rows of one load
+  constexpr int kHalf = T / 2;
+  constexpr int kImageRow = T * 2 * PLANES + 16;            // staged results, bytes of a row
+  constexpr int kImage = kHalf * kImageRow;
+  constexpr int kFloatRow = (T + 4) * 4, kFloatTallRow = (kHalf + 4) * 4;
+  constexpr int kFloats = kHalf * kFloatRow > T * kFloatTallRow ? kHalf * kFloatRow : T * kFloatTallRow;
+  constexpr int kResult = KIND == kNsLast ? kFloats : kImage;
+  constexpr int kLds = 2 * kStage > kResult ? 2 * kStage : kResult;
+  static_assert(kTurned <= 1024 && kLoads >= 1 && kLds <= 160 * 1024, "tile");
+  __shared__ __align__(1024) char lds[kLds];
+
+  const Place place = locate(args, tile_of_block(blockIdx.x, gridDim.x, run));
+  const NsClass& cls = args.cls[place.cls];
+  const uint32_t mp = cls.mp, np = cls.np;
+  const uint64_t x_bytes = uint64_t(mp) * np * 2 * PLANES, a_bytes = uint64_t(mp) * mp * 2 * PLANES;
+  char* const buffers = args.workspace + cls.base + place.item * cls.item_bytes;
+  char* const x = buffers + (step & 1 ? x_bytes : 0);
+  char* const x_next = buffers + (step & 1 ? 0 : x_bytes);
+  char* const gram = buffers + 2 * x_bytes;
+  char* const poly = gram + a_bytes;
+
+  // Tile (r0, c0) of the result, and where it is found in the operands.
+  uint32_t r0, c0;
+  if constexpr (kApplies) {
+    // columns of X by four tiles of rows of P
+    const uint32_t tall_tiles = mp / T, wide_tiles = np / T, band = 4 * wide_tiles;
+    const uint32_t g = place.part / band, in = place.part - g * band;
+    const uint32_t high = tall_tiles - g * 4 < 4 ? tall_tiles - g * 4 : 4;
+    r0 = in / high * T;
+    c0 = (g * 4 + in % high) * T;
+  } else {
+    uint32_t row = static_cast<uint32_t>((sqrtf(8.f * place.part + 1.f) - 1.f) * 0.5f);
+    if ((row + 1) * (row + 2) / 2 <= place.part) ++row;
+    if (row * (row + 1) / 2 > place.part) --row;
+    c0 = row * T;
+    r0 = (place.part - row * (row + 1) / 2) * T;            // r0 <= c0
+  }
+
+  const uint32_t thread = threadIdx.x, lane = thread & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  const uint32_t wr = wave / WC, wc = wave % WC;
+
+  const char* const first = kApplies ? x : (KIND == kNsGram ? x : gram);
+  const char* const second = kApplies ? poly : (KIND == kNsGram ? x : gram);
+  const uint32_t first_ld = (KIND == kNsSquare ? mp : np) * 2 * PLANES, second_ld = (KIND == kNsGram ? np : mp) * 2 * PLANES;
+  const uint32_t first_bytes = static_cast<uint32_t>(KIND == kNsSquare ? a_bytes : x_bytes);
+  const uint32_t second_bytes = static_cast<uint32_t>(KIND == kNsGram ? x_bytes : a_bytes);
+  const uint4v first_buffer = buffer_words(first, first_bytes), second_buffer = buffer_words(second, second_bytes);
+  const uint32_t stages = ((KIND == kNsGram ? cls.n : cls.m) + kDepth - 1) / kDepth;
+
+  // Where a lane's 16 bytes of a load come from.
+  uint32_t plain_first[2], plain_second[2], turned[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t chunk = (lane & 7) ^ (((i << 2) | (lane >> 4)) & 7);
+    plain_first[i] = (lane >> 3) * first_ld + chunk * 16;
+    plain_second[i] = (lane >> 3) * second_ld + chunk * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t in_row = lane * 16 % kTurned, row = lane * 16 / kTurned;
+    const uint32_t k = i * kTurnedRows + row;
+    const uint32_t turn = kTurned >= 256 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
+    turned[i] = row * first_ld + ((in_row >> 4) ^ turn) * 16;
+  }
+  const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_memory char*)lds));
+  auto ask = [&](uint32_t stage) {
+    const uint32_t to = lds_at + (stage & 1) * kStage;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t load = wave * kLoads + i;
+      if constexpr (kApplies)
+        load_to_lds(first_buffer, turned[i & 3], (stage * kDepth + load * kTurnedRows) * first_ld + r0 * 2 * PLANES, to + load * 1024);
+      else
+        load_to_lds(first_buffer, plain_first[(kLoads > 1 ? i : load) & 1], (r0 + load * 8) * first_ld + stage * 128, to + load * 1024);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t load = wave * kLoads + i;
+      load_to_lds(second_buffer, plain_second[(kLoads > 1 ? i : load) & 1], (c0 + load * 8) * second_ld + stage * 128, to + kOperand + load * 1024);
+    }
+  };
+
+  // Where a lane's fragments lie in a stage.
+  const uint32_t fr = lane & 31, fk = lane >> 5;
+  const uint32_t plain_r = (wr * (T / WR) + fr) * 128, plain_c = kOperand + (wc * (T / WC) + fr) * 128;
+  uint32_t turned_at[4];
+  {
+    const uint32_t k = (lane >> 5) * 8 + ((lane >> 2) & 3), byte = (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+    const uint32_t turn = kTurned >= 256 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t of_block = wr * (T / WR) * 2 * PLANES + i * 64 + byte;        // 64 bytes: 32 columns of one plane
+      turned_at[i] = k * kTurned + (((of_block >> 4) ^ turn) << 4) + (of_block & 15);
+    }
+  }
+  struct Fragments { half8 r[PLANES][MB], c[PLANES][NB]; };
+  auto read = [&](uint32_t stage, int slice, Fragments& f) {
+    const char* from = lds + (stage & 1) * kStage;
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) {
+      const uint32_t q = ((p * 4 + slice * 2 + fk) ^ ((fr >> 1) & 7)) * 16;
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        if constexpr (kApplies) {
+          const int b = i * PLANES + p;                      // 64 bytes each
+          const uint32_t at = turned_at[b & 3] + (b >> 2) * 256 + slice * 16 * kTurned;
+          const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(from + at));
+          const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(from + at + 4 * kTurned));
+          const half4 l = __builtin_bit_cast(half4, lo), h = __builtin_bit_cast(half4, hi);
+          f.r[p][i] = __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+          f.r[p][i] = *reinterpret_cast<const half8*>(from + plain_r + i * 4096 + q);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) f.c[p][j] = *reinterpret_cast<const half8*>(from + plain_c + j * 4096 + q);
+    }
+  };
+  float16v acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  auto multiply = [&](const Fragments& f) {
+    if constexpr (PLANES == 2) {
+      // the small products first
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.r[1][i], f.c[0][j], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.r[0][i], f.c[1][j], acc[i][j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.r[0][i], f.c[0][j], acc[i][j], 0, 0, 0);
+  };
+
+  ask(0);
+  if (stages > 1) {
+    ask(1);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+  } else {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  __builtin_amdgcn_s_barrier();
+  Fragments even, odd;
+  read(0, 0, even);
+  for (uint32_t s = 0; s < stages; ++s) {
+#pragma unroll
+    for (int slice = 0; slice < kSlices; ++slice) {
+      Fragments& now = slice & 1 ? odd : even;
+      Fragments& next = slice & 1 ? even : odd;
+      if (slice + 1 < kSlices) {
+        read(s, slice + 1, next);
+      } else {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        if (s + 2 < stages) ask(s + 2);
+        if (s + 1 < stages) read(s + 1, 0, next);
+      }
+      multiply(now);
+    }
+  }
+
+  // A wave's results go through the LDS, half of the tile's columns at a time, and from there in whole lines.
+  // Block (i, j), element e of a lane: r = 32 i + 8 (e / 4) + 4 fk + e % 4, c = 32 j + fr.
+  const uint32_t r_of = wr * (T / WR) + 4 * fk, c_of = (wc % (WC / 2)) * (T / WC) + fr;
+  if constexpr (KIND != kNsLast) {
+    char* const to = KIND == kNsGram ? gram : (KIND == kNsSquare ? poly : x_next);
+    const uint64_t to_ld = uint64_t(KIND == kNsApply ? np : mp) * 2 * PLANES;
+    // X and A are held in units of 2^-13, P of 2^-12
+    if constexpr (KIND == kNsSquare) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const uint32_t r = r0 + r_of + i * 32 + e * 2, c = c0 + wc * (T / WC) + fr + j * 32;
+            const char* from = gram + c * to_ld + (PLANES == 1 ? r * 2 : (r / 32) * 128 + (r % 32) * 2);
+            const half4 high = *reinterpret_cast<const half4*>(from);
+            half4 low;
+            if constexpr (PLANES == 2) low = *reinterpret_cast<const half4*>(from + 64);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float v = static_cast<float>(high[k]);
+              if constexpr (PLANES == 2) v += static_cast<float>(low[k]);
+              acc[i][j][e + k] = cc * (acc[i][j][e + k] * (kNsUnitP / (kNsUnit * kNsUnit))) + cb * (v * (kNsUnitP / kNsUnit)) +
+                                 (r + k == c ? ca * kNsUnitP : 0.f);
+            }
+          }
+    }
+    constexpr float kUnit = KIND == kNsGram ? 1.f / kNsUnit : (KIND == kNsSquare ? 1.f : 1.f / kNsUnitP);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __syncthreads();
+      if (wc / (WC / 2) == h) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const uint32_t r = r_of + i * 32 + e * 2;
+              char* at = lds + (c_of + j * 32) * kImageRow + (PLANES == 1 ? r * 2 : (r / 32) * 128 + (r % 32) * 2);
+              half4 high, low;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float v = acc[i][j][e + k] * kUnit;
+                high[k] = static_cast<_Float16>(v);
+                low[k] = static_cast<_Float16>(v - static_cast<float>(high[k]));
+              }
+              *reinterpret_cast<half4*>(at) = high;
+              if constexpr (PLANES == 2) *reinterpret_cast<half4*>(at + 64) = low;
+            }
+      }
+      __syncthreads();
+      // rows of the result's transpose, as they lie
+      constexpr int kChunks = T * 2 * PLANES / 16;
+      for (uint32_t v = thread; v < kHalf * kChunks; v += kThreads) {
+        const uint32_t row = v / kChunks, chunk = v % kChunks;
+        const uint4v data = *reinterpret_cast<const uint4v*>(lds + row * kImageRow + chunk * 16);
+        *reinterpret_cast<uint4v*>(to + uint64_t(c0 + h * kHalf + row) * to_ld + r0 * 2 * PLANES + chunk * 16) = data;
+      }
+      if constexpr (!kApplies) {
+        // and the result itself, through the transposing reads: a wave takes 16 rows of 32 columns
+        if (r0 != c0)
+          for (uint32_t v = wave; v < (T / 16) * (kHalf / 32); v += kWaves) {
+            const uint32_t rb = v / (kHalf / 32) * 16, cb32 = v % (kHalf / 32) * 32;
+            const uint32_t c = cb32 + (lane >> 4) * 8 + ((lane >> 2) & 3);
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+              const uint32_t at = c * kImageRow + (PLANES == 1 ? rb * 2 : (rb / 32) * 128 + (rb % 32) * 2 + p * 64) + (lane & 3) * 8;
+              const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(lds + at));
+              const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(lds + at + 4 * kImageRow));
+              const uint32_t row = r0 + rb + (lane & 15), col = c0 + h * kHalf + cb32 + (lane >> 4) * 8;
+              char* out = to + row * to_ld + (PLANES == 1 ? col * 2 : (col / 32) * 128 + (col % 32) * 2 + p * 64);
+              typedef short short8v __attribute__((ext_vector_type(8)));
+              *reinterpret_cast<short8v*>(out) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+          }
+      }
+    }
+  } else {
+    // r counts X's columns (the long side), c its rows.  A tall matrix has r as its row.
+    const NsItem item = args.items[cls.first_item + place.item];
+    const bool tall = cls.tall != 0;
+    Out* const out = static_cast<Out*>(arrays.out) + item.offset;
+    const bool vectors = ((reinterpret_cast<uintptr_t>(out) / sizeof(Out)) | static_cast<uint64_t>(item.row_stride)) % 4 == 0;
+    const float by = arrays.lr * item.scale;
+    const bool update = arrays.update != 0;
+    auto put = [&](Out* at, float v) {
+      if (update) {
+        float old;
+        if constexpr (sizeof(Out) == 2) old = widen(*at); else old = *at;
+        v = old * arrays.keep - by * v;
+      }
+      if constexpr (sizeof(Out) == 2) *at = narrow(v); else *at = v;
+    };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __syncthreads();
+      if (wc / (WC / 2) == h) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const uint32_t r = r_of + i * 32 + e * 2, c = c_of + j * 32;
+              float4v v;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[k] = acc[i][j][e + k] * (1.f / (kNsUnit * kNsUnitP));
+              if (!tall) {
+                *reinterpret_cast<float4v*>(lds + c * kFloatRow + r * 4) = v;
+              } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) *reinterpret_cast<float*>(lds + (r + k) * kFloatTallRow + c * 4) = v[k];
+              }
+            }
+      }
+      __syncthreads();
+      const uint32_t wide = tall ? kHalf : T, high = tall ? T : kHalf, lds_row = tall ? kFloatTallRow : kFloatRow;
+      const uint32_t row0 = tall ? r0 : c0 + h * kHalf, col0 = tall ? c0 + h * kHalf : r0;
+      const uint32_t rows = tall ? cls.n : cls.m, cols = tall ? cls.m : cls.n;
+      if (vectors) {
+        for (uint32_t v = thread; v < high * (wide / 4); v += kThreads) {
+          const uint32_t r = v / (wide / 4), c = v % (wide / 4) * 4;
+          if (row0 + r >= rows || col0 + c >= cols) continue;
+          const float4v d = *reinterpret_cast<const float4v*>(lds + r * lds_row + c * 4);
+          Out* at = out + static_cast<int64_t>(row0 + r) * item.row_stride + col0 + c;
+          if (col0 + c + 4 <= cols) {
+            typedef Out out4 __attribute__((ext_vector_type(4)));
+            out4 got;
+            if (update) got = *reinterpret_cast<const out4*>(at);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float value = d[k];
+              if (update) {
+                float old;
+                if constexpr (sizeof(Out) == 2) old = widen(got[k]); else old = got[k];
+                value = old * arrays.keep - by * value;
+              }
+              if constexpr (sizeof(Out) == 2) got[k] = narrow(value); else got[k] = value;
+            }
+            *reinterpret_cast<out4*>(at) = got;
+          } else {
+            for (int k = 0; k < 4 && col0 + c + k < cols; ++k) put(at + k, d[k]);
+          }
+        }
+      } else {
+        for (uint32_t v = thread; v < high * wide; v += kThreads) {
+          const uint32_t r = v / wide, c = v % wide;
+          if (row0 + r >= rows || col0 + c >= cols) continue;
+          put(out + static_cast<int64_t>(row0 + r) * item.row_stride + col0 + c, *reinterpret_cast<const float*>(lds + r * lds_row + c * 4));
+        }
+      }
+    }
+  }
+}
+
+template <int T, int WR, int WC, int PLANES>
+int launch_product(const NsArgs& args, const NsArrays& arrays, int kind, int step, float a, float b, float c, uint32_t run,
+                   uint32_t workgroups, void* stream) {
+  constexpr uint32_t kThreads = WR * WC * 64;
+  switch (kind) {
+    case kNsGram: return enqueue(ns_product<T, WR, WC, kNsGram, PLANES, float>, workgroups, kThreads, stream, args, arrays, step, a, b, c, run);
+    case kNsSquare: return enqueue(ns_product<T, WR, WC, kNsSquare, PLANES, float>, workgroups, kThreads, stream, args, arrays, step, a, b, c, run);
+    case kNsApply: return enqueue(ns_product<T, WR, WC, kNsApply, PLANES, float>, workgroups, kThreads, stream, args, arrays, step, a, b, c, run);
+    default:
+      return arrays.out_bf16 ? enqueue(ns_product<T, WR, WC, kNsLast, PLANES, uint16_t>, workgroups, kThreads, stream, args, arrays, step, a, b, c, run)
+                             : enqueue(ns_product<T, WR, WC, kNsLast, PLANES, float>, workgroups, kThreads, stream, args, arrays, step, a, b, c, run);
+  }
+}
+
+}  // namespace
+
+int launch_ns_sums(const NsArgs& args, const NsArrays& arrays, uint32_t workgroups, void* stream) {
+  if (arrays.momentum != nullptr)
+    return arrays.in_bf16 ? enqueue(ns_sums<true, true>, workgroups, 256, stream, args, arrays)
+                          : enqueue(ns_sums<false, true>, workgroups, 256, stream, args, arrays);
+  return arrays.in_bf16 ? enqueue(ns_sums<true, false>, workgroups, 256, stream, args, arrays)
+                        : enqueue(ns_sums<false, false>, workgroups, 256, stream, args, arrays);
+}
+
+int launch_ns_start(const NsArgs& args, const NsArrays& arrays, int planes, uint32_t workgroups, void* stream) {
+  auto pick = [&](auto one, auto two) { return enqueue(planes == 1 ? one : two, workgroups, 256, stream, args, arrays); };
+  if (arrays.momentum != nullptr)
+    return arrays.in_bf16 ? pick(ns_start<true, true, 1>, ns_start<true, true, 2>) : pick(ns_start<false, true, 1>, ns_start<false, true, 2>);
+  return arrays.in_bf16 ? pick(ns_start<true, false, 1>, ns_start<true, false, 2>) : pick(ns_start<false, false, 1>, ns_start<false, false, 2>);
+}
+
+int launch_ns_product(const NsArgs& args, const NsArrays& arrays, int kind, int tile, int planes, int step,
+                      float a, float b, float c, uint32_t workgroups, void* stream) {
+  if (tile == 256)
+    return planes == 1 ? launch_product<256, 2, 4, 1>(args, arrays, kind, step, a, b, c, 32, workgroups, stream)
+                       : launch_product<256, 2, 4, 2>(args, arrays, kind, step, a, b, c, 32, workgroups, stream);
+  if (tile == 128)
+    return planes == 1 ? launch_product<128, 2, 2, 1>(args, arrays, kind, step, a, b, c, 64, workgroups, stream)
+                       : launch_product<128, 2, 2, 2>(args, arrays, kind, step, a, b, c, 64, workgroups, stream);
+  return planes == 1 ? launch_product<64, 2, 2, 1>(args, arrays, kind, step, a, b, c, 64, workgroups, stream)
+                     : launch_product<64, 2, 2, 2>(args, arrays, kind, step, a, b, c, 64, workgroups, stream);
+}
+
+}  // namespace noloco
