@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 #include <limits>
 #include <memory>
 #include <new>
@@ -18,6 +19,7 @@ using noloco::NsArgs;
 using noloco::NsArrays;
 using noloco::NsClass;
 using noloco::NsItem;
+using noloco::NsTable;
 
 constexpr int64_t kDefaultWorkspace = 4ll << 30;
 constexpr int64_t kMostNumbers = 1ll << 28, kMostSide = 1ll << 22, kMostItems = 1ll << 24;
@@ -47,11 +49,12 @@ struct Shape {
   uint64_t item_bytes(int planes) const { return noloco::ns_item_bytes(mp(), np(), planes); }
 };
 
-// What goes through the products together, with its launches' arguments.
+// What goes through the products together: where the tables of its launches are among all of them, and their workgroups.
+enum { kSums, kStart, kSymmetric, kApply, kTables };
 struct Batch {
   int tile;
-  NsArgs sums, start, symmetric, apply;
-  uint32_t sums_groups, start_groups, symmetric_groups, apply_groups;
+  uint32_t first_table;
+  uint32_t groups[kTables];
 };
 
 // The tile that takes the least time by a rough model: a workgroup's share of the rate that products of this tile reach
@@ -81,7 +84,11 @@ struct noloco_muon_plan {
   int64_t elements = 0;
   int64_t workspace_bytes = 0;
   std::vector<Batch> batches[2];     // one binary16 a number, pairs
-  char* block = nullptr;             // the one device allocation: items, sums, workspace
+  const NsTable* tables = nullptr;   // these four point into the block
+  const NsItem* items = nullptr;
+  double* sums = nullptr;
+  char* workspace = nullptr;
+  char* block = nullptr;             // the one device allocation
 
   noloco_muon_plan() = default;
   noloco_muon_plan(const noloco_muon_plan&) = delete;
@@ -125,36 +132,32 @@ noloco_status check_overlap(const std::vector<noloco_matrix>& matrices) {
   return NOLOCO_OK;
 }
 
-// Splits the items of all shapes into batches that fit `room` bytes and a launch's table of classes.
-void make_batches(const std::vector<Shape>& shapes, int planes, uint64_t room, std::vector<Batch>* out) {
+// Splits the items of all shapes into batches that fit `room` bytes and a launch's table of classes.  Returns the most items
+// that a batch has.
+uint32_t make_batches(const std::vector<Shape>& shapes, int planes, uint64_t room, std::vector<Batch>* out, std::vector<NsTable>* tables) {
   size_t shape = 0;
-  uint32_t done = 0;      // of that shape's items
+  uint32_t done = 0, most = 0;      // of that shape's items; of a batch
   while (shape < shapes.size()) {
-    Batch b;
+    Batch b{};
     b.tile = shapes[shape].tile;
-    b.sums_groups = b.start_groups = b.symmetric_groups = b.apply_groups = 0;
-    uint64_t used = 0;
-    uint32_t first_sum = 0;
-    int classes = 0;
-    for (NsArgs* a : {&b.sums, &b.start, &b.symmetric, &b.apply}) {
-      a->items = nullptr;
-      a->workspace = nullptr;
-      a->sums = nullptr;
-      for (int i = 0; i < noloco::kNsClasses; ++i) {
-        a->end[i] = 0xffffffffu;
-        a->cls[i] = NsClass{};
-      }
+    b.first_table = static_cast<uint32_t>(tables->size());
+    NsTable table[kTables];
+    for (NsTable& t : table) {
+      std::fill(t.end, t.end + noloco::kNsClasses, 0xffffffffu);
+      std::fill(t.cls, t.cls + noloco::kNsClasses, NsClass{});
     }
+    uint64_t used = 0;
+    uint32_t items = 0;
+    int classes = 0;
     while (shape < shapes.size() && shapes[shape].tile == b.tile && classes < noloco::kNsClasses) {
       const Shape& s = shapes[shape];
       const uint64_t each = s.item_bytes(planes), elements = uint64_t(s.rows) * s.cols;
       const uint32_t mt = s.mp() / b.tile, nt = s.np() / b.tile;
       const uint32_t chunks = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>((elements + noloco::kNsChunkElems - 1) / noloco::kNsChunkElems, 1), noloco::kNsChunks));
-      const uint32_t per[4] = {chunks, s.mp() / 64 * (s.np() / 64), mt * (mt + 1) / 2, mt * nt};
-      uint32_t* groups[4] = {&b.sums_groups, &b.start_groups, &b.symmetric_groups, &b.apply_groups};
+      const uint32_t per[kTables] = {chunks, s.mp() / 64 * (s.np() / 64), mt * (mt + 1) / 2, mt * nt};
       uint64_t fit = std::min<uint64_t>(s.items - done, (room - used) / each);
-      for (int k = 0; k < 4; ++k) {
-        const uint64_t left = *groups[k] < kMostGroups ? kMostGroups - *groups[k] : 0;
+      for (int k = 0; k < kTables; ++k) {
+        const uint64_t left = b.groups[k] < kMostGroups ? kMostGroups - b.groups[k] : 0;
         fit = std::min(fit, std::max<uint64_t>(left / per[k], used == 0 ? 1 : 0));
       }
       if (fit == 0) break;
@@ -162,39 +165,28 @@ void make_batches(const std::vector<Shape>& shapes, int planes, uint64_t room, s
       c.base = used;
       c.item_bytes = each;
       c.first_item = s.first_item + done;
-      c.first_sum = first_sum;
+      c.first_sum = items;
       c.m = s.m();
       c.n = s.n();
       c.mp = s.mp();
       c.np = s.np();
       c.tall = s.rows > s.cols ? 1 : 0;
-      NsArgs* args[4] = {&b.sums, &b.start, &b.symmetric, &b.apply};
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kTables; ++k) {
         c.per_item = per[k];
-        *groups[k] += per[k] * static_cast<uint32_t>(fit);
-        args[k]->cls[classes] = c;
-        args[k]->end[classes] = *groups[k];
+        b.groups[k] += per[k] * static_cast<uint32_t>(fit);
+        table[k].cls[classes] = c;
+        table[k].end[classes] = b.groups[k];
       }
       ++classes;
       used += each * fit;
-      first_sum += static_cast<uint32_t>(fit);
+      items += static_cast<uint32_t>(fit);
       done += static_cast<uint32_t>(fit);
       if (done < s.items) break;
       ++shape;
       done = 0;
     }
     out->push_back(b);
-  }
-}
-
-uint32_t most_items(const std::vector<Batch>& batches) {
-  uint32_t most = 0;
-  for (const Batch& b : batches) {
-    uint32_t items = 0, last = 0;
-    for (int i = 0; i < noloco::kNsClasses && b.sums.end[i] != 0xffffffffu; ++i) {
-      items += (b.sums.end[i] - last) / b.sums.cls[i].per_item;
-      last = b.sums.end[i];
-    }
+    tables->insert(tables->end(), table, table + kTables);
     most = std::max(most, items);
   }
   return most;
@@ -255,24 +247,32 @@ noloco_status create_muon_plan(const noloco_matrix* given, int32_t num, int64_t 
   }
   const uint64_t room = std::max(largest, std::min(all, static_cast<uint64_t>(workspace > 0 ? workspace : kDefaultWorkspace)));
   plan->workspace_bytes = static_cast<int64_t>(room);
-  for (int planes = 1; planes <= 2; ++planes) make_batches(shapes, planes, room, &plan->batches[planes - 1]);
-  const uint64_t sums = std::max(most_items(plan->batches[0]), most_items(plan->batches[1]));
-  auto whole = [](uint64_t bytes) { return (bytes + 4095) / 4096 * 4096; };
-  const uint64_t item_bytes = whole(items.size() * sizeof(NsItem)), sum_bytes = whole(sums * noloco::kNsChunks * sizeof(double));
+  std::vector<NsTable> tables;
+  uint32_t summed = 0;
+  for (int planes = 1; planes <= 2; ++planes)
+    summed = std::max(summed, make_batches(shapes, planes, room, &plan->batches[planes - 1], &tables));
+  // Tables and items, filled by one copy; then the sums and the workspace.
+  std::vector<char> host;
+  auto append = [&host](const void* data, size_t bytes) {
+    const size_t at = host.size();
+    host.resize((at + bytes + 4095) / 4096 * 4096);
+    if (bytes > 0) std::memcpy(host.data() + at, data, bytes);
+    return at;
+  };
+  const size_t tables_at = append(tables.data(), tables.size() * sizeof(NsTable));
+  const size_t items_at = append(items.data(), items.size() * sizeof(NsItem));
+  const uint64_t sum_bytes = (uint64_t(summed) * noloco::kNsChunks * sizeof(double) + 4095) / 4096 * 4096;
   if (hipGetDevice(&plan->device) != hipSuccess ||
-      hipMalloc(reinterpret_cast<void**>(&plan->block), item_bytes + sum_bytes + room + 4096) != hipSuccess) {
+      hipMalloc(reinterpret_cast<void**>(&plan->block), host.size() + sum_bytes + room + 4096) != hipSuccess) {
     plan->block = nullptr;
     return NOLOCO_ERR_DEVICE;
   }
-  if (!items.empty() && hipMemcpy(plan->block, items.data(), items.size() * sizeof(NsItem), hipMemcpyHostToDevice) != hipSuccess)
+  if (!host.empty() && hipMemcpy(plan->block, host.data(), host.size(), hipMemcpyHostToDevice) != hipSuccess)
     return NOLOCO_ERR_DEVICE;
-  for (std::vector<Batch>& batches : plan->batches)
-    for (Batch& b : batches)
-      for (NsArgs* a : {&b.sums, &b.start, &b.symmetric, &b.apply}) {
-        a->items = reinterpret_cast<const NsItem*>(plan->block);
-        a->sums = reinterpret_cast<double*>(plan->block + item_bytes);
-        a->workspace = plan->block + item_bytes + sum_bytes;
-      }
+  plan->tables = reinterpret_cast<const NsTable*>(plan->block + tables_at);
+  plan->items = reinterpret_cast<const NsItem*>(plan->block + items_at);
+  plan->sums = reinterpret_cast<double*>(plan->block + host.size());
+  plan->workspace = plan->block + host.size() + sum_bytes;
   *out = plan.release();
   return NOLOCO_OK;
 }
@@ -313,15 +313,17 @@ noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, 
                                                                     : (arrays.out_bf16 ? NOLOCO_PRODUCTS_F16 : NOLOCO_PRODUCTS_PAIRS);
   const int planes = products == NOLOCO_PRODUCTS_F16 ? 1 : 2;
   for (const Batch& b : plan->batches[planes - 1]) {
-    if (noloco::launch_ns_sums(b.sums, arrays, b.sums_groups, stream) != 0) return NOLOCO_ERR_DEVICE;
-    if (noloco::launch_ns_start(b.start, arrays, planes, b.start_groups, stream) != 0) return NOLOCO_ERR_DEVICE;
+    auto args = [&](int table) { return NsArgs{plan->tables + b.first_table + table, plan->items, plan->workspace, plan->sums}; };
+    if (noloco::launch_ns_sums(args(kSums), arrays, b.groups[kSums], stream) != 0) return NOLOCO_ERR_DEVICE;
+    if (noloco::launch_ns_start(args(kStart), arrays, planes, b.groups[kStart], stream) != 0) return NOLOCO_ERR_DEVICE;
     for (int32_t s = 0; s < method->steps; ++s) {
-      const float *k = method->coefficients + 3 * s;
-      const int last = s + 1 == method->steps ? noloco::kNsLast : noloco::kNsApply;
-      if (noloco::launch_ns_product(b.symmetric, arrays, noloco::kNsGram, b.tile, planes, s, k[0], k[1], k[2], b.symmetric_groups, stream) != 0 ||
-          noloco::launch_ns_product(b.symmetric, arrays, noloco::kNsSquare, b.tile, planes, s, k[0], k[1], k[2], b.symmetric_groups, stream) != 0 ||
-          noloco::launch_ns_product(b.apply, arrays, last, b.tile, planes, s, k[0], k[1], k[2], b.apply_groups, stream) != 0)
-        return NOLOCO_ERR_DEVICE;
+      const float* k = method->coefficients + 3 * s;
+      const int kinds[3] = {noloco::kNsGram, noloco::kNsSquare, s + 1 == method->steps ? noloco::kNsLast : noloco::kNsApply};
+      for (int kind : kinds) {
+        const int table = kind == noloco::kNsGram || kind == noloco::kNsSquare ? kSymmetric : kApply;
+        if (noloco::launch_ns_product(args(table), arrays, kind, b.tile, planes, s, k[0], k[1], k[2], b.groups[table], stream) != 0)
+          return NOLOCO_ERR_DEVICE;
+      }
     }
   }
   return NOLOCO_OK;

@@ -37,9 +37,12 @@ typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 // vmcnt itself.
 __device__ __forceinline__ uint4v buffer_words(const void* p, uint32_t bytes) {
   const uint64_t at = reinterpret_cast<uint64_t>(p);
-  return uint4v{static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32) & 0xffffu, bytes, 0x00020000u};
+  auto same = [](uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v))); };
+  return uint4v{same(static_cast<uint32_t>(at)), same(static_cast<uint32_t>(at >> 32) & 0xffffu), same(bytes), 0x00020000u};
 }
 __device__ __forceinline__ void load_to_lds(uint4v buffer, uint32_t lane_offset, uint32_t offset, uint32_t to) {
+  offset = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(offset)));
+  to = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(to)));
   asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
                :: "v"(lane_offset), "s"(buffer), "s"(offset), "s"(to) : "memory");
 }
@@ -59,19 +62,31 @@ __device__ __forceinline__ uint16_t narrow(float v) {   // to bf16, nearest, tie
   return static_cast<uint16_t>((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
 }
 
+// Tables that no kernel writes are read through the scalar cache.
+#define scalar_memory __attribute__((address_space(4)))
+__device__ __forceinline__ NsItem item_at(const NsArgs& args, uint32_t i) {
+  const scalar_memory NsItem* p = (const scalar_memory NsItem*)args.items + i;
+  return {p->offset, p->row_stride, p->scale, 0};
+}
+
 // Which class and item workgroup `group` works on, and which workgroup of the item it is.
-struct Place { uint32_t cls, item, part; };
+struct Place { NsClass cls; uint32_t item, part; };
 __device__ __forceinline__ Place locate(const NsArgs& args, uint32_t group) {
+  const scalar_memory NsTable* table = (const scalar_memory NsTable*)args.table;
   uint32_t cls = 0, begin = 0;
 #pragma unroll
   for (int i = 0; i < kNsClasses - 1; ++i) {
-    const bool past = args.end[i] <= group;
+    const uint32_t end = table->end[i];
+    const bool past = end <= group;
     cls += past ? 1u : 0u;
-    begin = past ? args.end[i] : begin;
+    begin = past ? end : begin;
   }
-  const uint32_t at = group - begin, per = args.cls[cls].per_item;
-  const uint32_t item = at / per;
-  return {cls, item, at - item * per};
+  const scalar_memory NsClass* c = table->cls + cls;
+  Place p{{c->base, c->item_bytes, c->per_item, c->first_item, c->first_sum, c->m, c->n, c->mp, c->np, c->tall}, 0, 0};
+  const uint32_t at = group - begin;
+  p.item = at / p.cls.per_item;
+  p.part = at - p.item * p.cls.per_item;
+  return p;
 }
 
 // ---------------------------------------------------------------------------
@@ -93,8 +108,8 @@ __device__ __forceinline__ float direction(float g, float moved, float mu, bool 
 template <bool BF16, bool MOMENTUM>
 __global__ __launch_bounds__(256) void ns_sums(NsArgs args, NsArrays arrays) {
   const Place place = locate(args, blockIdx.x);
-  const NsClass& cls = args.cls[place.cls];
-  const NsItem item = args.items[cls.first_item + place.item];
+  const NsClass& cls = place.cls;
+  const NsItem item = item_at(args, cls.first_item + place.item);
   const uint32_t cols = cls.tall ? cls.m : cls.n;
   const uint64_t total = uint64_t(cls.m) * cls.n;
   const uint64_t size = (total + cls.per_item - 1) / cls.per_item;
@@ -142,8 +157,8 @@ __global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
   __shared__ float tile[64][65];
   __shared__ double part[4];
   const Place place = locate(args, blockIdx.x);
-  const NsClass& cls = args.cls[place.cls];
-  const NsItem item = args.items[cls.first_item + place.item];
+  const NsClass& cls = place.cls;
+  const NsItem item = item_at(args, cls.first_item + place.item);
   const uint32_t chunks = chunks_of(uint64_t(cls.m) * cls.n);
   double sum = threadIdx.x < chunks ? args.sums[uint64_t(cls.first_sum + place.item) * kNsChunks + threadIdx.x] : 0.;
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
@@ -195,6 +210,9 @@ __global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
 // The products
 // ---------------------------------------------------------------------------
 
+struct Yes { constexpr operator bool() const { return true; } };
+struct No { constexpr operator bool() const { return false; } };
+
 // Workgroups are dealt to the 8 XCDs in turn; each XCD takes runs of `run` consecutive tiles, which share rows and
 // columns in its L2.
 __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t blocks, uint32_t run) {
@@ -240,7 +258,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   __shared__ __align__(1024) char lds[kLds];
 
   const Place place = locate(args, tile_of_block(blockIdx.x, gridDim.x, run));
-  const NsClass& cls = args.cls[place.cls];
+  const NsClass& cls = place.cls;
   const uint32_t mp = cls.mp, np = cls.np;
   const uint64_t x_bytes = uint64_t(mp) * np * 2 * PLANES, a_bytes = uint64_t(mp) * mp * 2 * PLANES;
   char* const buffers = args.workspace + cls.base + place.item * cls.item_bytes;
@@ -262,6 +280,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
     uint32_t row = static_cast<uint32_t>((sqrtf(8.f * place.part + 1.f) - 1.f) * 0.5f);
     if ((row + 1) * (row + 2) / 2 <= place.part) ++row;
     if (row * (row + 1) / 2 > place.part) --row;
+    row = __builtin_amdgcn_readfirstlane(row);
     c0 = row * T;
     r0 = (place.part - row * (row + 1) / 2) * T;            // r0 <= c0
   }
@@ -382,7 +401,8 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   __builtin_amdgcn_s_barrier();
   Fragments even, odd;
   read(0, 0, even);
-  for (uint32_t s = 0; s < stages; ++s) {
+  // The last two stages by themselves, so that nothing in the loop is conditional.
+  auto stage = [&](uint32_t s, auto ask_more, auto read_next) {
 #pragma unroll
     for (int slice = 0; slice < kSlices; ++slice) {
       Fragments& now = slice & 1 ? odd : even;
@@ -392,12 +412,18 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
       } else {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
-        if (s + 2 < stages) ask(s + 2);
-        if (s + 1 < stages) read(s + 1, 0, next);
+        if constexpr (read_next) read(s + 1, 0, next);
+        if constexpr (ask_more) ask(s + 2);
       }
       multiply(now);
+      // the products of a slice stay behind its reads, which the compiler would put in front of the next barrier
+      if constexpr (T == 256 && PLANES == 1) __builtin_amdgcn_sched_barrier(0);
     }
-  }
+  };
+  uint32_t s = 0;
+  for (; s + 2 < stages; ++s) stage(s, Yes{}, Yes{});
+  if (s + 1 < stages) stage(s++, No{}, Yes{});
+  stage(s, No{}, No{});
 
   // A wave's results go through the LDS, half of the tile's columns at a time, and from there in whole lines.
   // Block (i, j), element e of a lane: r = 32 i + 8 (e / 4) + 4 fk + e % 4, c = 32 j + fr.
@@ -480,7 +506,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
     }
   } else {
     // r counts X's columns (the long side), c its rows.  A tall matrix has r as its row.
-    const NsItem item = args.items[cls.first_item + place.item];
+    const NsItem item = item_at(args, cls.first_item + place.item);
     const bool tall = cls.tall != 0;
     Out* const out = static_cast<Out*>(arrays.out) + item.offset;
     const bool vectors = ((reinterpret_cast<uintptr_t>(out) / sizeof(Out)) | static_cast<uint64_t>(item.row_stride)) % 4 == 0;

@@ -79,12 +79,12 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
     CHECK(launch.groups > 0 && launch.groups <= (1u << 22) + (1u << 21));
     uint32_t last = 0;
     uint64_t end_of_last = 0;
-    for (int i = 0; i < kNsClasses && launch.args.end[i] != 0xffffffffu; ++i) {
-      const NsClass& c = launch.args.cls[i];
-      const uint32_t groups = launch.args.end[i] - last;
+    for (int i = 0; i < kNsClasses && launch.args.table->end[i] != 0xffffffffu; ++i) {
+      const NsClass& c = launch.args.table->cls[i];
+      const uint32_t groups = launch.args.table->end[i] - last;
       CHECK(groups > 0 && groups % c.per_item == 0);
       const uint32_t items = groups / c.per_item;
-      last = launch.args.end[i];
+      last = launch.args.table->end[i];
       CHECK(c.m <= c.n && c.mp >= c.m && c.np >= c.n && c.mp % 64 == 0 && c.np % 64 == 0);
       CHECK(ns_x_bytes(c.mp, c.np, planes) >> 32 == 0);
       CHECK(c.item_bytes == ns_item_bytes(c.mp, c.np, planes) && c.base >= end_of_last);
