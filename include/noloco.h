@@ -316,6 +316,9 @@ typedef struct noloco_matrix {
   float scale;             /* noloco_muon_step: its learning rate is lr * scale */
 } noloco_matrix;
 
+/* Most steps of a Newton-Schulz orthogonalisation. */
+#define NOLOCO_MAX_NEWTON_SCHULZ_STEPS 32
+
 /* How products take their operands (sums are always binary32).
  *   F16    one binary16 a number: results to a few 2^-12 of their norm, what a bf16 result needs
  *   PAIRS  a pair of binary16 (high and low half, 22 bits) and three products for each: a float result's last bits
@@ -327,7 +330,7 @@ typedef enum noloco_products { NOLOCO_PRODUCTS_AUTO = 0, NOLOCO_PRODUCTS_F16 = 1
  *   X_0 = U / (|U|_F + eps);   step s:  A = X X^T,  X <- (a_s + b_s A + c_s A^2) X
  * which takes every singular value x of X to x (a + b x^2 + c x^4), for suitable coefficients towards 1.
  * A matrix of zeros gives zeros; a NaN or an infinity in U makes all of its result NaN (and of no other matrix).
- *   steps         >= 1
+ *   steps         1 to NOLOCO_MAX_NEWTON_SCHULZ_STEPS (NOLOCO_ERR_UNSUPPORTED beyond)
  *   coefficients  host, float[3 * steps]: a, b, c of every step.  Starting from singular values up to 1, every step
  *                 must keep a + b x^2 + c x^4 within +-15.5 and its results within 2.79 (what binary16 has room
  *                 for), else NOLOCO_ERR_UNSUPPORTED; NaN or infinite ones give NOLOCO_ERR_INVALID_ARG

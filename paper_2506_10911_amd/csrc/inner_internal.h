@@ -16,9 +16,12 @@ constexpr int kNsClasses = 32;
 constexpr int kNsChunks = 256;          // partial sums of squares of one matrix
 constexpr int kNsChunkElems = 8192;     // elements that a workgroup sums, as long as kNsChunks of them are enough
 
-// X and A are held times 2^13, P times 2^12, so that binary16 has room for what they can be (A's eigenvalues up to
-// kNsMostA, P's up to kNsMostP) and the low halves of pairs are not subnormal.
-constexpr float kNsUnit = 8192.f, kNsUnitP = 4096.f;
+// X, A and P are held times powers of two, so that binary16 has room for what they can be (A's eigenvalues up to kNsMostA,
+// P's up to kNsMostP).  One binary16 a number: units in which X X^T comes out as A is held, and P X as X is.  Pairs: larger
+// ones, or the low halves would be subnormal.
+constexpr float ns_unit_x(int planes) { return planes == 1 ? 64.f : 8192.f; }
+constexpr float ns_unit_a(int planes) { return planes == 1 ? 4096.f : 8192.f; }
+constexpr float ns_unit_p(int planes) { return planes == 1 ? 1.f : 4096.f; }
 constexpr double kNsMostA = 7.8, kNsMostP = 15.5;
 
 // A worker's copy of a matrix.
@@ -58,6 +61,23 @@ struct NsArgs {
 inline uint64_t ns_x_bytes(uint32_t mp, uint32_t np, int planes) { return uint64_t(mp) * np * 2 * planes; }
 inline uint64_t ns_item_bytes(uint32_t mp, uint32_t np, int planes) { return 2 * (ns_x_bytes(mp, np, planes) + ns_x_bytes(mp, mp, planes)); }
 
+// A matrix whose X, A and P fit a CU's LDS goes through all steps in one workgroup: rows padded to 32, 16 bytes behind
+// each of them.
+constexpr int kNsSmallLds = 160 * 1024;
+constexpr int kNsSmallThreads = 512;
+constexpr int kNsSmallSums = 8 * 8;       // bytes in front of X
+// Numbers of X's rows, in whole eights: a thread's 128, of pairs 80 (more do not fit the LDS).
+constexpr uint64_t ns_small_numbers(int planes) { return (planes == 1 ? 128 : 80) * kNsSmallThreads; }
+inline uint64_t ns_small_bytes(uint32_t m, uint32_t n, int planes) {
+  const uint64_t mp = (uint64_t(m) + 31) / 32 * 32, np = (uint64_t(n) + 31) / 32 * 32;
+  const uint64_t shares = mp <= 64 ? 8 * 1024 * sizeof(float) : 0;
+  return kNsSmallSums + mp * (np * 2 * planes + 16) + 2 * mp * (mp * 2 * planes + 16) + shares;
+}
+struct NsSteps {
+  int32_t count;
+  float k[3 * NOLOCO_MAX_NEWTON_SCHULZ_STEPS];
+};
+
 enum NsKind { kNsGram = 0, kNsSquare = 1, kNsApply = 2, kNsLast = 3 };
 
 // The arrays that hold the matrices (device, all workers' rows).
@@ -74,6 +94,8 @@ struct NsArrays {
   float eps;
 };
 
+int launch_ns_small(const NsArgs& args, const NsArrays& arrays, const NsSteps& steps, int planes, uint32_t workgroups,
+                    uint32_t lds_bytes, void* stream);
 int launch_ns_sums(const NsArgs& args, const NsArrays& arrays, uint32_t workgroups, void* stream);
 int launch_ns_start(const NsArgs& args, const NsArrays& arrays, int planes, uint32_t workgroups, void* stream);
 // Step `step` reads X number step & 1.

@@ -47,14 +47,19 @@ struct Shape {
   uint32_t mp() const { return padded(m(), tile); }
   uint32_t np() const { return padded(n(), tile); }
   uint64_t item_bytes(int planes) const { return noloco::ns_item_bytes(mp(), np(), planes); }
+  uint64_t small_bytes(int planes) const { return noloco::ns_small_bytes(m(), n(), planes); }
+  // Four rows of P are what a wave keeps of a column: 128.
+  bool small(int planes) const { return m() <= 128 && uint64_t(m()) * ((n() + 7) / 8 * 8) <= noloco::ns_small_numbers(planes) && small_bytes(planes) <= noloco::kNsSmallLds; }
 };
 
 // What goes through the products together: where the tables of its launches are among all of them, and their workgroups.
+// Small matrices (tile 0) take one launch of a workgroup each, with the first table.
 enum { kSums, kStart, kSymmetric, kApply, kTables };
 struct Batch {
   int tile;
   uint32_t first_table;
   uint32_t groups[kTables];
+  uint32_t lds;             // of a workgroup of small matrices
 };
 
 // The tile that takes the least time by a rough model: a workgroup's share of the rate that products of this tile reach
@@ -134,12 +139,25 @@ noloco_status check_overlap(const std::vector<noloco_matrix>& matrices) {
 
 // Splits the items of all shapes into batches that fit `room` bytes and a launch's table of classes.  Returns the most items
 // that a batch has.
-uint32_t make_batches(const std::vector<Shape>& shapes, int planes, uint64_t room, std::vector<Batch>* out, std::vector<NsTable>* tables) {
+uint32_t make_batches(std::vector<Shape> shapes, int planes, uint64_t room, std::vector<Batch>* out, std::vector<NsTable>* tables) {
+  // Small ones last and by size: a launch claims as much LDS as its largest matrix needs.  Where there are more of them than
+  // CUs, those that let two workgroups share a CU have a launch of their own.
+  uint64_t smalls = 0;
+  for (const Shape& s : shapes) smalls += s.small(planes) ? s.items : 0;
+  auto sharing = [&](const Shape& s) { return smalls <= 256 ? 1 : std::min<uint64_t>(noloco::kNsSmallLds / s.small_bytes(planes), 2); };
+  std::stable_sort(shapes.begin(), shapes.end(), [&](const Shape& a, const Shape& b) {
+    const bool as = a.small(planes), bs = b.small(planes);
+    if (as != bs) return bs;
+    return as ? a.small_bytes(planes) > b.small_bytes(planes) : a.tile > b.tile;
+  });
   size_t shape = 0;
   uint32_t done = 0, most = 0;      // of that shape's items; of a batch
   while (shape < shapes.size()) {
+    const Shape& head = shapes[shape];
+    const bool small = head.small(planes);
     Batch b{};
-    b.tile = shapes[shape].tile;
+    b.tile = small ? 0 : head.tile;
+    b.lds = small ? static_cast<uint32_t>(head.small_bytes(planes)) : 0;
     b.first_table = static_cast<uint32_t>(tables->size());
     NsTable table[kTables];
     for (NsTable& t : table) {
@@ -149,16 +167,18 @@ uint32_t make_batches(const std::vector<Shape>& shapes, int planes, uint64_t roo
     uint64_t used = 0;
     uint32_t items = 0;
     int classes = 0;
-    while (shape < shapes.size() && shapes[shape].tile == b.tile && classes < noloco::kNsClasses) {
+    while (shape < shapes.size() && classes < noloco::kNsClasses) {
       const Shape& s = shapes[shape];
-      const uint64_t each = s.item_bytes(planes), elements = uint64_t(s.rows) * s.cols;
-      const uint32_t mt = s.mp() / b.tile, nt = s.np() / b.tile;
+      if (s.small(planes) != small || (small ? sharing(s) != sharing(head) : s.tile != b.tile)) break;
+      const uint64_t each = small ? 0 : s.item_bytes(planes), elements = uint64_t(s.rows) * s.cols;
+      const uint32_t mt = s.mp() / s.tile, nt = s.np() / s.tile;
       const uint32_t chunks = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>((elements + noloco::kNsChunkElems - 1) / noloco::kNsChunkElems, 1), noloco::kNsChunks));
-      const uint32_t per[kTables] = {chunks, s.mp() / 64 * (s.np() / 64), mt * (mt + 1) / 2, mt * nt};
-      uint64_t fit = std::min<uint64_t>(s.items - done, (room - used) / each);
-      for (int k = 0; k < kTables; ++k) {
+      const uint32_t per[kTables] = {small ? 1 : chunks, s.mp() / 64 * (s.np() / 64), mt * (mt + 1) / 2, mt * nt};
+      uint64_t fit = s.items - done;
+      if (!small) fit = std::min<uint64_t>(fit, (room - used) / each);
+      for (int k = 0; k < (small ? 1 : kTables); ++k) {
         const uint64_t left = b.groups[k] < kMostGroups ? kMostGroups - b.groups[k] : 0;
-        fit = std::min(fit, std::max<uint64_t>(left / per[k], used == 0 ? 1 : 0));
+        fit = std::min(fit, std::max<uint64_t>(left / per[k], items == 0 ? 1 : 0));
       }
       if (fit == 0) break;
       NsClass c{};
@@ -171,7 +191,7 @@ uint32_t make_batches(const std::vector<Shape>& shapes, int planes, uint64_t roo
       c.mp = s.mp();
       c.np = s.np();
       c.tall = s.rows > s.cols ? 1 : 0;
-      for (int k = 0; k < kTables; ++k) {
+      for (int k = 0; k < (small ? 1 : kTables); ++k) {
         c.per_item = per[k];
         b.groups[k] += per[k] * static_cast<uint32_t>(fit);
         table[k].cls[classes] = c;
@@ -186,8 +206,8 @@ uint32_t make_batches(const std::vector<Shape>& shapes, int planes, uint64_t roo
       done = 0;
     }
     out->push_back(b);
-    tables->insert(tables->end(), table, table + kTables);
-    most = std::max(most, items);
+    tables->insert(tables->end(), table, table + (small ? 1 : kTables));
+    if (!small) most = std::max(most, items);
   }
   return most;
 }
@@ -238,14 +258,14 @@ noloco_status create_muon_plan(const noloco_matrix* given, int32_t num, int64_t 
     shapes.push_back(s);
     i = end;
   }
-  std::stable_sort(shapes.begin(), shapes.end(), [](const Shape& a, const Shape& b) { return a.tile > b.tile; });
-
-  uint64_t all = 0, largest = 0;
-  for (const Shape& s : shapes) {
-    all += s.item_bytes(2) * s.items;
-    largest = std::max(largest, s.item_bytes(2));
-  }
-  const uint64_t room = std::max(largest, std::min(all, static_cast<uint64_t>(workspace > 0 ? workspace : kDefaultWorkspace)));
+  uint64_t all[2] = {0, 0}, largest = 0;
+  for (const Shape& s : shapes)
+    for (int planes = 1; planes <= 2; ++planes)
+      if (!s.small(planes)) {
+        all[planes - 1] += s.item_bytes(planes) * s.items;
+        largest = std::max(largest, s.item_bytes(planes));
+      }
+  const uint64_t room = std::max(largest, std::min(std::max(all[0], all[1]), static_cast<uint64_t>(workspace > 0 ? workspace : kDefaultWorkspace)));
   plan->workspace_bytes = static_cast<int64_t>(room);
   std::vector<NsTable> tables;
   uint32_t summed = 0;
@@ -280,6 +300,7 @@ noloco_status create_muon_plan(const noloco_matrix* given, int32_t num, int64_t 
 // Do the coefficients keep what binary16 holds in its range?  Singular values start at most at 1.
 noloco_status check_method(const noloco_newton_schulz* method) {
   if (method == nullptr || method->coefficients == nullptr) return NOLOCO_ERR_NULL;
+  if (method->steps > NOLOCO_MAX_NEWTON_SCHULZ_STEPS) return NOLOCO_ERR_UNSUPPORTED;
   if (method->steps < 1 || !(method->eps >= 0.f) || !std::isfinite(method->eps)) return NOLOCO_ERR_INVALID_ARG;
   if (method->products < NOLOCO_PRODUCTS_AUTO || method->products > NOLOCO_PRODUCTS_PAIRS) return NOLOCO_ERR_INVALID_ARG;
   for (int32_t i = 0; i < 3 * method->steps; ++i)
@@ -312,8 +333,15 @@ noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, 
   const int32_t products = method->products != NOLOCO_PRODUCTS_AUTO ? method->products
                                                                     : (arrays.out_bf16 ? NOLOCO_PRODUCTS_F16 : NOLOCO_PRODUCTS_PAIRS);
   const int planes = products == NOLOCO_PRODUCTS_F16 ? 1 : 2;
+  noloco::NsSteps steps{};
+  steps.count = method->steps;
+  std::copy(method->coefficients, method->coefficients + 3 * method->steps, steps.k);
   for (const Batch& b : plan->batches[planes - 1]) {
     auto args = [&](int table) { return NsArgs{plan->tables + b.first_table + table, plan->items, plan->workspace, plan->sums}; };
+    if (b.tile == 0) {
+      if (noloco::launch_ns_small(args(kSums), arrays, steps, planes, b.groups[kSums], b.lds, stream) != 0) return NOLOCO_ERR_DEVICE;
+      continue;
+    }
     if (noloco::launch_ns_sums(args(kSums), arrays, b.groups[kSums], stream) != 0) return NOLOCO_ERR_DEVICE;
     if (noloco::launch_ns_start(args(kStart), arrays, planes, b.groups[kStart], stream) != 0) return NOLOCO_ERR_DEVICE;
     for (int32_t s = 0; s < method->steps; ++s) {

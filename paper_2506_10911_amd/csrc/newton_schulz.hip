@@ -50,16 +50,18 @@ __device__ __forceinline__ void load_to_lds(uint4v buffer, uint32_t lane_offset,
 // Enqueue a kernel and return the launch status itself.
 template <typename T> struct same { typedef T type; };
 template <typename... KArgs>
-int enqueue(void (*kernel)(KArgs...), uint32_t grid, uint32_t block, void* stream, typename same<KArgs>::type... args) {
+int enqueue_with(uint32_t lds, void (*kernel)(KArgs...), uint32_t grid, uint32_t block, void* stream, typename same<KArgs>::type... args) {
   void* argv[] = {static_cast<void*>(&args)...};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(grid), dim3(block), argv, 0, static_cast<hipStream_t>(stream));
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(grid), dim3(block), argv, lds, static_cast<hipStream_t>(stream));
+}
+template <typename... KArgs>
+int enqueue(void (*kernel)(KArgs...), uint32_t grid, uint32_t block, void* stream, typename same<KArgs>::type... args) {
+  return enqueue_with(0, kernel, grid, block, stream, args...);
 }
 
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
 __device__ __forceinline__ uint16_t narrow(float v) {   // to bf16, nearest, ties to even; NaN stays NaN
-  const uint32_t u = __float_as_uint(v);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return static_cast<uint16_t>((u >> 16) | 0x40u);
-  return static_cast<uint16_t>((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
 }
 
 // Tables that no kernel writes are read through the scalar cache.
@@ -89,9 +91,9 @@ __device__ __forceinline__ Place locate(const NsArgs& args, uint32_t group) {
   return p;
 }
 
-// ---------------------------------------------------------------------------
-// Momentum, and the sum of squares of what is orthogonalised
-// ---------------------------------------------------------------------------
+struct Yes { constexpr operator bool() const { return true; } };
+struct No { constexpr operator bool() const { return false; } };
+template <int N> struct Number { static constexpr int value = N; };
 
 template <bool BF16> __device__ __forceinline__ float load_one(const void* p, int64_t i) {
   if constexpr (BF16) return widen(static_cast<const uint16_t*>(p)[i]);
@@ -102,6 +104,505 @@ template <bool BF16> __device__ __forceinline__ float load_one(const void* p, in
 __device__ __forceinline__ float direction(float g, float moved, float mu, bool nesterov) {
   return nesterov ? g + mu * moved : moved;
 }
+
+template <bool BF16> struct Stored { typedef float type; };
+template <> struct Stored<true> { typedef uint16_t type; };
+
+// N neighbouring numbers of type E (float, or bf16 as stored) as floats.
+template <typename E, int N> struct Numbers {
+  typedef E vector __attribute__((ext_vector_type(4)));
+  float v[N];
+  __device__ __forceinline__ void load(const E* p) {
+    E raw[N];
+    if constexpr (N == 4) {
+      const vector x = *reinterpret_cast<const vector*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[i] = x[i];
+    } else {
+      raw[0] = *p;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (sizeof(E) == 2) v[i] = widen(raw[i]); else v[i] = raw[i];
+    }
+  }
+  __device__ __forceinline__ void store(E* p) const {
+    static_assert(sizeof(E) == 4, "momentum");
+    if constexpr (N == 4) *reinterpret_cast<vector*>(p) = vector{v[0], v[1], v[2], v[3]};
+    else *p = v[0];
+  }
+};
+
+// The result v of one element goes to where it belongs.
+template <typename Out> __device__ __forceinline__ void put_result(const NsArrays& arrays, Out* at, float by, float v) {
+  if (arrays.update) {
+    float old;
+    if constexpr (sizeof(Out) == 2) old = widen(*at); else old = *at;
+    v = old * arrays.keep - by * v;
+  }
+  if constexpr (sizeof(Out) == 2) *at = narrow(v); else *at = v;
+}
+
+// Four neighbouring ones, of which `there` exist; `whole` if they are aligned as one vector.
+template <typename Out>
+__device__ __forceinline__ void put_four(const NsArrays& arrays, Out* at, float by, float4v v, int there, bool whole) {
+  if (whole && there >= 4) {
+    typedef Out out4 __attribute__((ext_vector_type(4)));
+    out4 got;
+    if (arrays.update) got = *reinterpret_cast<const out4*>(at);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float value = v[k];
+      if (arrays.update) {
+        float old;
+        if constexpr (sizeof(Out) == 2) old = widen(got[k]); else old = got[k];
+        value = old * arrays.keep - by * value;
+      }
+      if constexpr (sizeof(Out) == 2) got[k] = narrow(value); else got[k] = value;
+    }
+    *reinterpret_cast<out4*>(at) = got;
+  } else {
+    for (int k = 0; k < 4 && k < there; ++k) put_result(arrays, at + k, by, v[k]);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Small matrices: everything in one workgroup
+// ---------------------------------------------------------------------------
+
+// X [mp][np], A and P [mp][mp] stay in the LDS from the first step to the last, rows 16 bytes longer than their numbers,
+// so that 16 rows of a fragment begin in 16 different quarters of the banks.  Blocks of 32 x 32: those of A and P on and
+// below the diagonal are dealt to the waves (of A with one or three blocks several waves share one's k); of P X a wave
+// takes 32 columns of X, which nobody else reads, holds them in registers and writes their next values in their place.
+//
+// Numbers come and go in chunks of eight, a thread every 512th chunk: eight along X's row, 16 bytes of the LDS.  (Results of
+// a tall matrix leave as four columns of two rows, since half a wave would write 128 bytes of a row only.)  They are read once: until the norm is known the LDS holds them as binary16 with a power of two for each chunk, or, where
+// there is room for pairs, the two halves of a binary32 number in the places of high and low half.
+template <int PLANES, bool BF16, bool MOMENTUM, typename Out>
+__global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArrays arrays, NsSteps steps) {
+  extern __shared__ __align__(16) char lds[];
+  constexpr uint32_t kThreads = kNsSmallThreads, kWaves = kThreads / 64;
+  constexpr float kUnitGram = ns_unit_a(PLANES) / (ns_unit_x(PLANES) * ns_unit_x(PLANES));
+  constexpr int kAhead = 4;
+  typedef typename Stored<BF16>::type In;
+  typedef uint16_t ushort8 __attribute__((ext_vector_type(8)));
+  const uint32_t thread = threadIdx.x, lane = thread & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  const Place place = locate(args, blockIdx.x);
+  const NsItem item = item_at(args, place.cls.first_item + place.item);
+  const uint32_t m = place.cls.m, n = place.cls.n, mp = (m + 31) / 32 * 32, np = (n + 31) / 32 * 32;
+  const bool tall = place.cls.tall != 0;
+  const uint32_t x_row = np * 2 * PLANES + 16, a_row = mp * 2 * PLANES + 16;
+  double* const part = reinterpret_cast<double*>(lds);
+  char* const x = lds + kNsSmallSums;
+  char* const gram = x + mp * x_row;
+  char* const poly = gram + mp * a_row;
+  float* const shares = reinterpret_cast<float*>(poly + mp * a_row);
+  auto spot = [](uint32_t j) { return PLANES == 1 ? j * 2 : (j / 32) * 128 + (j % 32) * 2; };   // of number j in a row
+
+  // Chunk by chunk: where its first number is in X and in the matrix (the matrix's first for a chunk that is not there).
+  // kWay: 0 eight along X's row, one by one; 1 the same in vectors, eight columns of a row; 2 four columns of two rows.
+  const uint32_t along = (n + 7) / 8;
+  const bool aligned = (static_cast<uint64_t>(item.offset) | static_cast<uint64_t>(item.row_stride)) % 4 == 0;
+  const bool row_vectors = !tall && aligned && n % 8 == 0, tall_vectors = tall && aligned && m % 4 == 0 && n % 2 == 0;
+  const int64_t apart = tall ? item.row_stride : 1;
+  struct Spot { bool there; uint32_t i, j; int64_t at; };
+  struct Walk { uint32_t all, divisor, up, over, chunk, high, low; };
+  auto walk_of = [&](auto way) {
+    Walk w;
+    w.divisor = decltype(way)::value == 2 ? m / 4 : (tall ? m : along);
+    w.all = decltype(way)::value == 2 ? m / 4 * (n / 2) : m * along;
+    w.up = kThreads / w.divisor;
+    w.over = kThreads - w.up * w.divisor;
+    w.chunk = thread;
+    w.high = thread / w.divisor;
+    w.low = thread - w.high * w.divisor;
+    return w;
+  };
+  auto next_chunk = [&](auto way, Walk& w) {
+    Spot c;
+    c.there = w.chunk < w.all;
+    c.i = c.there ? (decltype(way)::value == 2 ? w.low * 4 : (tall ? w.low : w.high)) : 0;
+    c.j = c.there ? (decltype(way)::value == 2 ? w.high * 2 : (tall ? w.high : w.low) * 8) : 0;
+    c.at = item.offset + (tall ? c.j * item.row_stride + c.i : c.i * item.row_stride + c.j);
+    w.chunk += kThreads;
+    w.high += w.up;
+    w.low += w.over;
+    if (w.low >= w.divisor) { w.low -= w.divisor; ++w.high; }
+    return c;
+  };
+  // Number e of a chunk from its first one on, in the matrix, and whether it is there; all eight of them in a plane of the LDS.
+  auto offset_of = [&](auto way, int e) {
+    return decltype(way)::value == 2 ? (e / 4) * apart + e % 4 : (decltype(way)::value == 1 ? e : e * apart);
+  };
+  auto real = [&](auto way, const Spot& c, int e) { return decltype(way)::value == 0 ? c.there && c.j + e < n : c.there; };
+  auto put = [&](const Spot& c, int plane, ushort8 v) {
+    if (c.there) *reinterpret_cast<ushort8*>(x + c.i * x_row + spot(c.j) + plane * 64) = v;
+  };
+  auto get = [&](auto way, const Spot& c, int plane) {
+    const char* const from = x + c.i * x_row + spot(c.j) + plane * 64;
+    ushort8 v;
+    if constexpr (decltype(way)::value == 2) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t two = *reinterpret_cast<const uint32_t*>(from + k * x_row);
+        v[k] = static_cast<uint16_t>(two);
+        v[4 + k] = static_cast<uint16_t>(two >> 16);
+      }
+    } else {
+      v = *reinterpret_cast<const ushort8*>(from);
+    }
+    return v;
+  };
+
+  // Nobody's rows and eights of columns of X are zeros.
+  for (uint32_t at = m * x_row + thread * 16; at < mp * x_row; at += kThreads * 16) *reinterpret_cast<uint4v*>(x + at) = uint4v{0, 0, 0, 0};
+  for (uint32_t row = thread; row < m; row += kThreads)
+    for (uint32_t j = along * 8; j < np; j += 8)
+#pragma unroll
+      for (int p = 0; p < PLANES; ++p) *reinterpret_cast<uint4v*>(x + row * x_row + spot(j) + p * 64) = uint4v{0, 0, 0, 0};
+
+  // Momentum, the sum of squares, and the numbers to the LDS.  Four chunks are on their way while one is worked on.
+  // A chunk's squares are summed with its power of two taken out: gradients are small enough for squares to leave
+  // binary32's range.
+  double sum = 0.;
+  uint8_t* const powers = reinterpret_cast<uint8_t*>(gram);        // of the chunks, as long as there is no A
+  const uint32_t all_chunks = m * along;
+  auto load = [&](auto way) {
+    constexpr int V = decltype(way)::value != 0 ? 4 : 1;
+    Walk walk = walk_of(way);
+    Spot c[kAhead];
+    Numbers<In, V> g[kAhead][8 / V];
+    Numbers<float, V> moved[kAhead][8 / V];
+    auto ask = [&](int k) {
+      c[k] = next_chunk(way, walk);
+#pragma unroll
+      for (int e = 0; e < 8; e += V) {
+        const int64_t from = c[k].at + (real(way, c[k], e) ? offset_of(way, e) : 0);
+        g[k][e / V].load(static_cast<const In*>(arrays.in) + from);
+        if constexpr (MOMENTUM) moved[k][e / V].load(arrays.momentum + from);
+      }
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) ask(k);
+#pragma unroll 1
+    for (uint32_t done = 0; done < all_chunks; done += kAhead * kThreads) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (done + k * kThreads >= all_chunks) break;
+      const Spot here = c[k];
+      float u[8];
+      int most = -127;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        u[e] = g[k][e / V].v[e % V];
+        if constexpr (MOMENTUM) {
+          float& v = moved[k][e / V].v[e % V];
+          v = arrays.mu * v + u[e];
+          u[e] = direction(u[e], v, arrays.mu, arrays.nesterov != 0);
+        }
+        if (!real(way, here, e)) u[e] = 0.f;
+        most = max(most, static_cast<int>(__float_as_uint(u[e]) >> 23 & 255) - 127);
+      }
+      if constexpr (MOMENTUM) {
+#pragma unroll
+        for (int e = 0; e < 8; e += V)
+          if (real(way, here, e)) moved[k][e / V].store(arrays.momentum + here.at + offset_of(way, e));
+      }
+      if (done + (k + kAhead) * kThreads < all_chunks) ask(k);
+      float squares = 0.f, scaled[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        scaled[e] = ldexpf(u[e], 14 - most);
+        squares += scaled[e] * scaled[e];
+      }
+      sum += ldexp(static_cast<double>(squares), 2 * (most - 14));
+      if constexpr (PLANES == 1) {
+        if (here.there) powers[done + k * kThreads + thread] = static_cast<uint8_t>(most + 127);
+        half8 h;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(scaled[e]);
+        put(here, 0, __builtin_bit_cast(ushort8, h));
+      } else {
+        ushort8 high, low;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          high[e] = static_cast<uint16_t>(__float_as_uint(u[e]) >> 16);
+          low[e] = static_cast<uint16_t>(__float_as_uint(u[e]));
+        }
+        put(here, 0, high);
+        put(here, 1, low);
+      }
+    }
+    }
+  };
+  if (row_vectors) load(Number<1>{}); else load(Number<0>{});
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
+  if (lane == 0) part[wave] = sum;
+  __syncthreads();
+  double squares = 0.;
+#pragma unroll
+  for (uint32_t w = 0; w < kWaves; ++w) squares += part[w];
+  const double norm = sqrt(squares) + static_cast<double>(arrays.eps);
+  {
+    // X_0 = u * ns_unit_x / norm, the factor as a number near 1 and a power of two, which float has room for whatever the norm.
+    // A matrix of zeros stays one.
+    int power = 0;
+    const float near = norm == 0. ? 0.f : static_cast<float>(frexp(static_cast<double>(ns_unit_x(PLANES)) / norm, &power));
+    const Number<0> way;           // in the LDS both ways are the same
+    Walk walk = walk_of(way);
+#pragma unroll 2
+    for (uint32_t done = 0; done < all_chunks; done += kThreads) {
+      const Spot c = next_chunk(way, walk);
+      half8 high, low;
+      if constexpr (PLANES == 1) {
+        const int chunk_power = power + static_cast<int>(c.there ? powers[done + thread] : 0) - 127 - 14;
+        const half8 h = __builtin_bit_cast(half8, get(way, c, 0));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) high[e] = static_cast<_Float16>(ldexpf(static_cast<float>(h[e]) * near, chunk_power));
+      } else {
+        const ushort8 hi = get(way, c, 0), lo = get(way, c, 1);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float v = ldexpf(__uint_as_float(static_cast<uint32_t>(hi[e]) << 16 | lo[e]) * near, power);
+          high[e] = static_cast<_Float16>(v);
+          low[e] = static_cast<_Float16>(v - static_cast<float>(high[e]));
+        }
+        put(c, 1, __builtin_bit_cast(ushort8, low));
+      }
+      put(c, 0, __builtin_bit_cast(ushort8, high));
+    }
+  }
+  __syncthreads();
+
+  // fragments: row (or column) lane % 32, eight k from 8 (lane / 32) on
+  const uint32_t of32 = lane & 31, half = lane >> 5;
+  struct Fragment { half8 p[PLANES]; };
+  auto plain = [&](const char* rows32, uint32_t row, uint32_t slice) {     // 16 k from 16 slice on of 32 rows
+    Fragment f;
+    const char* at = rows32 + of32 * row + (PLANES == 1 ? slice * 32 : (slice >> 1) * 128 + (slice & 1) * 32) + half * 16;
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) f.p[p] = *reinterpret_cast<const half8*>(at + p * 64);
+    return f;
+  };
+  auto multiply = [](const Fragment& a, const Fragment& b, float16v d) {
+    if constexpr (PLANES == 2) {
+      d = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[1], b.p[0], d, 0, 0, 0);
+      d = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[0], b.p[1], d, 0, 0, 0);
+    }
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.p[0], b.p[0], d, 0, 0, 0);
+  };
+  auto nothing = [] {
+    float16v d;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) d[e] = 0.f;
+    return d;
+  };
+  // Of a block, d[e] is row 8 (e / 4) + 4 half + e % 4, column of32.  Four rows' numbers from `quad` = e / 4 on, written as part
+  // of a row of the block's transpose, which begins at number j of `row`; and as they stand.
+  auto write_four = [&](char* row, uint32_t j, uint32_t quad, float4v v) {
+    const half4 high = __builtin_convertvector(v, half4);
+    char* at = row + spot(j) + (quad * 8 + half * 4) * 2;
+    *reinterpret_cast<half4*>(at) = high;
+    if constexpr (PLANES == 2) *reinterpret_cast<half4*>(at + 64) = __builtin_convertvector(v - __builtin_convertvector(high, float4v), half4);
+  };
+  auto write_column = [&](char* block_rows, uint32_t row_bytes, uint32_t j, uint32_t quad, float4v v) {
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+      char* at = block_rows + (quad * 8 + half * 4 + e) * row_bytes + spot(j);
+      const _Float16 high = static_cast<_Float16>(v[e]);
+      *reinterpret_cast<_Float16*>(at) = high;
+      if constexpr (PLANES == 2) *reinterpret_cast<_Float16*>(at + 64) = static_cast<_Float16>(v[e] - static_cast<float>(high));
+    }
+  };
+  auto four_of = [](const float16v& d, int quad) { return float4v{d[quad * 4], d[quad * 4 + 1], d[quad * 4 + 2], d[quad * 4 + 3]}; };
+
+  const uint32_t blocks = mp / 32, pairs = blocks * (blocks + 1) / 2;
+  auto below = [](uint32_t t, uint32_t& bi, uint32_t& bj) {     // block t on and below the diagonal, bj <= bi
+    bi = 0;
+    while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
+    bj = t - bi * (bi + 1) / 2;
+  };
+  // Sum over slices [k, end) of block (bi, bj) of the product of a matrix with its transpose.
+  auto block_product = [&](const char* matrix, uint32_t row_bytes, uint32_t bi, uint32_t bj, uint32_t k, uint32_t end) {
+    float16v d = nothing();
+    const char *r = matrix + bj * 32 * row_bytes, *c = matrix + bi * 32 * row_bytes;
+    constexpr uint32_t kAtOnce = PLANES == 1 ? 4 : 2;
+    if (bi == bj) {
+      for (; k + kAtOnce <= end; k += kAtOnce) {
+        Fragment a[kAtOnce];
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) a[i] = plain(r, row_bytes, k + i);
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) d = multiply(a[i], a[i], d);
+      }
+    } else {
+      for (; k + kAtOnce <= end; k += kAtOnce) {
+        Fragment a[kAtOnce], b[kAtOnce];
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+          a[i] = plain(r, row_bytes, k + i);
+          b[i] = plain(c, row_bytes, k + i);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) d = multiply(a[i], b[i], d);
+      }
+    }
+    for (; k < end; ++k) d = multiply(plain(r, row_bytes, k), plain(c, row_bytes, k), d);
+    return d;
+  };
+
+  // The symmetric product of `from` with its transpose, block by block; result(bi, bj, quad, d) makes four of its numbers
+  // what is written to both their places in `to`.  With one or three blocks of long rows all waves share their k, and then
+  // their results.
+  auto symmetric = [&](const char* from, uint32_t row_bytes, uint32_t slices, char* to, bool share_k, auto result) {
+    auto write = [&](uint32_t bi, uint32_t bj, uint32_t quad, float4v d) {
+      const float4v v = result(bi, bj, quad, d);
+      write_four(to + (bi * 32 + of32) * a_row, bj * 32, quad, v);
+      if (bi != bj) write_column(to + bj * 32 * a_row, a_row, bi * 32 + of32, quad, v);
+    };
+    if (share_k) {
+      // four waves take the block that has two operands to read, two each of the others
+      const uint32_t sharing = blocks == 1 ? kWaves : (wave < 4 ? 4 : 2), share = blocks == 1 ? wave : (wave < 4 ? wave : wave & 1);
+      const uint32_t bi = blocks == 1 || wave / 2 == 2 ? 0 : 1, bj = blocks == 1 || wave < 6 ? 0 : 1;
+      const float16v d = block_product(from, row_bytes, bi, bj, slices * share / sharing, slices * (share + 1) / sharing);
+#pragma unroll
+      for (int quad = 0; quad < 4; ++quad) *reinterpret_cast<float4v*>(shares + ((wave * 4 + quad) * 64 + lane) * 4) = four_of(d, quad);
+      __syncthreads();
+      for (uint32_t t = wave; t < pairs * 4; t += kWaves) {
+        const uint32_t block = t / 4, quad = t % 4;                  // blocks (1, 0), (0, 0), (1, 1), or (0, 0) alone
+        const uint32_t first = blocks == 1 ? 0 : (block == 0 ? 0 : 2 + block * 2), count = blocks == 1 ? kWaves : (block == 0 ? 4 : 2);
+        float4v sum = *reinterpret_cast<const float4v*>(shares + ((first * 4 + quad) * 64 + lane) * 4);
+        for (uint32_t other = 1; other < count; ++other) sum += *reinterpret_cast<const float4v*>(shares + (((first + other) * 4 + quad) * 64 + lane) * 4);
+        write(blocks == 1 || block == 1 ? 0 : 1, block == 2 ? 1 : 0, quad, sum);
+      }
+    } else {
+      for (uint32_t t = wave; t < pairs; t += kWaves) {
+        uint32_t bi, bj;
+        below(t, bi, bj);
+        const float16v d = block_product(from, row_bytes, bi, bj, 0, slices);
+#pragma unroll
+        for (int quad = 0; quad < 4; ++quad) write(bi, bj, quad, four_of(d, quad));
+      }
+    }
+    __syncthreads();
+  };
+
+  for (int step = 0; step < steps.count; ++step) {
+    const float constant = steps.k[3 * step] * ns_unit_p(PLANES), linear = steps.k[3 * step + 1] * (ns_unit_p(PLANES) / ns_unit_a(PLANES));
+    const float square = steps.k[3 * step + 2] * (ns_unit_p(PLANES) / (ns_unit_a(PLANES) * ns_unit_a(PLANES)));
+    symmetric(x, x_row, np / 16, gram, blocks <= 2, [&](uint32_t, uint32_t, uint32_t, float4v d) { return d * kUnitGram; });
+    symmetric(gram, a_row, mp / 16, poly, false, [&](uint32_t bi, uint32_t bj, uint32_t quad, float4v d) {
+      const uint32_t row = bj * 32 + quad * 8 + half * 4, col = bi * 32 + of32;
+      const char* at = gram + col * a_row + spot(bj * 32) + (quad * 8 + half * 4) * 2;
+      float4v a = __builtin_convertvector(*reinterpret_cast<const half4*>(at), float4v);
+      if constexpr (PLANES == 2) a += __builtin_convertvector(*reinterpret_cast<const half4*>(at + 64), float4v);
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) d[e] = square * d[e] + linear * a[e] + (row + e == col ? constant : 0.f);
+      return d;
+    });
+    // B = mp / 32 blocks of rows
+    auto apply = [&](auto count) {
+      constexpr int B = decltype(count)::value, S = 2 * B;
+      constexpr bool kKept = B * S * PLANES <= 16;         // P stays in registers for all columns
+      Fragment q[kKept ? B : 1][S];
+      if constexpr (kKept) {
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+          for (int k = 0; k < S; ++k) q[b][k] = plain(poly + b * 32 * a_row, a_row, k);
+      }
+      for (uint32_t j0 = wave * 32; j0 < np; j0 += kWaves * 32) {
+        Fragment f[S];
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+          const char* at = x + (k * 16 + half * 8 + ((lane >> 2) & 3)) * x_row + spot(j0) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+          for (int p = 0; p < PLANES; ++p) {
+            const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(at + p * 64));
+            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(at + p * 64 + 4 * x_row));
+            const half4 l = __builtin_bit_cast(half4, lo), h = __builtin_bit_cast(half4, hi);
+            f[k].p[p] = __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
+          }
+        }
+        constexpr int kRows = B < 2 ? B : 2;                // blocks of rows side by side
+#pragma unroll
+        for (int b0 = 0; b0 < B; b0 += kRows) {
+          float16v d[kRows];
+#pragma unroll
+          for (int b = 0; b < kRows; ++b) d[b] = nothing();
+#pragma unroll
+          for (int k = 0; k < S; ++k)
+#pragma unroll
+            for (int b = 0; b < kRows; ++b)
+              if (b0 + b < B) d[b] = multiply(f[k], kKept ? q[kKept ? b0 + b : 0][k] : plain(poly + (b0 + b) * 32 * a_row, a_row, k), d[b]);
+#pragma unroll
+          for (int b = 0; b < kRows; ++b)
+            if (b0 + b < B) {
+#pragma unroll
+              for (int quad = 0; quad < 4; ++quad)
+                write_four(x + ((b0 + b) * 32 + of32) * x_row, j0, quad, four_of(d[b], quad) * (1.f / ns_unit_p(PLANES)));
+            }
+        }
+      }
+    };
+    if (blocks == 1) apply(Number<1>{});
+    else if (blocks == 2) apply(Number<2>{});
+    else if (blocks == 3) apply(Number<3>{});
+    else apply(Number<4>{});
+    __syncthreads();
+  }
+
+  auto finish = [&](auto way) {
+    constexpr int V = decltype(way)::value != 0 ? 4 : 1;
+    typedef Out out4 __attribute__((ext_vector_type(4)));
+    const float by = arrays.lr * item.scale;
+    Walk walk = walk_of(way);
+#pragma unroll 1
+    for (uint32_t done = 0; done < walk.all; done += kAhead * kThreads) {
+      Spot c[kAhead];
+      Numbers<Out, V> old[kAhead][8 / V];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        c[k] = next_chunk(way, walk);
+        if (arrays.update) {
+#pragma unroll
+          for (int e = 0; e < 8; e += V)
+            old[k][e / V].load(static_cast<const Out*>(arrays.out) + c[k].at + (real(way, c[k], e) ? offset_of(way, e) : 0));
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const half8 high = __builtin_bit_cast(half8, get(way, c[k], 0));
+        half8 low;
+        if constexpr (PLANES == 2) low = __builtin_bit_cast(half8, get(way, c[k], 1));
+        Out v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float value = static_cast<float>(high[e]);
+          if constexpr (PLANES == 2) value += static_cast<float>(low[e]);
+          value *= 1.f / ns_unit_x(PLANES);
+          if (arrays.update) value = old[k][e / V].v[e % V] * arrays.keep - by * value;
+          if constexpr (sizeof(Out) == 2) v[e] = narrow(value); else v[e] = value;
+        }
+        Out* const out = static_cast<Out*>(arrays.out) + c[k].at;
+#pragma unroll
+        for (int e = 0; e < 8; e += V) {
+          if (!real(way, c[k], e)) continue;
+          if constexpr (V == 4) *reinterpret_cast<out4*>(out + offset_of(way, e)) = out4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+          else out[offset_of(way, e)] = v[e];
+        }
+      }
+    }
+  };
+  if (row_vectors) finish(Number<1>{});
+  else if (tall_vectors) finish(Number<2>{});
+  else finish(Number<0>{});
+}
+
+// ---------------------------------------------------------------------------
+// Momentum, and the sum of squares of what is orthogonalised
+// ---------------------------------------------------------------------------
 
 // One workgroup sums one chunk of an item: elements chunk * size .. of the matrix in row-major order.
 // Squares are summed in binary64: gradients are small enough for their squares to leave binary32's range.
@@ -186,7 +687,7 @@ __global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
   __syncthreads();
   const double norm = sqrt(part[0] + part[1] + part[2] + part[3]) + static_cast<double>(arrays.eps);
   // A matrix of zeros stays one.
-  const double unit = norm == 0. ? 0. : static_cast<double>(kNsUnit) / norm;
+  const double unit = norm == 0. ? 0. : static_cast<double>(ns_unit_x(PLANES)) / norm;
   char* x = args.workspace + cls.base + place.item * cls.item_bytes;
   const uint64_t ld = uint64_t(cls.np) * 2 * PLANES;
   // eight numbers of a row a thread: two rounds
@@ -209,9 +710,6 @@ __global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
 // ---------------------------------------------------------------------------
 // The products
 // ---------------------------------------------------------------------------
-
-struct Yes { constexpr operator bool() const { return true; } };
-struct No { constexpr operator bool() const { return false; } };
 
 // Workgroups are dealt to the 8 XCDs in turn; each XCD takes runs of `run` consecutive tiles, which share rows and
 // columns in its L2.
@@ -431,8 +929,9 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   if constexpr (KIND != kNsLast) {
     char* const to = KIND == kNsGram ? gram : (KIND == kNsSquare ? poly : x_next);
     const uint64_t to_ld = uint64_t(KIND == kNsApply ? np : mp) * 2 * PLANES;
-    // X and A are held in units of 2^-13, P of 2^-12
     if constexpr (KIND == kNsSquare) {
+      const float constant = ca * ns_unit_p(PLANES), linear = cb * (ns_unit_p(PLANES) / ns_unit_a(PLANES));
+      const float square = cc * (ns_unit_p(PLANES) / (ns_unit_a(PLANES) * ns_unit_a(PLANES)));
 #pragma unroll
       for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -448,12 +947,12 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
             for (int k = 0; k < 4; ++k) {
               float v = static_cast<float>(high[k]);
               if constexpr (PLANES == 2) v += static_cast<float>(low[k]);
-              acc[i][j][e + k] = cc * (acc[i][j][e + k] * (kNsUnitP / (kNsUnit * kNsUnit))) + cb * (v * (kNsUnitP / kNsUnit)) +
-                                 (r + k == c ? ca * kNsUnitP : 0.f);
+              acc[i][j][e + k] = square * acc[i][j][e + k] + linear * v + (r + k == c ? constant : 0.f);
             }
           }
     }
-    constexpr float kUnit = KIND == kNsGram ? 1.f / kNsUnit : (KIND == kNsSquare ? 1.f : 1.f / kNsUnitP);
+    constexpr float kUnit = KIND == kNsGram ? ns_unit_a(PLANES) / (ns_unit_x(PLANES) * ns_unit_x(PLANES))
+                                            : (KIND == kNsSquare ? 1.f : 1.f / ns_unit_p(PLANES));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       __syncthreads();
@@ -466,15 +965,12 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
             for (int e = 0; e < 16; e += 4) {
               const uint32_t r = r_of + i * 32 + e * 2;
               char* at = lds + (c_of + j * 32) * kImageRow + (PLANES == 1 ? r * 2 : (r / 32) * 128 + (r % 32) * 2);
-              half4 high, low;
+              float4v v;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float v = acc[i][j][e + k] * kUnit;
-                high[k] = static_cast<_Float16>(v);
-                low[k] = static_cast<_Float16>(v - static_cast<float>(high[k]));
-              }
+              for (int k = 0; k < 4; ++k) v[k] = acc[i][j][e + k] * kUnit;
+              const half4 high = __builtin_convertvector(v, half4);
               *reinterpret_cast<half4*>(at) = high;
-              if constexpr (PLANES == 2) *reinterpret_cast<half4*>(at + 64) = low;
+              if constexpr (PLANES == 2) *reinterpret_cast<half4*>(at + 64) = __builtin_convertvector(v - __builtin_convertvector(high, float4v), half4);
             }
       }
       __syncthreads();
@@ -511,15 +1007,6 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
     Out* const out = static_cast<Out*>(arrays.out) + item.offset;
     const bool vectors = ((reinterpret_cast<uintptr_t>(out) / sizeof(Out)) | static_cast<uint64_t>(item.row_stride)) % 4 == 0;
     const float by = arrays.lr * item.scale;
-    const bool update = arrays.update != 0;
-    auto put = [&](Out* at, float v) {
-      if (update) {
-        float old;
-        if constexpr (sizeof(Out) == 2) old = widen(*at); else old = *at;
-        v = old * arrays.keep - by * v;
-      }
-      if constexpr (sizeof(Out) == 2) *at = narrow(v); else *at = v;
-    };
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       __syncthreads();
@@ -533,7 +1020,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
               const uint32_t r = r_of + i * 32 + e * 2, c = c_of + j * 32;
               float4v v;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) v[k] = acc[i][j][e + k] * (1.f / (kNsUnit * kNsUnitP));
+              for (int k = 0; k < 4; ++k) v[k] = acc[i][j][e + k] * (1.f / (ns_unit_x(PLANES) * ns_unit_p(PLANES)));
               if (!tall) {
                 *reinterpret_cast<float4v*>(lds + c * kFloatRow + r * 4) = v;
               } else {
@@ -550,32 +1037,14 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
         for (uint32_t v = thread; v < high * (wide / 4); v += kThreads) {
           const uint32_t r = v / (wide / 4), c = v % (wide / 4) * 4;
           if (row0 + r >= rows || col0 + c >= cols) continue;
-          const float4v d = *reinterpret_cast<const float4v*>(lds + r * lds_row + c * 4);
-          Out* at = out + static_cast<int64_t>(row0 + r) * item.row_stride + col0 + c;
-          if (col0 + c + 4 <= cols) {
-            typedef Out out4 __attribute__((ext_vector_type(4)));
-            out4 got;
-            if (update) got = *reinterpret_cast<const out4*>(at);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              float value = d[k];
-              if (update) {
-                float old;
-                if constexpr (sizeof(Out) == 2) old = widen(got[k]); else old = got[k];
-                value = old * arrays.keep - by * value;
-              }
-              if constexpr (sizeof(Out) == 2) got[k] = narrow(value); else got[k] = value;
-            }
-            *reinterpret_cast<out4*>(at) = got;
-          } else {
-            for (int k = 0; k < 4 && col0 + c + k < cols; ++k) put(at + k, d[k]);
-          }
+          put_four(arrays, out + static_cast<int64_t>(row0 + r) * item.row_stride + col0 + c, by,
+                   *reinterpret_cast<const float4v*>(lds + r * lds_row + c * 4), static_cast<int>(cols - col0 - c), true);
         }
       } else {
         for (uint32_t v = thread; v < high * wide; v += kThreads) {
           const uint32_t r = v / wide, c = v % wide;
           if (row0 + r >= rows || col0 + c >= cols) continue;
-          put(out + static_cast<int64_t>(row0 + r) * item.row_stride + col0 + c, *reinterpret_cast<const float*>(lds + r * lds_row + c * 4));
+          put_result(arrays, out + static_cast<int64_t>(row0 + r) * item.row_stride + col0 + c, by, *reinterpret_cast<const float*>(lds + r * lds_row + c * 4));
         }
       }
     }
@@ -597,6 +1066,20 @@ int launch_product(const NsArgs& args, const NsArrays& arrays, int kind, int ste
 }
 
 }  // namespace
+
+int launch_ns_small(const NsArgs& args, const NsArrays& arrays, const NsSteps& steps, int planes, uint32_t workgroups,
+                    uint32_t lds_bytes, void* stream) {
+  auto pick = [&](auto momentum, auto bf16, auto out) {
+    typedef decltype(out) Out;
+    return enqueue_with(lds_bytes, planes == 1 ? ns_small<1, bf16, momentum, Out> : ns_small<2, bf16, momentum, Out>, workgroups,
+                        kNsSmallThreads, stream, args, arrays, steps);
+  };
+  auto with_out = [&](auto momentum, auto bf16) {
+    return arrays.out_bf16 ? pick(momentum, bf16, uint16_t{}) : pick(momentum, bf16, float{});
+  };
+  if (arrays.momentum != nullptr) return arrays.in_bf16 ? with_out(Yes{}, Yes{}) : with_out(Yes{}, No{});
+  return arrays.in_bf16 ? with_out(No{}, Yes{}) : with_out(No{}, No{});
+}
 
 int launch_ns_sums(const NsArgs& args, const NsArrays& arrays, uint32_t workgroups, void* stream) {
   if (arrays.momentum != nullptr)

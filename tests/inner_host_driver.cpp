@@ -27,7 +27,7 @@ extern "C" hipError_t hipFree(void* ptr) { ++frees; std::free(ptr); return hipSu
 extern "C" hipError_t hipMemcpy(void* dst, const void* src, size_t size, hipMemcpyKind) { std::memcpy(dst, src, size); return hipSuccess; }
 
 namespace noloco {
-struct Launch { int what, kind, tile, planes, step; uint32_t groups; NsArgs args; };
+struct Launch { int what, kind, tile, planes, step; uint32_t groups; NsArgs args; uint32_t lds; };
 static std::vector<Launch> launches;
 static int fail_at = -1;
 static int record(const Launch& l) {
@@ -35,10 +35,13 @@ static int record(const Launch& l) {
   launches.push_back(l);
   return 0;
 }
-int launch_ns_sums(const NsArgs& args, const NsArrays&, uint32_t groups, void*) { return record({0, 0, 0, 0, 0, groups, args}); }
-int launch_ns_start(const NsArgs& args, const NsArrays&, int planes, uint32_t groups, void*) { return record({1, 0, 0, planes, 0, groups, args}); }
+int launch_ns_sums(const NsArgs& args, const NsArrays&, uint32_t groups, void*) { return record({0, 0, 0, 0, 0, groups, args, 0}); }
+int launch_ns_start(const NsArgs& args, const NsArrays&, int planes, uint32_t groups, void*) { return record({1, 0, 0, planes, 0, groups, args, 0}); }
 int launch_ns_product(const NsArgs& args, const NsArrays&, int kind, int tile, int planes, int step, float, float, float, uint32_t groups, void*) {
-  return record({2, kind, tile, planes, step, groups, args});
+  return record({2, kind, tile, planes, step, groups, args, 0});
+}
+int launch_ns_small(const NsArgs& args, const NsArrays&, const NsSteps& steps, int planes, uint32_t groups, uint32_t lds, void*) {
+  return record({3, 0, 0, planes, steps.count, groups, args, lds});
 }
 static int lookups = 0, gradients = 0;
 int launch_embed_lookup(const EmbedArgs&, void*) { ++lookups; return 0; }
@@ -66,16 +69,21 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
   char* const y = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(here) + uintptr_t(W) * stride * 8 + 4096) / 256 * 256);
   CHECK(noloco_orthogonalize(plan, x, NOLOCO_F32, y, out_dtype, &method, nullptr) == NOLOCO_OK);
   const int planes = out_dtype == NOLOCO_BF16 ? 1 : 2;
-  CHECK(launches.size() == static_cast<size_t>(batches[planes - 1]) * (2 + 3 * 2));
   std::map<int64_t, int> seen;
+  size_t in_batch = 0, batch = 0;
   for (size_t l = 0; l < launches.size(); ++l) {
     const Launch& launch = launches[l];
-    const size_t in_batch = l % 8;
-    CHECK(launch.what == (in_batch == 0 ? 0 : (in_batch == 1 ? 1 : 2)));
+    if (launch.what == 3) {
+      CHECK(in_batch == 0 && launch.planes == planes && launch.step == 2 && launch.lds <= kNsSmallLds);
+      ++batch;
+    } else {
+      CHECK(launch.what == (in_batch == 0 ? 0 : (in_batch == 1 ? 1 : 2)));
+    }
     if (launch.what == 2) {
       const int kinds[6] = {kNsGram, kNsSquare, kNsApply, kNsGram, kNsSquare, kNsLast};
       CHECK(launch.kind == kinds[in_batch - 2] && launch.planes == planes && launch.step == static_cast<int>(in_batch - 2) / 3);
     }
+    if (launch.what != 3 && ++in_batch == 8) { in_batch = 0; ++batch; }
     CHECK(launch.groups > 0 && launch.groups <= (1u << 22) + (1u << 21));
     uint32_t last = 0;
     uint64_t end_of_last = 0;
@@ -87,26 +95,31 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
       last = launch.args.table->end[i];
       CHECK(c.m <= c.n && c.mp >= c.m && c.np >= c.n && c.mp % 64 == 0 && c.np % 64 == 0);
       CHECK(ns_x_bytes(c.mp, c.np, planes) >> 32 == 0);
-      CHECK(c.item_bytes == ns_item_bytes(c.mp, c.np, planes) && c.base >= end_of_last);
-      end_of_last = c.base + c.item_bytes * items;
-      CHECK(end_of_last <= static_cast<uint64_t>(bytes));
+      if (launch.what == 3) {
+        CHECK(c.per_item == 1 && c.m <= 128 && ns_small_bytes(c.m, c.n, planes) <= launch.lds);
+      } else {
+        CHECK(c.item_bytes == ns_item_bytes(c.mp, c.np, planes) && c.base >= end_of_last);
+        end_of_last = c.base + c.item_bytes * items;
+        CHECK(end_of_last <= static_cast<uint64_t>(bytes));
+      }
       if (launch.what == 2) {
         const uint32_t mt = c.mp / launch.tile, nt = c.np / launch.tile;
         CHECK(c.mp % launch.tile == 0 && c.np % launch.tile == 0);
         CHECK(c.per_item == (launch.kind >= kNsApply ? mt * nt : mt * (mt + 1) / 2));
       }
       if (launch.what == 1) CHECK(c.per_item == c.mp / 64 * (c.np / 64));
-      if (launch.what == 0) {
+      if (launch.what == 0 || launch.what == 3) {
         CHECK(c.per_item >= 1 && c.per_item <= kNsChunks);
         for (uint32_t j = 0; j < items; ++j) {
           const NsItem& item = launch.args.items[c.first_item + j];
-          CHECK(reinterpret_cast<const char*>(launch.args.sums + uint64_t(c.first_sum + j + 1) * kNsChunks) <= launch.args.workspace);
+          if (launch.what == 0) CHECK(reinterpret_cast<const char*>(launch.args.sums + uint64_t(c.first_sum + j + 1) * kNsChunks) <= launch.args.workspace);
           ++seen[item.offset];
         }
       }
     }
     CHECK(last == launch.groups);
   }
+  CHECK(in_batch == 0 && batch == static_cast<size_t>(batches[planes - 1]));
   size_t wanted = 0;
   for (const noloco_matrix& m : matrices)
     if (m.rows > 0 && m.cols > 0)
@@ -115,9 +128,9 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
   // a launch that the runtime refuses ends the call
   if (!launches.empty()) {
     launches.clear();
-    fail_at = 1;
+    fail_at = 0;
     CHECK(noloco_orthogonalize(plan, x, NOLOCO_F32, y, out_dtype, &method, nullptr) == NOLOCO_ERR_DEVICE);
-    CHECK(launches.size() == 1);
+    CHECK(launches.empty());
     fail_at = -1;
   }
   CHECK(noloco_muon_plan_destroy(plan) == NOLOCO_OK);
