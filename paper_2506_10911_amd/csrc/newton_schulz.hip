@@ -604,49 +604,80 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
 // Momentum, and the sum of squares of what is orthogonalised
 // ---------------------------------------------------------------------------
 
-// One workgroup sums one chunk of an item: elements chunk * size .. of the matrix in row-major order.
-// Squares are summed in binary64: gradients are small enough for their squares to leave binary32's range.
-template <bool BF16, bool MOMENTUM>
-__global__ __launch_bounds__(256) void ns_sums(NsArgs args, NsArrays arrays) {
-  const Place place = locate(args, blockIdx.x);
-  const NsClass& cls = place.cls;
-  const NsItem item = item_at(args, cls.first_item + place.item);
+// One workgroup sums one chunk of an item: numbers part * size .. of the matrix in row-major order, V at a time where
+// rows are whole vectors, and four (V = 1: eight) of a thread's on their way together.  Squares are summed in binary64: gradients
+// are small enough for their squares to leave binary32's range.
+template <bool BF16, bool MOMENTUM, int V>
+__device__ __forceinline__ double sum_chunk(const NsArrays& arrays, const NsClass& cls, const NsItem& item, uint32_t part) {
+  constexpr int kAtOnce = V == 4 ? 4 : 8;
+  typedef typename Stored<BF16>::type In;
   const uint32_t cols = cls.tall ? cls.m : cls.n;
   const uint64_t total = uint64_t(cls.m) * cls.n;
-  const uint64_t size = (total + cls.per_item - 1) / cls.per_item;
-  const uint64_t begin = place.part * size, end = begin + size < total ? begin + size : total;
+  const uint64_t size = ((total + cls.per_item - 1) / cls.per_item + V - 1) / V * V;
+  const uint64_t begin = part * size, end = begin + size < total ? begin + size : total;
+  uint64_t e = begin + threadIdx.x * V;
+  uint64_t row = e / cols, col = e - row * cols;
+  const uint32_t step_rows = 256 * V / cols, step_cols = 256 * V - step_rows * cols;
   double sum = 0.;
-  if (begin + threadIdx.x < end) {
-    const uint64_t first = begin + threadIdx.x;
-    uint64_t row = first / cols, col = first - row * cols;
-    const uint32_t step_rows = 256 / cols, step_cols = 256 - step_rows * cols;
-    for (uint64_t e = first; e < end; e += 256) {
-      const int64_t at = item.offset + static_cast<int64_t>(row) * item.row_stride + static_cast<int64_t>(col);
-      float u = load_one<BF16>(arrays.in, at);
-      if constexpr (MOMENTUM) {
-        const float moved = arrays.mu * arrays.momentum[at] + u;
-        arrays.momentum[at] = moved;
-        u = direction(u, moved, arrays.mu, arrays.nesterov != 0);
-      }
-      sum += static_cast<double>(u) * u;
+  while (e < end) {
+    int64_t at[kAtOnce];
+    Numbers<In, V> g[kAtOnce];
+    Numbers<float, V> moved[kAtOnce];
+    const uint64_t first = e;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      at[k] = item.offset + (e < end ? static_cast<int64_t>(row) * item.row_stride + static_cast<int64_t>(col) : 0);
+      g[k].load(static_cast<const In*>(arrays.in) + at[k]);
+      if constexpr (MOMENTUM) moved[k].load(arrays.momentum + at[k]);
+      e += 256 * V;
       row += step_rows;
       col += step_cols;
       if (col >= cols) { col -= cols; ++row; }
     }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const bool there = first + k * 256 * V < end;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float u = g[k].v[i];
+        if constexpr (MOMENTUM) {
+          moved[k].v[i] = arrays.mu * moved[k].v[i] + u;
+          u = direction(u, moved[k].v[i], arrays.mu, arrays.nesterov != 0);
+        }
+        sum += there ? static_cast<double>(u) * u : 0.;
+      }
+      if constexpr (MOMENTUM)
+        if (there) moved[k].store(arrays.momentum + at[k]);
+    }
   }
+  return sum;
+}
+
+// Whether four neighbouring numbers of a row are one vector, wherever they begin at a multiple of four.
+__device__ __forceinline__ bool whole_vectors(const NsItem& item, uint32_t cols) {
+  return (static_cast<uint64_t>(item.offset) | static_cast<uint64_t>(item.row_stride) | cols) % 4 == 0;
+}
+
+template <bool BF16, bool MOMENTUM>
+__global__ __launch_bounds__(256) void ns_sums(NsArgs args, NsArrays arrays) {
+  const Place place = locate(args, blockIdx.x);
+  const NsItem item = item_at(args, place.cls.first_item + place.item);
+  double sum = whole_vectors(item, place.cls.tall ? place.cls.m : place.cls.n)
+                   ? sum_chunk<BF16, MOMENTUM, 4>(arrays, place.cls, item, place.part)
+                   : sum_chunk<BF16, MOMENTUM, 1>(arrays, place.cls, item, place.part);
   __shared__ double part[4];
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
   __syncthreads();
   if (threadIdx.x == 0)
-    args.sums[uint64_t(cls.first_sum + place.item) * kNsChunks + place.part] = part[0] + part[1] + part[2] + part[3];
+    args.sums[uint64_t(place.cls.first_sum + place.item) * kNsChunks + place.part] = part[0] + part[1] + part[2] + part[3];
 }
 
 // ---------------------------------------------------------------------------
 // X_0
 // ---------------------------------------------------------------------------
 
-// chunks of an item in ns_sums; the same on the host
+// workgroups of an item in ns_sums; the same on the host
 __host__ __device__ inline uint32_t chunks_of(uint64_t elements) {
   const uint64_t c = (elements + kNsChunkElems - 1) / kNsChunkElems;
   return c < 1 ? 1 : (c > kNsChunks ? kNsChunks : static_cast<uint32_t>(c));
@@ -655,39 +686,53 @@ __host__ __device__ inline uint32_t chunks_of(uint64_t elements) {
 // A workgroup writes a 64 x 64 tile of X_0, zeros where it is padded.
 template <bool BF16, bool MOMENTUM, int PLANES>
 __global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
-  __shared__ float tile[64][65];
+  __shared__ __align__(16) float tile[64][68];
   __shared__ double part[4];
+  typedef typename Stored<BF16>::type In;
   const Place place = locate(args, blockIdx.x);
   const NsClass& cls = place.cls;
   const NsItem item = item_at(args, cls.first_item + place.item);
   const uint32_t chunks = chunks_of(uint64_t(cls.m) * cls.n);
   double sum = threadIdx.x < chunks ? args.sums[uint64_t(cls.first_sum + place.item) * kNsChunks + threadIdx.x] : 0.;
-  for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
 
   const uint32_t across = cls.np / 64;
   const uint32_t i0 = place.part / across * 64, j0 = place.part % across * 64;     // of X
   const bool tall = cls.tall != 0;
   const uint32_t rows = tall ? cls.n : cls.m, cols = tall ? cls.m : cls.n;
   const uint32_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;                         // of the matrix
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (uint32_t r = wave; r < 64; r += 4) {
-    float u = 0.f;
-    if (r0 + r < rows && c0 + lane < cols) {
-      const int64_t at = item.offset + static_cast<int64_t>(r0 + r) * item.row_stride + c0 + lane;
-      if constexpr (MOMENTUM) {
-        const float moved = arrays.momentum[at];
-        u = arrays.nesterov ? direction(load_one<BF16>(arrays.in, at), moved, arrays.mu, true) : moved;
-      } else {
-        u = load_one<BF16>(arrays.in, at);
+  auto fetch = [&](auto vectors) {
+    constexpr int V = vectors ? 4 : 1, N = 16 / V;
+    const uint32_t c = threadIdx.x % (64 / V) * V, r_first = threadIdx.x / (64 / V);
+    Numbers<In, V> g[N];
+    Numbers<float, V> moved[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const uint32_t r = r_first + k * (4 * V);
+      const int64_t at = item.offset + (r0 + r < rows && c0 + c < cols ? static_cast<int64_t>(r0 + r) * item.row_stride + c0 + c : 0);
+      if (!MOMENTUM || arrays.nesterov) g[k].load(static_cast<const In*>(arrays.in) + at);
+      if constexpr (MOMENTUM) moved[k].load(arrays.momentum + at);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const uint32_t r = r_first + k * (4 * V);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float u;
+        if constexpr (MOMENTUM) u = arrays.nesterov ? direction(g[k].v[i], moved[k].v[i], arrays.mu, true) : moved[k].v[i];
+        else u = g[k].v[i];
+        if (r0 + r >= rows || c0 + c >= cols) u = 0.f;
+        if (tall) tile[c + i][r] = u; else tile[r][c + i] = u;
       }
     }
-    if (tall) tile[lane][r] = u; else tile[r][lane] = u;
-  }
+  };
+  if (whole_vectors(item, cols)) fetch(Yes{}); else fetch(No{});
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
   __syncthreads();
   const double norm = sqrt(part[0] + part[1] + part[2] + part[3]) + static_cast<double>(arrays.eps);
-  // A matrix of zeros stays one.
-  const double unit = norm == 0. ? 0. : static_cast<double>(ns_unit_x(PLANES)) / norm;
+  // The factor as a number near 1 and a power of two, which float has room for whatever the norm.  A matrix of zeros stays one.
+  int power = 0;
+  const float near = norm == 0. ? 0.f : static_cast<float>(frexp(static_cast<double>(ns_unit_x(PLANES)) / norm, &power));
   char* x = args.workspace + cls.base + place.item * cls.item_bytes;
   const uint64_t ld = uint64_t(cls.np) * 2 * PLANES;
   // eight numbers of a row a thread: two rounds
@@ -696,7 +741,7 @@ __global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
     half8 high, low;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float f = static_cast<float>(static_cast<double>(tile[r][c + e]) * unit);
+      const float f = ldexpf(tile[r][c + e] * near, power);
       high[e] = static_cast<_Float16>(f);
       low[e] = static_cast<_Float16>(f - static_cast<float>(high[e]));
     }
@@ -726,7 +771,7 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t block
 // ones and so on, so that a stage of 128 bytes of every row is 64 numbers, or 32 pairs.
 //
 // A wave owns a (T / WR) x (T / WC) part in 32 x 32 blocks.  The operands come to the LDS by loads that bypass the
-// registers, two stages deep; fragments are read one slice of 16 k ahead of the products that use them, across the
+// registers, two stages deep (eight in tiles of 64, which are taken where there are few: nothing else hides a load's way); fragments are read one slice of 16 k ahead of the products that use them, across the
 // stage's end too: the barrier in front of the last slice's products tells that the next stage has come and that
 // this one's buffer is free.
 //
@@ -741,6 +786,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   constexpr int kSlices = kDepth / 16;
   constexpr int kOperand = T * 128;                         // bytes of one operand's stage
   constexpr int kStage = 2 * kOperand;
+  constexpr int kStages = T == 64 ? 8 : 2;
   constexpr int MB = T / WR / 32, NB = T / WC / 32;         // a wave's blocks
   constexpr int kLoads = T / 8 / kWaves;                    // of 1 KiB, of a wave, operand and stage
   constexpr int kTurned = T * 2 * PLANES;                   // bytes of a row of the transposed operand
@@ -751,8 +797,8 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   constexpr int kFloatRow = (T + 4) * 4, kFloatTallRow = (kHalf + 4) * 4;
   constexpr int kFloats = kHalf * kFloatRow > T * kFloatTallRow ? kHalf * kFloatRow : T * kFloatTallRow;
   constexpr int kResult = KIND == kNsLast ? kFloats : kImage;
-  constexpr int kLds = 2 * kStage > kResult ? 2 * kStage : kResult;
-  static_assert(kTurned <= 1024 && kLoads >= 1 && kLds <= 160 * 1024, "tile");
+  constexpr int kLds = kStages * kStage > kResult ? kStages * kStage : kResult;
+  static_assert(kTurned <= 1024 && kLoads >= 1 && kLds <= 160 * 1024 && (kStages & (kStages - 1)) == 0, "tile");
   __shared__ __align__(1024) char lds[kLds];
 
   const Place place = locate(args, tile_of_block(blockIdx.x, gridDim.x, run));
@@ -812,7 +858,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   }
   const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_memory char*)lds));
   auto ask = [&](uint32_t stage) {
-    const uint32_t to = lds_at + (stage & 1) * kStage;
+    const uint32_t to = lds_at + (stage % kStages) * kStage;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const uint32_t load = wave * kLoads + i;
@@ -843,7 +889,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   }
   struct Fragments { half8 r[PLANES][MB], c[PLANES][NB]; };
   auto read = [&](uint32_t stage, int slice, Fragments& f) {
-    const char* from = lds + (stage & 1) * kStage;
+    const char* from = lds + (stage % kStages) * kStage;
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) {
       const uint32_t q = ((p * 4 + slice * 2 + fk) ^ ((fr >> 1) & 7)) * 16;
@@ -889,17 +935,18 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
       for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.r[0][i], f.c[0][j], acc[i][j], 0, 0, 0);
   };
 
-  ask(0);
-  if (stages > 1) {
-    ask(1);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+  if (stages >= kStages) {
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) ask(i);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * 2 * kLoads) : "memory");
   } else {
+    for (uint32_t i = 0; i < stages; ++i) ask(i);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
   __builtin_amdgcn_s_barrier();
   Fragments even, odd;
   read(0, 0, even);
-  // The last two stages by themselves, so that nothing in the loop is conditional.
+  // The stages behind the last one that is asked for by themselves, so that nothing in the loop is conditional.
   auto stage = [&](uint32_t s, auto ask_more, auto read_next) {
 #pragma unroll
     for (int slice = 0; slice < kSlices; ++slice) {
@@ -908,10 +955,12 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
       if (slice + 1 < kSlices) {
         read(s, slice + 1, next);
       } else {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // the next stage has come, those behind it may be on their way
+        if constexpr (ask_more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * 2 * kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         if constexpr (read_next) read(s + 1, 0, next);
-        if constexpr (ask_more) ask(s + 2);
+        if constexpr (ask_more) ask(s + kStages);
       }
       multiply(now);
       // the products of a slice stay behind its reads, which the compiler would put in front of the next barrier
@@ -919,8 +968,8 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
     }
   };
   uint32_t s = 0;
-  for (; s + 2 < stages; ++s) stage(s, Yes{}, Yes{});
-  if (s + 1 < stages) stage(s++, No{}, Yes{});
+  for (; s + kStages < stages; ++s) stage(s, Yes{}, Yes{});
+  for (; s + 1 < stages; ++s) stage(s, No{}, Yes{});
   stage(s, No{}, No{});
 
   // A wave's results go through the LDS, half of the tile's columns at a time, and from there in whole lines.
