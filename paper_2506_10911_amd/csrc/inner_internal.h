@@ -108,6 +108,7 @@ int launch_ns_product(const NsArgs& args, const NsArrays& arrays, int kind, int 
 
 constexpr int kSortChunk = 2048;        // tokens that one workgroup sorts in its LDS
 constexpr int kMergeWays = 16;          // sorted lists that one merge joins
+constexpr int kMergeChunk = kSortChunk * kMergeWays;      // tokens that the first one holds in the LDS
 constexpr int kSumChunk = 32;           // sorted positions that a workgroup sums
 
 struct EmbedArgs {
@@ -120,8 +121,9 @@ struct EmbedArgs {
   int32_t W;
   float scale;
   int32_t table_bf16, rows_bf16, tokens_i64, accumulate;
-  int32_t vectors;        // four columns at a time: everything is aligned for it
-  uint64_t* sorted[2];    // [W][tokens] token << 32 | position
+  int32_t vectors;        // columns that everything is aligned for at a time: 1, 4 or 8
+  uint32_t* token[2];     // [W][tokens], sorted, and their positions
+  uint32_t* position[2];
   float* partial;         // [W][chunks][2][width]
 };
 

@@ -108,7 +108,7 @@ struct noloco_embedding_plan {
   int64_t offset = 0, vocab = 0, width = 0, stride = 0, max_tokens = 0;
   int32_t W = 0;
   char* block = nullptr;
-  uint64_t* sorted[2] = {};
+  uint32_t* lists[4] = {};          // tokens and positions, twice
   float* partial = nullptr;
 
   noloco_embedding_plan() = default;
@@ -465,17 +465,16 @@ extern "C" noloco_status noloco_embedding_plan_create(int64_t offset, int64_t vo
   plan->W = W;
   plan->max_tokens = max_tokens;
   auto whole = [](uint64_t bytes) { return (bytes + 255) / 256 * 256; };
-  const uint64_t list = whole(static_cast<uint64_t>(W) * max_tokens * sizeof(uint64_t));
+  const uint64_t list = whole(static_cast<uint64_t>(W) * max_tokens * sizeof(uint32_t));
   const uint64_t chunks = static_cast<uint64_t>(max_tokens + noloco::kSumChunk - 1) / noloco::kSumChunk;
   const uint64_t partial = static_cast<uint64_t>(W) * chunks * 2 * width * sizeof(float);
   if (hipGetDevice(&plan->device) != hipSuccess ||
-      hipMalloc(reinterpret_cast<void**>(&plan->block), 2 * list + partial + 256) != hipSuccess) {
+      hipMalloc(reinterpret_cast<void**>(&plan->block), 4 * list + partial + 256) != hipSuccess) {
     plan->block = nullptr;
     return NOLOCO_ERR_DEVICE;
   }
-  plan->sorted[0] = reinterpret_cast<uint64_t*>(plan->block);
-  plan->sorted[1] = reinterpret_cast<uint64_t*>(plan->block + list);
-  plan->partial = reinterpret_cast<float*>(plan->block + 2 * list);
+  for (int i = 0; i < 4; ++i) plan->lists[i] = reinterpret_cast<uint32_t*>(plan->block + i * list);
+  plan->partial = reinterpret_cast<float*>(plan->block + 4 * list);
   *out = plan.release();
   return NOLOCO_OK;
 }
@@ -521,9 +520,11 @@ noloco_status embed_args(const noloco_embedding_plan* plan, const void* table, i
   out->table_bf16 = table_dtype == NOLOCO_BF16;
   out->rows_bf16 = rows_dtype == NOLOCO_BF16;
   out->tokens_i64 = token_type == NOLOCO_I64;
-  out->vectors = plan->width % 4 == 0 && plan->offset % 4 == 0;
-  out->sorted[0] = plan->sorted[0];
-  out->sorted[1] = plan->sorted[1];
+  out->vectors = (plan->width | plan->offset) % 8 == 0 ? 8 : ((plan->width | plan->offset) % 4 == 0 ? 4 : 1);
+  for (int i = 0; i < 2; ++i) {
+    out->token[i] = plan->lists[2 * i];
+    out->position[i] = plan->lists[2 * i + 1];
+  }
   out->partial = plan->partial;
   return NOLOCO_OK;
 }

@@ -112,6 +112,11 @@ def test_gradient_of_many_tokens(T, vocab):
     check_gradient((1, T, vocab, 8, 0), "i64", "f32", "f32", False, "mixed")
 
 
+def test_gradient_of_a_vocabulary_beyond_21_bits():
+    """Tokens that need more bits than the short sort keys have."""
+    check_gradient((1, 3000, (1 << 21) + 77, 1, 0), "i64", "f32", "f32", False, "mixed")
+
+
 def test_no_tokens():
     a, stride = arena(2, 10, 6, 0, torch.float32)
     plan = nl.EmbeddingPlan(0, 10, 6, stride, 2, 0)
