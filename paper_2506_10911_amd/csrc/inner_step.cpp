@@ -62,22 +62,34 @@ struct Batch {
   uint32_t lds;             // of a workgroup of small matrices
 };
 
-// The tile that takes the least time by a rough model: a workgroup's share of the rate that products of this tile reach
-// with all its slots filled, for as many rounds as there are tiles.
-int tile_for(int64_t m, int64_t n, int64_t items) {
-  struct Kind { int tile; double slots, rate; };
-  constexpr Kind kinds[3] = {{256, 256, 1.0}, {128, 512, 0.9}, {64, 1024, 0.5}};
-  int best = 0;
-  double least = std::numeric_limits<double>::infinity();
-  for (const Kind& k : kinds) {
-    const double mp = padded(m, k.tile), np = padded(n, k.tile), mt = mp / k.tile, nt = np / k.tile;
-    if (noloco::ns_x_bytes(padded(m, k.tile), padded(n, k.tile), 2) >> 32 != 0) continue;      // a buffer's offsets have 32 bits
-    const double each = 2.0 * k.tile * k.tile * k.slots / k.rate;
-    auto rounds = [&](double tiles) { return std::max(1.0, tiles * items / k.slots); };
-    const double time = each * (rounds(mt * (mt + 1) / 2) * (n + m) + rounds(mt * nt) * m);
-    if (time < least) { least = time; best = k.tile; }
+// Tiles of 256 have the highest rate (4096^2, binary16, us a step: 256 1972, 128 2556) but take whole CUs: with less than two
+// rounds of them smaller ones are ahead (eight matrices of 2048^2 327 / 285, thirty-two 1060 / 1254), and below 1024 rows
+// too (96 of 768^2 in pairs 685 / 630; 48 of 768 x 3072 1091 / 971).  Tiles of 64 pay where those of 128 leave most CUs idle
+// (two matrices of 768^2 24 / 33, eight 63 / 50).  Tiles of X X^T are counted, of all matrices that go through launches together.
+constexpr int64_t kTiles256 = 512, kTiles128 = 96, kRows256 = 1024;
+
+int64_t lower_tiles(int64_t m, int tile) {
+  const int64_t t = padded(m, tile) / tile;
+  return t * (t + 1) / 2;
+}
+
+// Padding to 256 may cost a tenth of the products.
+bool pads_well(int64_t m, int64_t n) {
+  const double big = double(padded(m, 256)) * padded(m, 256) * padded(n, 256), less = double(padded(m, 128)) * padded(m, 128) * padded(n, 128);
+  return m >= kRows256 && big <= 1.1 * less && noloco::ns_x_bytes(padded(m, 256), padded(n, 256), 2) >> 32 == 0;
+}
+
+void choose_tiles(std::vector<Shape>* shapes) {
+  int64_t big = 0, all = 0;
+  for (const Shape& s : *shapes) {
+    if (s.small(1)) continue;
+    if (pads_well(s.m(), s.n())) big += s.items * lower_tiles(s.m(), 256);
+    all += s.items * lower_tiles(s.m(), 128);
   }
-  return best;
+  for (Shape& s : *shapes) {
+    s.tile = all < kTiles128 ? 64 : (big >= kTiles256 && pads_well(s.m(), s.n()) ? 256 : 128);
+    if (noloco::ns_x_bytes(padded(s.m(), s.tile), padded(s.n(), s.tile), 2) >> 32 != 0) s.tile = 64;      // a buffer's offsets have 32 bits
+  }
 }
 
 }  // namespace
@@ -254,10 +266,12 @@ noloco_status create_muon_plan(const noloco_matrix* given, int32_t num, int64_t 
       ++end;
     }
     s.items = static_cast<uint32_t>(items.size()) - s.first_item;
-    s.tile = tile_for(s.m(), s.n(), s.items);
+    s.tile = 64;
     shapes.push_back(s);
     i = end;
   }
+  choose_tiles(&shapes);
+
   uint64_t all[2] = {0, 0}, largest = 0;
   for (const Shape& s : shapes)
     for (int planes = 1; planes <= 2; ++planes)

@@ -127,9 +127,13 @@ template <typename E, int N> struct Numbers {
     }
   }
   __device__ __forceinline__ void store(E* p) const {
-    static_assert(sizeof(E) == 4, "momentum");
-    if constexpr (N == 4) *reinterpret_cast<vector*>(p) = vector{v[0], v[1], v[2], v[3]};
-    else *p = v[0];
+    E raw[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (sizeof(E) == 2) raw[i] = narrow(v[i]); else raw[i] = v[i];
+    }
+    if constexpr (N == 4) *reinterpret_cast<vector*>(p) = vector{raw[0], raw[1], raw[2], raw[3]};
+    else *p = raw[0];
   }
 };
 
@@ -141,29 +145,6 @@ template <typename Out> __device__ __forceinline__ void put_result(const NsArray
     v = old * arrays.keep - by * v;
   }
   if constexpr (sizeof(Out) == 2) *at = narrow(v); else *at = v;
-}
-
-// Four neighbouring ones, of which `there` exist; `whole` if they are aligned as one vector.
-template <typename Out>
-__device__ __forceinline__ void put_four(const NsArrays& arrays, Out* at, float by, float4v v, int there, bool whole) {
-  if (whole && there >= 4) {
-    typedef Out out4 __attribute__((ext_vector_type(4)));
-    out4 got;
-    if (arrays.update) got = *reinterpret_cast<const out4*>(at);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float value = v[k];
-      if (arrays.update) {
-        float old;
-        if constexpr (sizeof(Out) == 2) old = widen(got[k]); else old = got[k];
-        value = old * arrays.keep - by * value;
-      }
-      if constexpr (sizeof(Out) == 2) got[k] = narrow(value); else got[k] = value;
-    }
-    *reinterpret_cast<out4*>(at) = got;
-  } else {
-    for (int k = 0; k < 4 && k < there; ++k) put_result(arrays, at + k, by, v[k]);
-  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1082,20 +1063,39 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
       const uint32_t wide = tall ? kHalf : T, high = tall ? T : kHalf, lds_row = tall ? kFloatTallRow : kFloatRow;
       const uint32_t row0 = tall ? r0 : c0 + h * kHalf, col0 = tall ? c0 + h * kHalf : r0;
       const uint32_t rows = tall ? cls.n : cls.m, cols = tall ? cls.m : cls.n;
-      if (vectors) {
-        for (uint32_t v = thread; v < high * (wide / 4); v += kThreads) {
-          const uint32_t r = v / (wide / 4), c = v % (wide / 4) * 4;
-          if (row0 + r >= rows || col0 + c >= cols) continue;
-          put_four(arrays, out + static_cast<int64_t>(row0 + r) * item.row_stride + col0 + c, by,
-                   *reinterpret_cast<const float4v*>(lds + r * lds_row + c * 4), static_cast<int>(cols - col0 - c), true);
+      // Eight vectors (numbers, where they are none) of a thread at a time, what was there asked for before the first is written.
+      auto write = [&](auto four) {
+        constexpr int V = four ? 4 : 1;
+        for (uint32_t v0 = thread; v0 < high * (wide / V); v0 += 8 * kThreads) {
+          Numbers<Out, V> old[8];
+          Out* at[8];
+          uint32_t r[8], c[8];
+          int there[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const uint32_t v = v0 + k * kThreads;
+            r[k] = v / (wide / V);
+            c[k] = v % (wide / V) * V;
+            there[k] = v < high * (wide / V) && row0 + r[k] < rows ? static_cast<int>(cols) - static_cast<int>(col0 + c[k]) : 0;
+            at[k] = out + (there[k] > 0 ? static_cast<int64_t>(row0 + r[k]) * item.row_stride + col0 + c[k] : 0);
+            if (there[k] >= V && arrays.update) old[k].load(at[k]);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            if (there[k] <= 0) continue;
+            const float* from = reinterpret_cast<const float*>(lds + r[k] * lds_row + c[k] * 4);
+            if (there[k] >= V) {
+              Numbers<Out, V> value;
+#pragma unroll
+              for (int i = 0; i < V; ++i) value.v[i] = arrays.update ? old[k].v[i] * arrays.keep - by * from[i] : from[i];
+              value.store(at[k]);
+            } else {
+              for (int i = 0; i < there[k]; ++i) put_result(arrays, at[k] + i, by, from[i]);
+            }
+          }
         }
-      } else {
-        for (uint32_t v = thread; v < high * wide; v += kThreads) {
-          const uint32_t r = v / wide, c = v % wide;
-          if (row0 + r >= rows || col0 + c >= cols) continue;
-          put_result(arrays, out + static_cast<int64_t>(row0 + r) * item.row_stride + col0 + c, by, *reinterpret_cast<const float*>(lds + r * lds_row + c * 4));
-        }
-      }
+      };
+      if (vectors) write(Yes{}); else write(No{});
     }
   }
 }
