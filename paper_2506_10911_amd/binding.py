@@ -52,15 +52,6 @@ class _Matrix(C.Structure):
                 ("scale", C.c_float)]
 
 
-class _NewtonSchulz(C.Structure):
-    _fields_ = [("steps", C.c_int32), ("coefficients", C.POINTER(C.c_float)), ("eps", C.c_float),
-                ("products", C.c_int32)]
-
-
-class _MuonHParams(C.Structure):
-    _fields_ = [("lr", C.c_float), ("mu", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32)]
-
-
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(
@@ -108,21 +99,10 @@ def _load():
     L.noloco_muon_plan_destroy.argtypes = [C.c_void_p]
     L.noloco_muon_plan_info.restype = C.c_int
     L.noloco_muon_plan_info.argtypes = [C.c_void_p, C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
-    L.noloco_orthogonalize.restype = C.c_int
-    L.noloco_orthogonalize.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.POINTER(_NewtonSchulz), C.c_void_p]
-    L.noloco_muon_step.restype = C.c_int
-    L.noloco_muon_step.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(_MuonHParams),
-                                   C.POINTER(_NewtonSchulz), C.c_void_p]
     L.noloco_embedding_plan_create.restype = C.c_int
     L.noloco_embedding_plan_create.argtypes = [C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int64, C.POINTER(C.c_void_p)]
     L.noloco_embedding_plan_destroy.restype = C.c_int
     L.noloco_embedding_plan_destroy.argtypes = [C.c_void_p]
-    L.noloco_embed_lookup.restype = C.c_int
-    L.noloco_embed_lookup.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_void_p,
-                                      C.c_int32, C.c_void_p]
-    L.noloco_embed_gradient.restype = C.c_int
-    L.noloco_embed_gradient.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_void_p,
-                                        C.c_int32, C.c_int32, C.c_void_p]
     L.noloco_copy_probe.restype = C.c_int
     L.noloco_copy_probe.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
     L.noloco_read_probe.restype = C.c_int
@@ -150,6 +130,8 @@ def _load_calls():
     functions = (_lib.noloco_plan_groups, _lib.noloco_outer_step, _lib.noloco_replica_spread,
                  _lib.noloco_replica_spread_noalloc)
     _calls.bind(*(C.cast(f, C.c_void_p).value for f in functions), _int32)
+    inner = (_lib.noloco_orthogonalize, _lib.noloco_muon_step, _lib.noloco_embed_lookup, _lib.noloco_embed_gradient)
+    _calls.bind_inner(*(C.cast(f, C.c_void_p).value for f in inner))
     return _calls
 
 
@@ -310,7 +292,7 @@ class MuonPlan:
     (offset, rows, cols, row_stride) or (offset, rows, cols, row_stride, scale)."""
 
     def __init__(self, matrices, worker_stride: int, W: int, workspace_bytes: int = 0):
-        self._handle = C.c_void_p(0)
+        self._handle, self._address = C.c_void_p(0), 0
         self.worker_stride, self.W = int(worker_stride), int(W)
         arr = (_Matrix * max(len(matrices), 1))()
         for slot, m in zip(arr, matrices):
@@ -319,6 +301,7 @@ class MuonPlan:
             slot.scale = float(m[4]) if len(m) > 4 else 1.0
         _check(_lib.noloco_muon_plan_create(arr, len(matrices), self.worker_stride, self.W, int(workspace_bytes),
                                             C.byref(self._handle)), "noloco_muon_plan_create")
+        self._address = self._handle.value
 
     def info(self):
         e, b, one, two = C.c_int64(), C.c_int64(), C.c_int32(), C.c_int32()
@@ -329,7 +312,7 @@ class MuonPlan:
 
     def destroy(self):
         if self._handle:
-            handle, self._handle = self._handle, C.c_void_p(0)
+            handle, self._handle, self._address = self._handle, C.c_void_p(0), 0
             _check(_lib.noloco_muon_plan_destroy(handle), "noloco_muon_plan_destroy")
 
     def __del__(self):
@@ -339,28 +322,21 @@ class MuonPlan:
             pass
 
 
-def _newton_schulz(coefficients, eps, products):
-    flat = [float(v) for step in coefficients for v in step]
-    if len(flat) != 3 * len(coefficients):
-        raise ValueError("coefficients: three numbers for every step")
-    return _NewtonSchulz(len(coefficients), (C.c_float * max(len(flat), 1))(*flat), float(eps), int(products))
-
-
 def orthogonalize(plan: MuonPlan, x, x_dtype: int, out, out_dtype: int, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
                   products: int = PRODUCTS_AUTO, stream=None):
     """noloco_orthogonalize: out <- Newton-Schulz of every matrix of the plan in x, one (a, b, c) for every step."""
-    method = _newton_schulz(coefficients, eps, products)
-    _check(_lib.noloco_orthogonalize(plan._handle, _ptr(x), int(x_dtype), _ptr(out), int(out_dtype), C.byref(method),
-                                     _stream(stream)), "noloco_orthogonalize")
+    status = _calls.orthogonalize(plan._address, x, x_dtype, out, out_dtype, coefficients, eps, products, _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_orthogonalize")
 
 
 def muon_step(plan: MuonPlan, theta, theta_dtype: int, grad, grad_dtype: int, momentum, hparams, nesterov: bool = True,
               coefficients=NEWTON_SCHULZ, eps: float = 1e-7, products: int = PRODUCTS_AUTO, stream=None):
     """noloco_muon_step: one update of every matrix of the plan in place; hparams = (lr, mu, weight_decay)."""
-    method = _newton_schulz(coefficients, eps, products)
-    hp = _MuonHParams(float(hparams[0]), float(hparams[1]), float(hparams[2]), int(nesterov))
-    _check(_lib.noloco_muon_step(plan._handle, _ptr(theta), int(theta_dtype), _ptr(grad), int(grad_dtype), _ptr(momentum),
-                                 C.byref(hp), C.byref(method), _stream(stream)), "noloco_muon_step")
+    status = _calls.muon_step(plan._address, theta, theta_dtype, grad, grad_dtype, momentum, hparams, nesterov, coefficients,
+                              eps, products, _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_muon_step")
 
 
 class EmbeddingPlan:
@@ -368,13 +344,14 @@ class EmbeddingPlan:
     row, for up to max_tokens tokens a worker."""
 
     def __init__(self, offset: int, vocab: int, width: int, worker_stride: int, W: int, max_tokens: int):
-        self._handle = C.c_void_p(0)
+        self._handle, self._address = C.c_void_p(0), 0
         _check(_lib.noloco_embedding_plan_create(int(offset), int(vocab), int(width), int(worker_stride), int(W),
                                                  int(max_tokens), C.byref(self._handle)), "noloco_embedding_plan_create")
+        self._address = self._handle.value
 
     def destroy(self):
         if self._handle:
-            handle, self._handle = self._handle, C.c_void_p(0)
+            handle, self._handle, self._address = self._handle, C.c_void_p(0), 0
             _check(_lib.noloco_embedding_plan_destroy(handle), "noloco_embedding_plan_destroy")
 
     def __del__(self):
@@ -387,17 +364,19 @@ class EmbeddingPlan:
 def embed_lookup(plan: EmbeddingPlan, table, table_dtype: int, tokens, token_type: int, num_tokens: int, scale: float, out,
                  out_dtype: int, stream=None):
     """noloco_embed_lookup: out[w, t] <- scale * table_w[tokens[w, t]], zeros where the token is no row of the table."""
-    _check(_lib.noloco_embed_lookup(plan._handle, _ptr(table), int(table_dtype), _ptr(tokens), int(token_type),
-                                    int(num_tokens), float(scale), _ptr(out), int(out_dtype), _stream(stream)),
-           "noloco_embed_lookup")
+    status = _calls.embed_lookup(plan._address, table, table_dtype, tokens, token_type, num_tokens, scale, out, out_dtype,
+                                 _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_embed_lookup")
 
 
 def embed_gradient(plan: EmbeddingPlan, dout, dout_dtype: int, tokens, token_type: int, num_tokens: int, scale: float, grad,
                    grad_dtype: int, accumulate: bool = False, stream=None):
     """noloco_embed_gradient: grad_w[v] <- (grad_w[v] if accumulate) + scale * sum of dout[w, t] over tokens[w, t] = v."""
-    _check(_lib.noloco_embed_gradient(plan._handle, _ptr(dout), int(dout_dtype), _ptr(tokens), int(token_type),
-                                      int(num_tokens), float(scale), _ptr(grad), int(grad_dtype), int(accumulate),
-                                      _stream(stream)), "noloco_embed_gradient")
+    status = _calls.embed_gradient(plan._address, dout, dout_dtype, tokens, token_type, num_tokens, scale, grad, grad_dtype,
+                                   accumulate, _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_embed_gradient")
 
 
 def copy_probe(dst, src, nbytes: int, stream=None):

@@ -182,6 +182,150 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t count) {
   Py_RETURN_NONE;
 }
 
+decltype(&noloco_orthogonalize) orthogonalize_fn = nullptr;
+decltype(&noloco_muon_step) muon_step_fn = nullptr;
+decltype(&noloco_embed_lookup) lookup_fn = nullptr;
+decltype(&noloco_embed_gradient) gradient_fn = nullptr;
+
+bool int32_of(PyObject* x, int32_t* out) {
+  *out = static_cast<int32_t>(PyLong_AsUnsignedLongLongMask(x));
+  return !PyErr_Occurred();
+}
+
+bool float_of(PyObject* x, float* out) {
+  PyObject* value = PyNumber_Float(x);
+  if (value == nullptr) return false;
+  *out = static_cast<float>(PyFloat_AS_DOUBLE(value));
+  Py_DECREF(value);
+  return true;
+}
+
+// Newton-Schulz coefficients, a sequence of (a, b, c) for every step, with eps and products.  More steps than the library
+// takes are counted but not kept: it refuses them by their number.
+struct Method {
+  float k[3 * NOLOCO_MAX_NEWTON_SCHULZ_STEPS];
+  noloco_newton_schulz method;
+  bool open(PyObject* coefficients, PyObject* eps, PyObject* products) {
+    const Py_ssize_t steps = PySequence_Size(coefficients);
+    if (steps < 0) return false;
+    for (Py_ssize_t s = 0; s < steps; ++s) {
+      PyObject* step = PySequence_GetItem(coefficients, s);
+      if (step == nullptr) return false;
+      const Py_ssize_t count = PySequence_Size(step);
+      if (count != 3) {
+        Py_DECREF(step);
+        if (count >= 0) PyErr_SetString(PyExc_ValueError, "coefficients: three numbers for every step");
+        return false;
+      }
+      for (Py_ssize_t i = 0; i < 3; ++i) {
+        float value;
+        if (!float_at(step, i, &value)) {
+          Py_DECREF(step);
+          return false;
+        }
+        if (s < NOLOCO_MAX_NEWTON_SCHULZ_STEPS) k[3 * s + i] = value;
+      }
+      Py_DECREF(step);
+    }
+    method.steps = steps > INT32_MAX ? INT32_MAX : static_cast<int32_t>(steps);
+    method.coefficients = k;
+    return float_of(eps, &method.eps) && int32_of(products, &method.products);
+  }
+};
+
+// orthogonalize(plan, x, x_dtype, out, out_dtype, coefficients, eps, products, stream)
+PyObject* orthogonalize(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  if (!counted(count, 9)) return nullptr;
+  void *plan, *x, *out, *stream;
+  int32_t x_dtype, out_dtype;
+  Method method;
+  if (!address_of(args[0], &plan) || !address_of(args[1], &x) || !int32_of(args[2], &x_dtype) || !address_of(args[3], &out) ||
+      !int32_of(args[4], &out_dtype) || !method.open(args[5], args[6], args[7]) || !address_of(args[8], &stream))
+    return nullptr;
+  noloco_status status;
+  Py_BEGIN_ALLOW_THREADS
+  status = orthogonalize_fn(static_cast<noloco_muon_plan*>(plan), x, x_dtype, out, out_dtype, &method.method, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// muon_step(plan, theta, theta_dtype, grad, grad_dtype, momentum, (lr, mu, weight_decay), nesterov, coefficients, eps, products, stream)
+PyObject* muon_step(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  if (!counted(count, 12)) return nullptr;
+  void *plan, *theta, *grad, *momentum, *stream;
+  int32_t theta_dtype, grad_dtype;
+  noloco_muon_hparams hp;
+  Method method;
+  if (!address_of(args[0], &plan) || !address_of(args[1], &theta) || !int32_of(args[2], &theta_dtype) || !address_of(args[3], &grad) ||
+      !int32_of(args[4], &grad_dtype) || !address_of(args[5], &momentum) || !float_at(args[6], 0, &hp.lr) || !float_at(args[6], 1, &hp.mu) ||
+      !float_at(args[6], 2, &hp.weight_decay) || !int32_of(args[7], &hp.nesterov) || !method.open(args[8], args[9], args[10]) ||
+      !address_of(args[11], &stream))
+    return nullptr;
+  noloco_status status;
+  Py_BEGIN_ALLOW_THREADS
+  status = muon_step_fn(static_cast<noloco_muon_plan*>(plan), theta, theta_dtype, grad, grad_dtype, static_cast<float*>(momentum), &hp,
+                        &method.method, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// What lookup and gradient share: (plan, first, first_dtype, tokens, token_type, num_tokens, scale, second, second_dtype ...)
+struct Embedding {
+  void *plan, *first, *tokens, *second;
+  int32_t first_dtype, token_type, second_dtype;
+  int64_t num_tokens;
+  float scale;
+  bool open(PyObject* const* args) {
+    if (!address_of(args[0], &plan) || !address_of(args[1], &first) || !int32_of(args[2], &first_dtype) || !address_of(args[3], &tokens) ||
+        !int32_of(args[4], &token_type))
+      return false;
+    num_tokens = PyLong_AsLongLong(args[5]);
+    return !PyErr_Occurred() && float_of(args[6], &scale) && address_of(args[7], &second) && int32_of(args[8], &second_dtype);
+  }
+};
+
+// embed_lookup(plan, table, table_dtype, tokens, token_type, num_tokens, scale, out, out_dtype, stream)
+PyObject* embed_lookup(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  if (!counted(count, 10)) return nullptr;
+  Embedding e;
+  void* stream;
+  if (!e.open(args) || !address_of(args[9], &stream)) return nullptr;
+  noloco_status status;
+  Py_BEGIN_ALLOW_THREADS
+  status = lookup_fn(static_cast<noloco_embedding_plan*>(e.plan), e.first, e.first_dtype, e.tokens, e.token_type, e.num_tokens, e.scale,
+                     e.second, e.second_dtype, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// embed_gradient(plan, dout, dout_dtype, tokens, token_type, num_tokens, scale, grad, grad_dtype, accumulate, stream)
+PyObject* embed_gradient(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  if (!counted(count, 11)) return nullptr;
+  Embedding e;
+  int32_t accumulate;
+  void* stream;
+  if (!e.open(args) || !int32_of(args[9], &accumulate) || !address_of(args[10], &stream)) return nullptr;
+  noloco_status status;
+  Py_BEGIN_ALLOW_THREADS
+  status = gradient_fn(static_cast<noloco_embedding_plan*>(e.plan), e.first, e.first_dtype, e.tokens, e.token_type, e.num_tokens, e.scale,
+                       e.second, e.second_dtype, accumulate, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// bind_inner(addresses of noloco_orthogonalize, _muon_step, _embed_lookup, _embed_gradient)
+PyObject* bind_inner(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  if (!counted(count, 4)) return nullptr;
+  void* fn[4];
+  for (int i = 0; i < 4; ++i)
+    if (!address_of(args[i], &fn[i])) return nullptr;
+  orthogonalize_fn = reinterpret_cast<decltype(orthogonalize_fn)>(fn[0]);
+  muon_step_fn = reinterpret_cast<decltype(muon_step_fn)>(fn[1]);
+  lookup_fn = reinterpret_cast<decltype(lookup_fn)>(fn[2]);
+  gradient_fn = reinterpret_cast<decltype(gradient_fn)>(fn[3]);
+  Py_RETURN_NONE;
+}
+
 template <typename F> PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
 PyMethodDef methods[] = {
@@ -190,6 +334,11 @@ PyMethodDef methods[] = {
     {"outer_step", fast(outer_step), METH_FASTCALL, nullptr},
     {"replica_spread", fast(replica_spread), METH_FASTCALL, nullptr},
     {"replica_spread_noalloc", fast(replica_spread_noalloc), METH_FASTCALL, nullptr},
+    {"bind_inner", fast(bind_inner), METH_FASTCALL, nullptr},
+    {"orthogonalize", fast(orthogonalize), METH_FASTCALL, nullptr},
+    {"muon_step", fast(muon_step), METH_FASTCALL, nullptr},
+    {"embed_lookup", fast(embed_lookup), METH_FASTCALL, nullptr},
+    {"embed_gradient", fast(embed_gradient), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -40,7 +40,7 @@ def test_embedding_plans_refused(status, args):
 
 def test_null_plans_refused():
     class NoPlan:
-        _handle = None
+        _address = 0
     refused(1, nl.orthogonalize, NoPlan, 256, nl.F32, 512, nl.F32, stream=0)
     refused(1, nl.muon_step, NoPlan, 256, nl.F32, 512, nl.F32, 1024, (0.1, 0.9, 0.0), stream=0)
     refused(1, nl.embed_lookup, NoPlan, 256, nl.F32, 512, nl.I32, 1, 1.0, 1024, nl.F32, stream=0)
@@ -48,8 +48,10 @@ def test_null_plans_refused():
 
 
 def test_coefficients_come_in_threes():
+    class NoPlan:
+        _address = 0
     with pytest.raises(ValueError):
-        nl.orthogonalize(None, 0, nl.F32, 0, nl.F32, coefficients=((1.0, 2.0),), stream=0)
+        nl.orthogonalize(NoPlan, 0, nl.F32, 0, nl.F32, coefficients=((1.0, 2.0),), stream=0)
 
 
 def test_host_code_is_clean_under_asan_and_ubsan(tmp_path):
