@@ -54,6 +54,8 @@ struct NsArgs {
   const NsItem* items;
   char* workspace;
   double* sums;                 // [item][kNsChunks]
+  NsClass first;                // the table's first class, which is often the only one: its workgroups read no table
+  uint32_t first_end;
 };
 
 // What an item's buffers hold, in bytes from their start: X and the next X [mp][np], A and P [mp][mp], each number

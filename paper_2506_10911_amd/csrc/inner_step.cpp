@@ -60,6 +60,8 @@ struct Batch {
   uint32_t first_table;
   uint32_t groups[kTables];
   uint32_t lds;             // of a workgroup of small matrices
+  NsClass first[kTables];   // of the tables
+  uint32_t first_end[kTables];
 };
 
 // Tiles of 256 have the highest rate (4096^2, binary16, us a step: 256 1972, 128 2556) but take whole CUs: with less than two
@@ -217,6 +219,10 @@ uint32_t make_batches(std::vector<Shape> shapes, int planes, uint64_t room, std:
       ++shape;
       done = 0;
     }
+    for (int k = 0; k < kTables; ++k) {
+      b.first[k] = table[k].cls[0];
+      b.first_end[k] = table[k].end[0];
+    }
     out->push_back(b);
     tables->insert(tables->end(), table, table + (small ? 1 : kTables));
     if (!small) most = std::max(most, items);
@@ -351,7 +357,7 @@ noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, 
   steps.count = method->steps;
   std::copy(method->coefficients, method->coefficients + 3 * method->steps, steps.k);
   for (const Batch& b : plan->batches[planes - 1]) {
-    auto args = [&](int table) { return NsArgs{plan->tables + b.first_table + table, plan->items, plan->workspace, plan->sums}; };
+    auto args = [&](int table) { return NsArgs{plan->tables + b.first_table + table, plan->items, plan->workspace, plan->sums, b.first[table], b.first_end[table]}; };
     if (b.tile == 0) {
       if (noloco::launch_ns_small(args(kSums), arrays, steps, planes, b.groups[kSums], b.lds, stream) != 0) return NOLOCO_ERR_DEVICE;
       continue;

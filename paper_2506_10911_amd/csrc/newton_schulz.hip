@@ -74,17 +74,21 @@ __device__ __forceinline__ NsItem item_at(const NsArgs& args, uint32_t i) {
 // Which class and item workgroup `group` works on, and which workgroup of the item it is.
 struct Place { NsClass cls; uint32_t item, part; };
 __device__ __forceinline__ Place locate(const NsArgs& args, uint32_t group) {
-  const scalar_memory NsTable* table = (const scalar_memory NsTable*)args.table;
-  uint32_t cls = 0, begin = 0;
+  Place p{args.first, 0, 0};
+  uint32_t begin = 0;
+  if (group >= args.first_end) {
+    const scalar_memory NsTable* table = (const scalar_memory NsTable*)args.table;
+    uint32_t cls = 0;
 #pragma unroll
-  for (int i = 0; i < kNsClasses - 1; ++i) {
-    const uint32_t end = table->end[i];
-    const bool past = end <= group;
-    cls += past ? 1u : 0u;
-    begin = past ? end : begin;
+    for (int i = 0; i < kNsClasses - 1; ++i) {
+      const uint32_t end = table->end[i];
+      const bool past = end <= group;
+      cls += past ? 1u : 0u;
+      begin = past ? end : begin;
+    }
+    const scalar_memory NsClass* c = table->cls + cls;
+    p.cls = {c->base, c->item_bytes, c->per_item, c->first_item, c->first_sum, c->m, c->n, c->mp, c->np, c->tall};
   }
-  const scalar_memory NsClass* c = table->cls + cls;
-  Place p{{c->base, c->item_bytes, c->per_item, c->first_item, c->first_sum, c->m, c->n, c->mp, c->np, c->tall}, 0, 0};
   const uint32_t at = group - begin;
   p.item = at / p.cls.per_item;
   p.part = at - p.item * p.cls.per_item;
@@ -969,14 +973,12 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
             const uint32_t r = r0 + r_of + i * 32 + e * 2, c = c0 + wc * (T / WC) + fr + j * 32;
-            const char* from = gram + c * to_ld + (PLANES == 1 ? r * 2 : (r / 32) * 128 + (r % 32) * 2);
-            const half4 high = *reinterpret_cast<const half4*>(from);
-            half4 low;
-            if constexpr (PLANES == 2) low = *reinterpret_cast<const half4*>(from + 64);
+            // A is symmetric: its columns are read as rows, whose neighbouring numbers neighbouring lanes take
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              float v = static_cast<float>(high[k]);
-              if constexpr (PLANES == 2) v += static_cast<float>(low[k]);
+              const char* from = gram + (r + k) * to_ld + (PLANES == 1 ? c * 2 : (c / 32) * 128 + (c % 32) * 2);
+              float v = static_cast<float>(*reinterpret_cast<const _Float16*>(from));
+              if constexpr (PLANES == 2) v += static_cast<float>(*reinterpret_cast<const _Float16*>(from + 64));
               acc[i][j][e + k] = square * acc[i][j][e + k] + linear * v + (r + k == c ? constant : 0.f);
             }
           }

@@ -85,6 +85,7 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
     }
     if (launch.what != 3 && ++in_batch == 8) { in_batch = 0; ++batch; }
     CHECK(launch.groups > 0 && launch.groups <= (1u << 22) + (1u << 21));
+    CHECK(launch.args.first_end == launch.args.table->end[0] && std::memcmp(&launch.args.first, &launch.args.table->cls[0], sizeof(NsClass)) == 0);
     uint32_t last = 0;
     uint64_t end_of_last = 0;
     for (int i = 0; i < kNsClasses && launch.args.table->end[i] != 0xffffffffu; ++i) {
