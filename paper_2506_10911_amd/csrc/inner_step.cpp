@@ -42,6 +42,7 @@ struct Shape {
   uint32_t rows, cols;      // as stored
   int tile;
   uint32_t first_item, items;
+  bool alone[2];            // goes through all steps in one workgroup (one binary16 a number, pairs)
   uint32_t m() const { return std::min(rows, cols); }
   uint32_t n() const { return std::max(rows, cols); }
   uint32_t mp() const { return padded(m(), tile); }
@@ -49,7 +50,8 @@ struct Shape {
   uint64_t item_bytes(int planes) const { return noloco::ns_item_bytes(mp(), np(), planes); }
   uint64_t small_bytes(int planes) const { return noloco::ns_small_bytes(m(), n(), planes); }
   // Four rows of P are what a wave keeps of a column: 128.
-  bool small(int planes) const { return m() <= 128 && uint64_t(m()) * ((n() + 7) / 8 * 8) <= noloco::ns_small_numbers(planes) && small_bytes(planes) <= noloco::kNsSmallLds; }
+  bool small(int planes) const { return alone[planes - 1]; }
+  bool fits_lds(int planes) const { return m() <= 128 && uint64_t(m()) * ((n() + 7) / 8 * 8) <= noloco::ns_small_numbers(planes) && small_bytes(planes) <= noloco::kNsSmallLds; }
 };
 
 // What goes through the products together: where the tables of its launches are among all of them, and their workgroups.
@@ -64,11 +66,12 @@ struct Batch {
   uint32_t first_end[kTables];
 };
 
-// Tiles of 256 have the highest rate (4096^2, binary16, us a step: 256 1972, 128 2556) but take whole CUs: with less than two
-// rounds of them smaller ones are ahead (eight matrices of 2048^2 327 / 285, thirty-two 1060 / 1254), and below 1024 rows
-// too (96 of 768^2 in pairs 685 / 630; 48 of 768 x 3072 1091 / 971).  Tiles of 64 pay where those of 128 leave most CUs idle
-// (two matrices of 768^2 24 / 33, eight 63 / 50).  Tiles of X X^T are counted, of all matrices that go through launches together.
-constexpr int64_t kTiles256 = 512, kTiles128 = 96, kRows256 = 1024;
+// Tiles of 256 have the highest rate (eight matrices of 4096^2, binary16, us a step: 1972, tiles of 128 2556) but take whole
+// CUs: with less than two rounds of them smaller ones are ahead (eight of 2048^2 327 / 285, thirty-two 1060 / 1254), and below
+// 1024 rows too (96 of 768^2 in pairs 685 / 630; 48 of 768 x 3072 1091 / 971).  Tiles of 64 pay where there are less of 128
+// than CUs: one 1024 x 4096 39 / 70, four of 768^2 32 / 37, eight 44 / 48, sixteen (336 tiles) 72 / 74, one of 2048^2 76 / 76.
+// Tiles of X X^T are counted, of all matrices that go through launches together.
+constexpr int64_t kTiles256 = 512, kTiles128 = 256, kRows256 = 1024, kJoined = 256;
 
 int64_t lower_tiles(int64_t m, int tile) {
   const int64_t t = padded(m, tile) / tile;
@@ -84,13 +87,24 @@ bool pads_well(int64_t m, int64_t n) {
 void choose_tiles(std::vector<Shape>* shapes) {
   int64_t big = 0, all = 0;
   for (const Shape& s : *shapes) {
-    if (s.small(1)) continue;
+    if (s.fits_lds(1)) continue;
     if (pads_well(s.m(), s.n())) big += s.items * lower_tiles(s.m(), 256);
     all += s.items * lower_tiles(s.m(), 128);
   }
   for (Shape& s : *shapes) {
     s.tile = all < kTiles128 ? 64 : (big >= kTiles256 && pads_well(s.m(), s.n()) ? 256 : 128);
     if (noloco::ns_x_bytes(padded(s.m(), s.tile), padded(s.n(), s.tile), 2) >> 32 != 0) s.tile = 64;      // a buffer's offsets have 32 bits
+  }
+  // Small matrices beside others: the others' launches are there anyway, and up to kJoined tiles of P X more cost them less than
+  // a launch of their own, which lasts as long as its slowest workgroup (ragged float matrices, 32 small ones 41 us of 212).
+  for (int planes = 1; planes <= 2; ++planes) {
+    bool others = false;
+    int64_t tiles = 0;
+    for (const Shape& s : *shapes) {
+      if (!s.fits_lds(planes)) others = true;
+      else tiles += int64_t(s.items) * (s.mp() / s.tile) * (s.np() / s.tile);
+    }
+    for (Shape& s : *shapes) s.alone[planes - 1] = s.fits_lds(planes) && !(others && tiles <= kJoined);
   }
 }
 

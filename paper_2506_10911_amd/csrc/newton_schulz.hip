@@ -756,9 +756,15 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t block
 // ones and so on, so that a stage of 128 bytes of every row is 64 numbers, or 32 pairs.
 //
 // A wave owns a (T / WR) x (T / WC) part in 32 x 32 blocks.  The operands come to the LDS by loads that bypass the
-// registers, two stages deep (eight in tiles of 64, which are taken where there are few: nothing else hides a load's way); fragments are read one slice of 16 k ahead of the products that use them, across the
-// stage's end too: the barrier in front of the last slice's products tells that the next stage has come and that
-// this one's buffer is free.
+// registers, two stages deep (tiles of 64, which are taken where there are few, four: two of them share a CU; with eight
+// stages and a CU to itself P X of two 768 x 768 matrices took 10.0 us, so 7.0).  Fragments are read one slice of 16 k ahead
+// of the products that use them, across the stage's end too: the barrier in front of the last slice's products tells that
+// the next stage has come and that this one's buffer is free.
+//
+// What bounds it: a stage of 64 KiB takes 1.55 us of a CU when all CUs are at it, 1.0 of them its products at the clock
+// that the power leaves (1.8 of 2.4 GHz); stages of half the depth, four to five of them, were 2 to 10 % slower, so it is the
+// loads' rate and not their way that the rest is spent on.  P X of 4096 x 16384: 1170 to 1340 TFLOP/s by the card (a large library
+// product 1220 to 1480), X X^T 900 to 950 of those it computes.
 //
 // Rows of 128 bytes: 16-byte chunk q of row r lies at q ^ (r >> 1 & 7), so that the 16 lanes that read at once meet
 // 16 different quarters of the 64 banks.  Rows of X in the transposed operand: chunk q of row k at q ^ (k & 3) << 2
@@ -771,7 +777,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   constexpr int kSlices = kDepth / 16;
   constexpr int kOperand = T * 128;                         // bytes of one operand's stage
   constexpr int kStage = 2 * kOperand;
-  constexpr int kStages = T == 64 ? 8 : 2;
+  constexpr int kStages = T == 64 ? 4 : 2;
   constexpr int MB = T / WR / 32, NB = T / WC / 32;         // a wave's blocks
   constexpr int kLoads = T / 8 / kWaves;                    // of 1 KiB, of a wave, operand and stage
   constexpr int kTurned = T * 2 * PLANES;                   // bytes of a row of the transposed operand
