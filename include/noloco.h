@@ -322,7 +322,7 @@ typedef struct noloco_matrix {
 /* How products take their operands (sums are always binary32).
  *   F16    one binary16 a number: results to a few 2^-12 of their norm, what a bf16 result needs
  *   PAIRS  a pair of binary16 (high and low half, 22 bits) and three products for each: a float result's last bits
- *   AUTO   F16 for bf16 results, PAIRS for float ones */
+ *   AUTO   F16 for bf16 results, PAIRS for float ones and for plans of small matrices only (64 x 352 is, 128 x 128 not) */
 typedef enum noloco_products { NOLOCO_PRODUCTS_AUTO = 0, NOLOCO_PRODUCTS_F16 = 1, NOLOCO_PRODUCTS_PAIRS = 2 } noloco_products;
 
 /*
@@ -393,7 +393,7 @@ typedef struct noloco_muon_hparams {
  *   theta, grad   device, [W][worker_stride] float or bf16
  *   momentum      device, [W][worker_stride] float
  * all NOLOCO_BASE_ALIGN_BYTES-aligned and none overlapping another.  bf16 weights are rounded to nearest once, after the
- * update in float; AUTO takes products by theta's type.  As noloco_orthogonalize otherwise.
+ * update in float; AUTO takes products by theta's type, as there.  As noloco_orthogonalize otherwise.
  */
 noloco_status noloco_muon_step(const noloco_muon_plan* plan, void* theta, int32_t theta_dtype, const void* grad,
                                int32_t grad_dtype, float* momentum, const noloco_muon_hparams* hparams,

@@ -99,11 +99,6 @@ struct Yes { constexpr operator bool() const { return true; } };
 struct No { constexpr operator bool() const { return false; } };
 template <int N> struct Number { static constexpr int value = N; };
 
-template <bool BF16> __device__ __forceinline__ float load_one(const void* p, int64_t i) {
-  if constexpr (BF16) return widen(static_cast<const uint16_t*>(p)[i]);
-  else return static_cast<const float*>(p)[i];
-}
-
 // What is orthogonalised: x, the momentum, or the gradient that looks one step ahead.
 __device__ __forceinline__ float direction(float g, float moved, float mu, bool nesterov) {
   return nesterov ? g + mu * moved : moved;
@@ -161,8 +156,9 @@ template <typename Out> __device__ __forceinline__ void put_result(const NsArray
 // takes 32 columns of X, which nobody else reads, holds them in registers and writes their next values in their place.
 //
 // Numbers come and go in chunks of eight, a thread every 512th chunk: eight along X's row, 16 bytes of the LDS.  (Results of
-// a tall matrix leave as four columns of two rows, since half a wave would write 128 bytes of a row only.)  They are read once: until the norm is known the LDS holds them as binary16 with a power of two for each chunk, or, where
-// there is room for pairs, the two halves of a binary32 number in the places of high and low half.
+// a tall matrix leave as four columns of two rows, since half a wave would write 128 bytes of a row only.)  They are read
+// once: until the norm is known the LDS holds them as binary16 with a power of two for each chunk, or, where there is room
+// for pairs, the two halves of a binary32 number in the places of high and low half.
 template <int PLANES, bool BF16, bool MOMENTUM, typename Out>
 __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArrays arrays, NsSteps steps) {
   extern __shared__ __align__(16) char lds[];

@@ -2,6 +2,7 @@
 // kernel launchers are stand-ins that record what would be launched, device memory is host memory.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
@@ -63,7 +64,7 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
   CHECK(bytes >= 0 && static_cast<size_t>(bytes) <= allocated);
   launches.clear();
   const float k[6] = {1.5f, -.5f, 0.f, 1.5f, -.5f, 0.f};
-  const noloco_newton_schulz method = {2, k, 0.f, NOLOCO_PRODUCTS_AUTO};
+  const noloco_newton_schulz method = {2, k, 0.f, out_dtype == NOLOCO_BF16 ? NOLOCO_PRODUCTS_F16 : NOLOCO_PRODUCTS_PAIRS};
   static char here[256] __attribute__((aligned(256)));
   char* const x = here;
   char* const y = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(here) + uintptr_t(W) * stride * 8 + 4096) / 256 * 256);
@@ -126,6 +127,19 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
     if (m.rows > 0 && m.cols > 0)
       for (int32_t w = 0; w < W; ++w, ++wanted) CHECK(seen[w * stride + m.offset] == 1);
   CHECK(seen.size() == wanted);
+  // products by the result's type, pairs where small matrices are all there is
+  if (!launches.empty()) {
+    bool small = true;
+    for (const noloco_matrix& m : matrices) {
+      const int64_t lo = std::min(m.rows, m.cols), hi = std::max(m.rows, m.cols);
+      small = small && lo <= 128 && lo * ((hi + 7) / 8 * 8) <= static_cast<int64_t>(ns_small_numbers(2)) && ns_small_bytes(lo, hi, 2) <= kNsSmallLds;
+    }
+    const noloco_newton_schulz by_type = {2, k, 0.f, NOLOCO_PRODUCTS_AUTO};
+    launches.clear();
+    CHECK(noloco_orthogonalize(plan, x, NOLOCO_F32, y, out_dtype, &by_type, nullptr) == NOLOCO_OK);
+    for (const Launch& launch : launches)
+      if (launch.what >= 2) CHECK(launch.planes == (out_dtype == NOLOCO_BF16 && !small ? 1 : 2));
+  }
   // a launch that the runtime refuses ends the call
   if (!launches.empty()) {
     launches.clear();

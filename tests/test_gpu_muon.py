@@ -133,6 +133,32 @@ def test_other_coefficients(coefficients):
         assert (plain.view(got.cpu(), offset, rows, cols, row_stride)[0].double() - exact).norm().item() <= bound
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("products", ["f16", "pairs"])
+@pytest.mark.parametrize("shapes", [[(1, 1), (1, 70)], [(16, 64)], [(31, 2), (2, 31)], [(64, 64)], [(63, 97), (97, 63)], [(32, 200)], [(33, 300)]],
+                         ids=lambda s: "+".join("x".join(map(str, v)) for v in s))
+def test_small_matrices(shapes, products, out):
+    matrices, stride = layout(shapes)
+    x = filled(matrices, 3, stride, torch.float32, seed=9)
+    plan = nl.MuonPlan(matrices, stride, 3)
+    got = {}
+    for kind in (nl.PRODUCTS_F16, nl.PRODUCTS_PAIRS, nl.PRODUCTS_AUTO):
+        got[kind] = torch.zeros((3, stride), dtype=DTYPES[out], device="cuda")
+        nl.orthogonalize(plan, x.cuda(), nl.F32, got[kind], code(DTYPES[out]), products=kind)
+    check(matrices, got[nl.PRODUCTS_F16 if products == "f16" else nl.PRODUCTS_PAIRS].cpu(), x, products)
+    assert same_bits(got[nl.PRODUCTS_AUTO], got[nl.PRODUCTS_PAIRS])
+
+
+def test_one_large_matrix_takes_bf16_results_to_one_number():
+    matrices, stride = layout([(16, 64), (128, 128)])
+    x = filled(matrices, 1, stride, torch.bfloat16, seed=10)
+    plan = nl.MuonPlan(matrices, stride, 1)
+    got = [torch.zeros((1, stride), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    nl.orthogonalize(plan, x.cuda(), nl.BF16, got[0], nl.BF16)
+    nl.orthogonalize(plan, x.cuda(), nl.BF16, got[1], nl.BF16, products=nl.PRODUCTS_F16)
+    assert same_bits(*got)
+
+
 def test_sizes_of_numbers_do_not_matter():
     """Gradients whose squares leave binary32's range, either way."""
     matrices, stride = layout([(30, 70)])
