@@ -322,7 +322,8 @@ typedef struct noloco_matrix {
 /* How products take their operands (sums are always binary32).
  *   F16    one binary16 a number: results to a few 2^-12 of their norm, what a bf16 result needs
  *   PAIRS  a pair of binary16 (high and low half, 22 bits) and three products for each: a float result's last bits
- *   AUTO   F16 for bf16 results, PAIRS for float ones and for plans of small matrices only (64 x 352 is, 128 x 128 not) */
+ *   AUTO   F16 for bf16 results, PAIRS for float ones and for plans of small matrices only (64 x 352 is, 128 x 128 not),
+ *          or long ones of at most 64 rows or columns */
 typedef enum noloco_products { NOLOCO_PRODUCTS_AUTO = 0, NOLOCO_PRODUCTS_F16 = 1, NOLOCO_PRODUCTS_PAIRS = 2 } noloco_products;
 
 /*

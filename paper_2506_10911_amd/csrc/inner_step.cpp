@@ -117,7 +117,7 @@ struct noloco_muon_plan {
   int64_t elements = 0;
   int64_t workspace_bytes = 0;
   std::vector<Batch> batches[2];     // one binary16 a number, pairs
-  bool tiny = false;                 // every matrix fits a workgroup's LDS in pairs
+  bool pairs = false;                // also bf16 results take pairs
   const NsTable* tables = nullptr;   // these four point into the block
   const NsItem* items = nullptr;
   double* sums = nullptr;
@@ -292,7 +292,7 @@ noloco_status create_muon_plan(const noloco_matrix* given, int32_t num, int64_t 
     i = end;
   }
   choose_tiles(&shapes);
-  plan->tiny = std::all_of(shapes.begin(), shapes.end(), [](const Shape& s) { return s.fits_lds(2); });
+  plan->pairs = std::all_of(shapes.begin(), shapes.end(), [](const Shape& s) { return s.fits_lds(2) || (s.m() <= 64 && !s.fits_lds(1)); });
 
   uint64_t all[2] = {0, 0}, largest = 0;
   for (const Shape& s : shapes)
@@ -366,10 +366,12 @@ noloco_status check_method(const noloco_newton_schulz* method) {
 }
 
 noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, const noloco_newton_schulz* method, void* stream) {
-  // One binary16 a number leaves an error below a bf16 result's own rounding (0.0010 to 0.0016 of the norm, the rounding 0.0017),
-  // the more the less numbers average it.  The smallest matrices, whose step waits more than it computes, take pairs at
-  // 16 x 64 for 15.7 us instead of 13.2 and at 64 x 64 for 21.8 instead of 16.1, and leave the rounding alone.
-  const bool one = method->products == NOLOCO_PRODUCTS_F16 || (method->products == NOLOCO_PRODUCTS_AUTO && arrays.out_bf16 && !plan->tiny);
+  // One binary16 a number leaves an error below a bf16 result's own rounding (0.0007 to 0.0016 of the norm, the rounding 0.0017),
+  // the more the less numbers average it.  The smallest matrices, whose step waits more than it computes, take pairs (us, binary16
+  // and pairs: eight of 16 x 64 16.5 / 15.7, 32 of 64 x 64 19.3 / 22.1) and have the rounding alone.  So have long ones of few
+  // rows that go through launches: their singular values are so alike that one rounding is in all of them (4 x 6000: 0.0067 in
+  // binary16).
+  const bool one = method->products == NOLOCO_PRODUCTS_F16 || (method->products == NOLOCO_PRODUCTS_AUTO && arrays.out_bf16 && !plan->pairs);
   const int planes = one ? 1 : 2;
   noloco::NsSteps steps{};
   steps.count = method->steps;

@@ -155,6 +155,10 @@ template <typename Out> __device__ __forceinline__ void put_result(const NsArray
 // below the diagonal are dealt to the waves (of A with one or three blocks several waves share one's k); of P X a wave
 // takes 32 columns of X, which nobody else reads, holds them in registers and writes their next values in their place.
 //
+// With one binary16 a number the diagonals of A and P keep what it leaves of them, and P X adds it: where n is much more
+// than m all of A's diagonal is nearly the same number, its rounding the same relative error of every singular value, and
+// some steps' polynomials have slopes of ten there (32 x 512: 0.003 of the norm off without, 0.0007 with).
+//
 // Numbers come and go in chunks of eight, a thread every 512th chunk: eight along X's row, 16 bytes of the LDS.  (Results of
 // a tall matrix leave as four columns of two rows, since half a wave would write 128 bytes of a row only.)  They are read
 // once: until the norm is known the LDS holds them as binary16 with a power of two for each chunk, or, where there is room
@@ -435,12 +439,21 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
 
   // The symmetric product of `from` with its transpose, block by block; result(bi, bj, quad, d) makes four of its numbers
   // what is written to both their places in `to`.  With one or three blocks of long rows all waves share their k, and then
-  // their results.
+  // their results.  What single binary16 leave of a number on the diagonal and the three beside
+  // it goes into the row's last 16 bytes.
+  auto rest = [&](const char* matrix, uint32_t row) { return reinterpret_cast<const float*>(matrix + row * a_row + mp * 2)[row & 3]; };
   auto symmetric = [&](const char* from, uint32_t row_bytes, uint32_t slices, char* to, bool share_k, auto result) {
     auto write = [&](uint32_t bi, uint32_t bj, uint32_t quad, float4v d) {
       const float4v v = result(bi, bj, quad, d);
       write_four(to + (bi * 32 + of32) * a_row, bj * 32, quad, v);
       if (bi != bj) write_column(to + bj * 32 * a_row, a_row, bi * 32 + of32, quad, v);
+      else if constexpr (PLANES == 1) {
+        uint32_t fours = of32 & ~3u;
+        asm("" : "+v"(fours));            // compared here: masks kept from step to step do not fit the scalar registers
+        if (quad * 8 + half * 4 == fours) {
+          *reinterpret_cast<float4v*>(to + (bi * 32 + of32) * a_row + mp * 2) = v - __builtin_convertvector(__builtin_convertvector(v, half4), float4v);
+        }
+      }
     };
     if (share_k) {
       // four waves take the block that has two operands to read, two each of the others
@@ -478,8 +491,15 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
       const char* at = gram + col * a_row + spot(bj * 32) + (quad * 8 + half * 4) * 2;
       float4v a = __builtin_convertvector(*reinterpret_cast<const half4*>(at), float4v);
       if constexpr (PLANES == 2) a += __builtin_convertvector(*reinterpret_cast<const half4*>(at + 64), float4v);
+      float on_diagonal = constant;
+      if constexpr (PLANES == 1) {      // A with its diagonal's rests R: A^2 + A R + R A, and A + R
+        const float of_column = rest(gram, col);
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) d[e] = square * d[e] + linear * a[e] + (row + e == col ? constant : 0.f);
+        for (uint32_t e = 0; e < 4; ++e) d[e] += a[e] * (rest(gram, row + e) + of_column);
+        on_diagonal += linear * of_column;
+      }
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) d[e] = square * d[e] + linear * a[e] + (row + e == col ? on_diagonal : 0.f);
       return d;
     });
     // B = mp / 32 blocks of rows
@@ -520,9 +540,15 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
 #pragma unroll
           for (int b = 0; b < kRows; ++b)
             if (b0 + b < B) {
+              char* const row = x + ((b0 + b) * 32 + of32) * x_row;
+              float left = 0.f;
+              if constexpr (PLANES == 1) left = rest(poly, (b0 + b) * 32 + of32);
 #pragma unroll
-              for (int quad = 0; quad < 4; ++quad)
-                write_four(x + ((b0 + b) * 32 + of32) * x_row, j0, quad, four_of(d[b], quad) * (1.f / ns_unit_p(PLANES)));
+              for (int quad = 0; quad < 4; ++quad) {
+                float4v v = four_of(d[b], quad);
+                if constexpr (PLANES == 1) v += __builtin_convertvector(*reinterpret_cast<const half4*>(row + spot(j0) + (quad * 8 + half * 4) * 2), float4v) * left;
+                write_four(row, j0, quad, v * (1.f / ns_unit_p(PLANES)));
+              }
             }
         }
       }

@@ -132,7 +132,8 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
     bool small = true;
     for (const noloco_matrix& m : matrices) {
       const int64_t lo = std::min(m.rows, m.cols), hi = std::max(m.rows, m.cols);
-      small = small && lo <= 128 && lo * ((hi + 7) / 8 * 8) <= static_cast<int64_t>(ns_small_numbers(2)) && ns_small_bytes(lo, hi, 2) <= kNsSmallLds;
+      auto fits = [&](int planes) { return lo <= 128 && lo * ((hi + 7) / 8 * 8) <= static_cast<int64_t>(ns_small_numbers(planes)) && ns_small_bytes(lo, hi, planes) <= kNsSmallLds; };
+      small = small && (fits(2) || (lo <= 64 && !fits(1)));
     }
     const noloco_newton_schulz by_type = {2, k, 0.f, NOLOCO_PRODUCTS_AUTO};
     launches.clear();
