@@ -3,8 +3,8 @@
 //   lookup     out[w][t] = scale * table_w[tokens[w][t]]
 //   gradient   grad_w[v] = (accumulate ? grad_w[v] : 0) + scale * sum of dout[w][t] over the t with tokens[w][t] = v
 //
-// Both are bound by memory.  The gradient's rows are found by sorting (token, position) pairs: lists of 2048 are sorted in
-// the LDS, and sixteen lists at a time are joined by ranks (a pair's place is its place in its own list plus the number
+// Both are bound by memory.  The gradient's rows are found by sorting (token, position) pairs: lists of 2048 are sorted by a
+// workgroup each, and sixteen lists at a time are joined by ranks (a pair's place is its place in its own list plus the number
 // of smaller pairs in each other list).  No atomics anywhere: a row's sum is taken in the order of positions, in chunks
 // of 32 sorted pairs whose sums are joined in order.
 #include <hip/hip_runtime.h>
@@ -85,7 +85,8 @@ __device__ __forceinline__ uint32_t token_at(const EmbedArgs& a, int64_t i) {
   return token >= 0 && token < static_cast<int64_t>(a.vocab) ? static_cast<uint32_t>(token) : a.vocab;
 }
 
-// A wave takes four tokens at a time, whose rows are asked for together.
+// A wave takes four tokens at a time, whose rows are asked for together (one at a time 46 us where four take 43).  Bound by memory:
+// 8 x 8192 rows of 768, float to bf16, 40 us; what is written and the different rows that are read are 190 MB, 4.8 TB/s.
 template <typename Table, typename Row, int N>
 __global__ __launch_bounds__(256) void embed_lookup(EmbedArgs a) {
   constexpr int kTokens = 4;
@@ -142,7 +143,8 @@ template <int GAP> __device__ __forceinline__ uint64_t across(uint64_t v) {
 // A workgroup sorts up to 2048 positions of one worker: a bitonic network over (token, position in the list), keys of 32 bits
 // where tokens leave eleven for the position.  A thread holds places 128 wave + lane and 64 more, so that only places at
 // least 128 apart meet in the LDS, ten of the network's 66 stages; the others are a few instructions each (all stages in the
-// LDS took 16 us).
+// LDS took 16 us).  Bound by the network's chain: 8 x 8192 positions 10.8 us, with keys of 64 bits 17; a few microseconds fewer
+// where there are less.
 template <typename Key>
 __global__ __launch_bounds__(kSortChunk / 2) void embed_sort(EmbedArgs a) {
   constexpr uint32_t kPlaceBits = 11;
@@ -223,7 +225,8 @@ __device__ __forceinline__ int64_t merged_place(Tokens list, int64_t count, int6
 }
 
 // Lists that fit the LDS together.  The tokens of a wave lie between its first and its last one, and so do their places in
-// every other list: thirty-two lanes find these, and each lane searches between them only.
+// every other list: thirty-two lanes find these, and each lane searches between them only.  Bound by the searches' LDS reads:
+// 8 x 8192 positions 8.7 us, 2 x 32768 26.
 __global__ __launch_bounds__(1024) void embed_merge_lds(const uint32_t* token_in, const uint32_t* position_in, uint32_t* token_out,
                                                         uint32_t* position_out, int64_t num_tokens) {
   extern __shared__ uint32_t tokens[];
@@ -275,7 +278,7 @@ __global__ __launch_bounds__(1024) void embed_merge_lds(const uint32_t* token_in
   }
 }
 
-// Longer ones.
+// Longer ones, which do not fit: every search goes to memory.  2 x 200000 positions, the second of two joins, 52 us.
 __global__ __launch_bounds__(256) void embed_merge(const uint32_t* token_in, const uint32_t* position_in, uint32_t* token_out,
                                                    uint32_t* position_out, int64_t num_tokens, int64_t length) {
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
@@ -307,7 +310,9 @@ __device__ __forceinline__ void finish_row(const EmbedArgs& a, Table* at, const 
 // A workgroup takes 32 sorted positions and 256 * N columns.  A token whose positions all lie in the chunk is finished here;
 // the sum of one that the chunk before began goes to slot 0 of the chunk's partial rows, of one that goes on in
 // the next chunk to slot 1 (one that does both: slot 0).  Workgroups beyond the chunks write zeros to 64 rows of the table
-// each, those of tokens that do not come up.
+// each, those of tokens that do not come up.  Which of them do is looked up in the sorted list, so that no memory is cleared
+// and then written.  Bound by memory: 2 x 32768 rows of 4096, bf16, into a table of 50257 rows 277 us, 4.9 TB/s; 8 x 8192 rows of
+// 768 added to what is there 55 us.  Chunks of 32: a token that comes up often is spread over many workgroups.
 template <typename Table, typename Row, int N>
 __global__ __launch_bounds__(256) void embed_sums(EmbedArgs a, const uint32_t* token_list, const uint32_t* position_list, uint32_t chunks) {
   const int64_t w = blockIdx.y, T = a.num_tokens;
@@ -384,7 +389,8 @@ __global__ __launch_bounds__(256) void embed_sums(EmbedArgs a, const uint32_t* t
   }
 }
 
-// Joins the partial sums of the token that begins in a chunk and goes on beyond it.
+// Joins the partial sums of the token that begins in a chunk and goes on beyond it, in order, sixteen on their way at a time.
+// The most frequent token is what it waits for: 8 x 8192 positions 6 us, 2 x 32768 rows of 4096 20.
 template <typename Table, int N>
 __global__ __launch_bounds__(256) void embed_join(EmbedArgs a, const uint32_t* token_list, uint32_t chunks) {
   const int64_t w = blockIdx.y, T = a.num_tokens;

@@ -163,6 +163,12 @@ template <typename Out> __device__ __forceinline__ void put_result(const NsArray
 // a tall matrix leave as four columns of two rows, since half a wave would write 128 bytes of a row only.)  They are read
 // once: until the norm is known the LDS holds them as binary16 with a power of two for each chunk, or, where there is room
 // for pairs, the two halves of a binary32 number in the places of high and low half.
+//
+// What bounds it: each workgroup waits for its own chain.  1152 matrices of 64 x 768 in binary16, float in and bf16 out, take
+// 257 us (1.3 TB/s): four and a half rounds, in each of which all CUs load at once (14 us), then compute (six to seven us a
+// step), then write.  Two steps of loads and products side by side would need two matrices' LDS; asking for the next matrix
+// before the steps needs registers that are not there.  With launches for each product instead: 637 us.  24 matrices of
+// 64 x 64 to 64 x 256 in pairs: 34 us, with launches 99.
 template <int PLANES, bool BF16, bool MOMENTUM, typename Out>
 __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArrays arrays, NsSteps steps) {
   extern __shared__ __align__(16) char lds[];
@@ -613,7 +619,8 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
 
 // One workgroup sums one chunk of an item: numbers part * size .. of the matrix in row-major order, V at a time where
 // rows are whole vectors, and four (V = 1: eight) of a thread's on their way together.  Squares are summed in binary64: gradients
-// are small enough for their squares to leave binary32's range.
+// are small enough for their squares to leave binary32's range.  Bound by memory: 170M numbers, float, 12 bytes each, 381 us,
+// 5.3 TB/s (a copy reaches 5.9).
 template <bool BF16, bool MOMENTUM, int V>
 __device__ __forceinline__ double sum_chunk(const NsArrays& arrays, const NsClass& cls, const NsItem& item, uint32_t part) {
   constexpr int kAtOnce = V == 4 ? 4 : 8;
@@ -690,7 +697,9 @@ __host__ __device__ inline uint32_t chunks_of(uint64_t elements) {
   return c < 1 ? 1 : (c > kNsChunks ? kNsChunks : static_cast<uint32_t>(c));
 }
 
-// A workgroup writes a 64 x 64 tile of X_0, zeros where it is padded.
+// A workgroup writes a 64 x 64 tile of X_0, zeros where it is padded; tall matrices are turned in the LDS.  Each adds up the
+// item's partial sums itself, which costs less than a launch for it.  Bound by memory: the momentum (and gradient) is read again,
+// since a matrix's norm is known only after all of it: 170M numbers, 12 bytes each, 418 us, 4.9 TB/s.
 template <bool BF16, bool MOMENTUM, int PLANES>
 __global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
   __shared__ __align__(16) float tile[64][68];
@@ -764,7 +773,7 @@ __global__ __launch_bounds__(256) void ns_start(NsArgs args, NsArrays arrays) {
 // ---------------------------------------------------------------------------
 
 // Workgroups are dealt to the 8 XCDs in turn; each XCD takes runs of `run` consecutive tiles, which share rows and
-// columns in its L2.
+// columns in its L2: 32 of 256, one round of its CUs, 64 of the smaller ones, of which two share a CU.
 __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t blocks, uint32_t run) {
   const uint32_t whole = blocks / (8 * run) * (8 * run);
   if (block >= whole) return block;
@@ -786,7 +795,10 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t block
 // What bounds it: a stage of 64 KiB takes 1.55 us of a CU when all CUs are at it, 1.0 of them its products at the clock
 // that the power leaves (1.8 of 2.4 GHz); stages of half the depth, four to five of them, were 2 to 10 % slower, so it is the
 // loads' rate and not their way that the rest is spent on.  P X of 4096 x 16384: 1170 to 1340 TFLOP/s by the card (a large library
-// product 1220 to 1480), X X^T 900 to 950 of those it computes.
+// product 1220 to 1480), X X^T 900 to 950 of those it computes.  In pairs (768 x 768 to 768 x 3072, tiles of 128) 900 and 930,
+// three products a number counted.  A symmetric product ends with both its images, from registers the one and through
+// the LDS the other (tiles of 256: gram 6 us of a workgroup's 60, square 13), the last P X with the update of theta in the same
+// way (19 us, of theta's reads mostly).
 //
 // Rows of 128 bytes: 16-byte chunk q of row r lies at q ^ (r >> 1 & 7), so that the 16 lanes that read at once meet
 // 16 different quarters of the 64 banks.  Rows of X in the transposed operand: chunk q of row k at q ^ (k & 3) << 2
