@@ -368,7 +368,7 @@ noloco_status check_method(const noloco_newton_schulz* method) {
 noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, const noloco_newton_schulz* method, void* stream) {
   // One binary16 a number leaves an error below a bf16 result's own rounding (0.0007 to 0.0016 of the norm, the rounding 0.0017),
   // the more the less numbers average it.  The smallest matrices, whose step waits more than it computes, take pairs (us, binary16
-  // and pairs: eight of 16 x 64 16.5 / 15.7, 32 of 64 x 64 19.3 / 22.1) and have the rounding alone.  So have long ones of few
+  // and pairs: eight of 16 x 64 15.9 / 15.7, 32 of 64 x 64 18.2 / 21.6) and have the rounding alone.  So have long ones of few
   // rows that go through launches: their singular values are so alike that one rounding is in all of them (4 x 6000: 0.0067 in
   // binary16).
   const bool one = method->products == NOLOCO_PRODUCTS_F16 || (method->products == NOLOCO_PRODUCTS_AUTO && arrays.out_bf16 && !plan->pairs);

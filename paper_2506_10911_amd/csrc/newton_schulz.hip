@@ -449,8 +449,7 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
   // it goes into the row's last 16 bytes.
   auto rest = [&](const char* matrix, uint32_t row) { return reinterpret_cast<const float*>(matrix + row * a_row + mp * 2)[row & 3]; };
   auto symmetric = [&](const char* from, uint32_t row_bytes, uint32_t slices, char* to, bool share_k, auto result) {
-    auto write = [&](uint32_t bi, uint32_t bj, uint32_t quad, float4v d) {
-      const float4v v = result(bi, bj, quad, d);
+    auto write = [&](uint32_t bi, uint32_t bj, uint32_t quad, float4v v) {
       write_four(to + (bi * 32 + of32) * a_row, bj * 32, quad, v);
       if (bi != bj) write_column(to + bj * 32 * a_row, a_row, bi * 32 + of32, quad, v);
       else if constexpr (PLANES == 1) {
@@ -474,15 +473,19 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
         const uint32_t first = blocks == 1 ? 0 : (block == 0 ? 0 : 2 + block * 2), count = blocks == 1 ? kWaves : (block == 0 ? 4 : 2);
         float4v sum = *reinterpret_cast<const float4v*>(shares + ((first * 4 + quad) * 64 + lane) * 4);
         for (uint32_t other = 1; other < count; ++other) sum += *reinterpret_cast<const float4v*>(shares + (((first + other) * 4 + quad) * 64 + lane) * 4);
-        write(blocks == 1 || block == 1 ? 0 : 1, block == 2 ? 1 : 0, quad, sum);
+        const uint32_t ri = blocks == 1 || block == 1 ? 0 : 1, rj = block == 2 ? 1 : 0;
+        write(ri, rj, quad, result(ri, rj, quad, sum));
       }
     } else {
       for (uint32_t t = wave; t < pairs; t += kWaves) {
         uint32_t bi, bj;
         below(t, bi, bj);
         const float16v d = block_product(from, row_bytes, bi, bj, 0, slices);
+        float4v v[4];                 // all of them, since a read does not overtake a write
 #pragma unroll
-        for (int quad = 0; quad < 4; ++quad) write(bi, bj, quad, four_of(d, quad));
+        for (int quad = 0; quad < 4; ++quad) v[quad] = result(bi, bj, quad, four_of(d, quad));
+#pragma unroll
+        for (int quad = 0; quad < 4; ++quad) write(bi, bj, quad, v[quad]);
       }
     }
     __syncthreads();
@@ -538,6 +541,18 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
           float16v d[kRows];
 #pragma unroll
           for (int b = 0; b < kRows; ++b) d[b] = nothing();
+          half4 before[kRows][4];             // what X is, and of P's diagonal the rests
+          float left[kRows];
+          if constexpr (PLANES == 1) {
+#pragma unroll
+            for (int b = 0; b < kRows; ++b) {
+              if (b0 + b >= B) continue;
+              left[b] = rest(poly, (b0 + b) * 32 + of32);
+#pragma unroll
+              for (int quad = 0; quad < 4; ++quad)
+                before[b][quad] = *reinterpret_cast<const half4*>(x + ((b0 + b) * 32 + of32) * x_row + spot(j0) + (quad * 8 + half * 4) * 2);
+            }
+          }
 #pragma unroll
           for (int k = 0; k < S; ++k)
 #pragma unroll
@@ -547,12 +562,10 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
           for (int b = 0; b < kRows; ++b)
             if (b0 + b < B) {
               char* const row = x + ((b0 + b) * 32 + of32) * x_row;
-              float left = 0.f;
-              if constexpr (PLANES == 1) left = rest(poly, (b0 + b) * 32 + of32);
 #pragma unroll
               for (int quad = 0; quad < 4; ++quad) {
                 float4v v = four_of(d[b], quad);
-                if constexpr (PLANES == 1) v += __builtin_convertvector(*reinterpret_cast<const half4*>(row + spot(j0) + (quad * 8 + half * 4) * 2), float4v) * left;
+                if constexpr (PLANES == 1) v += __builtin_convertvector(before[b][quad], float4v) * left[b];
                 write_four(row, j0, quad, v * (1.f / ns_unit_p(PLANES)));
               }
             }
