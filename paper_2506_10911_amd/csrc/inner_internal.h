@@ -41,6 +41,8 @@ struct NsClass {
   uint32_t m, n;        // the short and the long side
   uint32_t mp, np;      // and what they are padded to
   uint32_t tall;        // the matrix has more rows than columns: X is its transpose
+  uint32_t splits;      // parts of the long side that X X^T is summed in, each by workgroups of its own
+  uint32_t pad;
 };
 
 // In device memory: as kernel arguments these 2 KB cost every launch 0.8 us (toy matrices, 17 launches 112 / 99 us).
@@ -54,12 +56,13 @@ struct NsArgs {
   const NsItem* items;
   char* workspace;
   double* sums;                 // [item][kNsChunks]
+  uint32_t splits;              // the most of the launch's classes
   NsClass first;                // the table's first class, which is often the only one: its workgroups read no table
   uint32_t first_end;
 };
 
 // What an item's buffers hold, in bytes from their start: X and the next X [mp][np], A and P [mp][mp], each number
-// one binary16 or a pair of them ("planes").
+// one binary16 or a pair of them ("planes").  While X X^T is summed in parts, these lie where the next X comes.
 inline uint64_t ns_x_bytes(uint32_t mp, uint32_t np, int planes) { return uint64_t(mp) * np * 2 * planes; }
 inline uint64_t ns_item_bytes(uint32_t mp, uint32_t np, int planes) { return 2 * (ns_x_bytes(mp, np, planes) + ns_x_bytes(mp, mp, planes)); }
 
@@ -75,6 +78,7 @@ inline uint64_t ns_small_bytes(uint32_t m, uint32_t n, int planes) {
   const uint64_t shares = mp <= 64 ? 8 * 1024 * sizeof(float) : 0;
   return kNsSmallSums + mp * (np * 2 * planes + 16) + 2 * mp * (mp * 2 * planes + 16) + shares;
 }
+constexpr int kNsSplitTile = 64, kNsSplitBytes = kNsSplitTile * kNsSplitTile * 4;      // a part of a tile of X X^T
 struct NsSteps {
   int32_t count;
   float k[3 * NOLOCO_MAX_NEWTON_SCHULZ_STEPS];

@@ -43,6 +43,7 @@ struct Shape {
   int tile;
   uint32_t first_item, items;
   bool alone[2];            // goes through all steps in one workgroup (one binary16 a number, pairs)
+  uint32_t parts[2];        // that X X^T is summed in, with one binary16 a number and with pairs
   uint32_t m() const { return std::min(rows, cols); }
   uint32_t n() const { return std::max(rows, cols); }
   uint32_t mp() const { return padded(m(), tile); }
@@ -62,6 +63,7 @@ struct Batch {
   uint32_t first_table;
   uint32_t groups[kTables];
   uint32_t lds;             // of a workgroup of small matrices
+  uint32_t splits;          // the most of the classes
   NsClass first[kTables];   // of the tables
   uint32_t first_end[kTables];
 };
@@ -84,6 +86,12 @@ bool pads_well(int64_t m, int64_t n) {
   return m >= kRows256 && big <= 1.1 * less && noloco::ns_x_bytes(padded(m, 256), padded(n, 256), 2) >> 32 == 0;
 }
 
+// X X^T of few rows is few tiles of long sums: where there are less tiles than twice the CUs the long side is shared out, as
+// long as each share has kShare stages (64 numbers, or 32 pairs) and the shares' sums have room where the next X comes.  Adding
+// them up is a launch more: five steps of float matrices with 33 stages (ragged, up to 1031) 164 us, shared out 184; with 125
+// (eight of 64 x 4000) 193 / 121; with 512 (130 x 16384) 546 / 166; 16384 x 1 in bf16 507 / 116.
+constexpr int64_t kSplitGroups = 512, kSplitStages = 48, kShare = 8, kMostSplits = 64;
+
 void choose_tiles(std::vector<Shape>* shapes) {
   int64_t big = 0, all = 0;
   for (const Shape& s : *shapes) {
@@ -105,6 +113,17 @@ void choose_tiles(std::vector<Shape>* shapes) {
       else tiles += int64_t(s.items) * (s.mp() / s.tile) * (s.np() / s.tile);
     }
     for (Shape& s : *shapes) s.alone[planes - 1] = s.fits_lds(planes) && !(others && tiles <= kJoined);
+    int64_t grams = 0;
+    for (const Shape& s : *shapes)
+      if (!s.alone[planes - 1]) grams += s.items * lower_tiles(s.m(), s.tile);
+    for (Shape& s : *shapes) {
+      s.parts[planes - 1] = 1;
+      if (s.alone[planes - 1] || s.tile != noloco::kNsSplitTile) continue;
+      const int64_t stages = (s.n() + 64 / planes - 1) / (64 / planes);
+      if (stages < kSplitStages) continue;
+      const int64_t room = noloco::ns_x_bytes(s.mp(), s.np(), planes) / (lower_tiles(s.m(), s.tile) * noloco::kNsSplitBytes);
+      s.parts[planes - 1] = static_cast<uint32_t>(std::max<int64_t>(1, std::min({kSplitGroups / grams, stages / kShare, room, kMostSplits})));
+    }
   }
 }
 
@@ -220,6 +239,8 @@ uint32_t make_batches(std::vector<Shape> shapes, int planes, uint64_t room, std:
       c.mp = s.mp();
       c.np = s.np();
       c.tall = s.rows > s.cols ? 1 : 0;
+      c.splits = s.parts[planes - 1];
+      b.splits = std::max(b.splits, c.splits);
       for (int k = 0; k < (small ? 1 : kTables); ++k) {
         c.per_item = per[k];
         b.groups[k] += per[k] * static_cast<uint32_t>(fit);
@@ -377,7 +398,7 @@ noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, 
   steps.count = method->steps;
   std::copy(method->coefficients, method->coefficients + 3 * method->steps, steps.k);
   for (const Batch& b : plan->batches[planes - 1]) {
-    auto args = [&](int table) { return NsArgs{plan->tables + b.first_table + table, plan->items, plan->workspace, plan->sums, b.first[table], b.first_end[table]}; };
+    auto args = [&](int table) { return NsArgs{plan->tables + b.first_table + table, plan->items, plan->workspace, plan->sums, b.splits, b.first[table], b.first_end[table]}; };
     if (b.tile == 0) {
       if (noloco::launch_ns_small(args(kSums), arrays, steps, planes, b.groups[kSums], b.lds, stream) != 0) return NOLOCO_ERR_DEVICE;
       continue;

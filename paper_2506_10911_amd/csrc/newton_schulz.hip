@@ -50,13 +50,13 @@ __device__ __forceinline__ void load_to_lds(uint4v buffer, uint32_t lane_offset,
 // Enqueue a kernel and return the launch status itself.
 template <typename T> struct same { typedef T type; };
 template <typename... KArgs>
-int enqueue_with(uint32_t lds, void (*kernel)(KArgs...), uint32_t grid, uint32_t block, void* stream, typename same<KArgs>::type... args) {
+int enqueue_with(uint32_t lds, void (*kernel)(KArgs...), dim3 grid, uint32_t block, void* stream, typename same<KArgs>::type... args) {
   void* argv[] = {static_cast<void*>(&args)...};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(grid), dim3(block), argv, lds, static_cast<hipStream_t>(stream));
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(block), argv, lds, static_cast<hipStream_t>(stream));
 }
 template <typename... KArgs>
 int enqueue(void (*kernel)(KArgs...), uint32_t grid, uint32_t block, void* stream, typename same<KArgs>::type... args) {
-  return enqueue_with(0, kernel, grid, block, stream, args...);
+  return enqueue_with(0, kernel, dim3(grid), block, stream, args...);
 }
 
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
@@ -87,7 +87,7 @@ __device__ __forceinline__ Place locate(const NsArgs& args, uint32_t group) {
       begin = past ? end : begin;
     }
     const scalar_memory NsClass* c = table->cls + cls;
-    p.cls = {c->base, c->item_bytes, c->per_item, c->first_item, c->first_sum, c->m, c->n, c->mp, c->np, c->tall};
+    p.cls = {c->base, c->item_bytes, c->per_item, c->first_item, c->first_sum, c->m, c->n, c->mp, c->np, c->tall, c->splits, 0};
   }
   const uint32_t at = group - begin;
   p.item = at / p.cls.per_item;
@@ -818,7 +818,7 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t block
 // (shorter rows: q ^ (k >> 1 & 1) << 2), since four lanes of a group of 16 read each of four rows.
 template <int T, int WR, int WC, int KIND, int PLANES, typename Out>
 __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays arrays, int32_t step, float ca, float cb, float cc, uint32_t run) {
-  constexpr bool kApplies = KIND == kNsApply || KIND == kNsLast;
+  constexpr bool kApplies = KIND == kNsApply || KIND == kNsLast, kSplits = KIND == kNsGram && T == kNsSplitTile;
   constexpr int kWaves = WR * WC, kThreads = kWaves * 64;
   constexpr int kDepth = 64 / PLANES;                       // k of a stage
   constexpr int kSlices = kDepth / 16;
@@ -877,15 +877,20 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   const uint32_t first_bytes = static_cast<uint32_t>(KIND == kNsSquare ? a_bytes : x_bytes);
   const uint32_t second_bytes = static_cast<uint32_t>(KIND == kNsGram ? x_bytes : a_bytes);
   const uint4v first_buffer = buffer_words(first, first_bytes), second_buffer = buffer_words(second, second_bytes);
-  const uint32_t stages = ((KIND == kNsGram ? cls.n : cls.m) + kDepth - 1) / kDepth;
+  uint32_t stages = ((KIND == kNsGram ? cls.n : cls.m) + kDepth - 1) / kDepth, first_stage = 0;
+  if constexpr (kSplits) {
+    if (blockIdx.y >= cls.splits) return;
+    first_stage = static_cast<uint32_t>(uint64_t(stages) * blockIdx.y / cls.splits);
+    stages = static_cast<uint32_t>(uint64_t(stages) * (blockIdx.y + 1) / cls.splits) - first_stage;
+  }
 
   // Where a lane's 16 bytes of a load come from.
   uint32_t plain_first[2], plain_second[2], turned[4];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const uint32_t chunk = (lane & 7) ^ (((i << 2) | (lane >> 4)) & 7);
-    plain_first[i] = (lane >> 3) * first_ld + chunk * 16;
-    plain_second[i] = (lane >> 3) * second_ld + chunk * 16;
+    plain_first[i] = (lane >> 3) * first_ld + chunk * 16 + first_stage * 128;
+    plain_second[i] = (lane >> 3) * second_ld + chunk * 16 + first_stage * 128;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -1009,6 +1014,16 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   for (; s + kStages < stages; ++s) stage(s, Yes{}, Yes{});
   for (; s + 1 < stages; ++s) stage(s, No{}, Yes{});
   stage(s, No{}, No{});
+
+  if constexpr (kSplits) {
+    if (cls.splits > 1) {       // a part, as the registers hold it
+      float4v* part = reinterpret_cast<float4v*>(x_next + (uint64_t(blockIdx.y) * cls.per_item + place.part) * kNsSplitBytes);
+#pragma unroll
+      for (int quad = 0; quad < 4; ++quad)
+        part[(wave * 4 + quad) * 64 + lane] = float4v{acc[0][0][quad * 4], acc[0][0][quad * 4 + 1], acc[0][0][quad * 4 + 2], acc[0][0][quad * 4 + 3]};
+      return;
+    }
+  }
 
   // A wave's results go through the LDS, half of the tile's columns at a time, and from there in whole lines.
   // Block (i, j), element e of a lane: r = 32 i + 8 (e / 4) + 4 fk + e % 4, c = 32 j + fr.
@@ -1155,12 +1170,60 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   }
 }
 
+// A from the parts that ns_product leaves of its tiles, in their order.  A workgroup adds a quarter of a tile: what one wave held.
+// Bound by its launch and the reads' way: 3 to 5 us, of up to 64 parts.
+template <int PLANES>
+__global__ __launch_bounds__(256) void ns_join(NsArgs args, int32_t step) {
+  const Place place = locate(args, blockIdx.x);
+  const NsClass& cls = place.cls;
+  if (cls.splits < 2) return;
+  const uint64_t x_bytes = uint64_t(cls.mp) * cls.np * 2 * PLANES;
+  char* const buffers = args.workspace + cls.base + place.item * cls.item_bytes;
+  const char* const parts = buffers + (step & 1 ? 0 : x_bytes) + uint64_t(place.part) * kNsSplitBytes;
+  char* const gram = buffers + 2 * x_bytes;
+  uint32_t row = 0;
+  while ((row + 1) * (row + 2) / 2 <= place.part) ++row;
+  const uint32_t c0 = row * kNsSplitTile, r0 = (place.part - row * (row + 1) / 2) * kNsSplitTile;
+  const uint32_t lane = threadIdx.x & 63, quad = threadIdx.x >> 6, wave = blockIdx.y;
+  const uint64_t from = ((wave * 4 + quad) * 64 + lane) * sizeof(float4v), each = uint64_t(cls.per_item) * kNsSplitBytes;
+  float4v sum = {0.f, 0.f, 0.f, 0.f};
+  constexpr uint32_t kAhead = 8;
+  uint32_t s = 0;
+  for (; s + kAhead <= cls.splits; s += kAhead) {
+    float4v v[kAhead];
+#pragma unroll
+    for (uint32_t k = 0; k < kAhead; ++k) v[k] = *reinterpret_cast<const float4v*>(parts + (s + k) * each + from);
+#pragma unroll
+    for (uint32_t k = 0; k < kAhead; ++k) sum += v[k];
+  }
+  for (; s < cls.splits; ++s) sum += *reinterpret_cast<const float4v*>(parts + s * each + from);
+  sum *= ns_unit_a(PLANES) / (ns_unit_x(PLANES) * ns_unit_x(PLANES));
+  const uint32_t r = r0 + wave / 2 * 32 + quad * 8 + (lane >> 5) * 4, c = c0 + wave % 2 * 32 + (lane & 31);
+  const uint64_t ld = uint64_t(cls.mp) * 2 * PLANES;
+  auto spot = [](uint32_t i) { return PLANES == 1 ? i * 2 : (i / 32) * 128 + (i % 32) * 2; };
+  const half4 high = __builtin_convertvector(sum, half4);
+  const half4 low = __builtin_convertvector(sum - __builtin_convertvector(high, float4v), half4);
+  *reinterpret_cast<half4*>(gram + c * ld + spot(r)) = high;
+  if constexpr (PLANES == 2) *reinterpret_cast<half4*>(gram + c * ld + spot(r) + 64) = low;
+  if (r0 != c0) {
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+      *reinterpret_cast<_Float16*>(gram + (r + k) * ld + spot(c)) = high[k];
+      if constexpr (PLANES == 2) *reinterpret_cast<_Float16*>(gram + (r + k) * ld + spot(c) + 64) = low[k];
+    }
+  }
+}
+
 template <int T, int WR, int WC, int PLANES>
 int launch_product(const NsArgs& args, const NsArrays& arrays, int kind, int step, float a, float b, float c, uint32_t run,
                    uint32_t workgroups, void* stream) {
   constexpr uint32_t kThreads = WR * WC * 64;
   switch (kind) {
-    case kNsGram: return enqueue(ns_product<T, WR, WC, kNsGram, PLANES, float>, workgroups, kThreads, stream, args, arrays, step, a, b, c, run);
+    case kNsGram: {
+      const uint32_t splits = T == kNsSplitTile ? args.splits : 1;
+      const int st = enqueue_with(0, ns_product<T, WR, WC, kNsGram, PLANES, float>, dim3(workgroups, splits), kThreads, stream, args, arrays, step, a, b, c, run);
+      return st != 0 || splits < 2 ? st : enqueue_with(0, ns_join<PLANES>, dim3(workgroups, 4), 256, stream, args, step);
+    }
     case kNsSquare: return enqueue(ns_product<T, WR, WC, kNsSquare, PLANES, float>, workgroups, kThreads, stream, args, arrays, step, a, b, c, run);
     case kNsApply: return enqueue(ns_product<T, WR, WC, kNsApply, PLANES, float>, workgroups, kThreads, stream, args, arrays, step, a, b, c, run);
     default:
@@ -1175,7 +1238,7 @@ int launch_ns_small(const NsArgs& args, const NsArrays& arrays, const NsSteps& s
                     uint32_t lds_bytes, void* stream) {
   auto pick = [&](auto momentum, auto bf16, auto out) {
     typedef decltype(out) Out;
-    return enqueue_with(lds_bytes, planes == 1 ? ns_small<1, bf16, momentum, Out> : ns_small<2, bf16, momentum, Out>, workgroups,
+    return enqueue_with(lds_bytes, planes == 1 ? ns_small<1, bf16, momentum, Out> : ns_small<2, bf16, momentum, Out>, dim3(workgroups),
                         kNsSmallThreads, stream, args, arrays, steps);
   };
   auto with_out = [&](auto momentum, auto bf16) {

@@ -108,6 +108,8 @@ static int check_plan(const std::vector<noloco_matrix>& matrices, int64_t stride
         const uint32_t mt = c.mp / launch.tile, nt = c.np / launch.tile;
         CHECK(c.mp % launch.tile == 0 && c.np % launch.tile == 0);
         CHECK(c.per_item == (launch.kind >= kNsApply ? mt * nt : mt * (mt + 1) / 2));
+        CHECK(c.splits >= 1 && c.splits <= launch.args.splits && c.splits * uint64_t(64 / planes) <= c.n + 64 / planes);
+        CHECK(c.splits == 1 || (launch.tile == kNsSplitTile && c.splits * (uint64_t(mt) * (mt + 1) / 2) * kNsSplitBytes <= ns_x_bytes(c.mp, c.np, planes)));
       }
       if (launch.what == 1) CHECK(c.per_item == c.mp / 64 * (c.np / 64));
       if (launch.what == 0 || launch.what == 3) {

@@ -149,6 +149,22 @@ def test_small_matrices(shapes, products, out):
     assert same_bits(got[nl.PRODUCTS_AUTO], got[nl.PRODUCTS_PAIRS])
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("shapes", [[(1, 9001)], [(5000, 3)], [(70, 3201)], [(3500, 130, 137)], [(129, 3077)], [(40, 4100), (1500, 90), (200, 300)]],
+                         ids=lambda s: "+".join("x".join(map(str, v)) for v in s))
+def test_few_long_rows(shapes, out):
+    matrices, stride = layout(shapes)
+    x = filled(matrices, 2, stride, torch.float32, seed=12)
+    plan = nl.MuonPlan(matrices, stride, 2)
+    for kind, products in ((nl.PRODUCTS_F16, "f16"), (nl.PRODUCTS_PAIRS, "pairs")):
+        got = [torch.full((2, stride), 3.0, dtype=DTYPES[out], device="cuda") for _ in range(2)]
+        for g in got:
+            nl.orthogonalize(plan, x.cuda(), nl.F32, g, code(DTYPES[out]), products=kind)
+        check(matrices, got[0].cpu(), x, products)
+        assert same_bits(*got)
+        assert (got[0].cpu()[~owned(matrices, 2, stride)] == 3.0).all()
+
+
 def test_one_large_matrix_takes_bf16_results_to_one_number():
     matrices, stride = layout([(16, 64), (128, 128)])
     x = filled(matrices, 1, stride, torch.bfloat16, seed=10)
