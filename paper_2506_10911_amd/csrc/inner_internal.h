@@ -62,9 +62,13 @@ struct NsArgs {
 };
 
 // What an item's buffers hold, in bytes from their start: X and the next X [mp][np], A and P [mp][mp], each number
-// one binary16 or a pair of them ("planes").  While X X^T is summed in parts, these lie where the next X comes.
+// one binary16 or a pair of them ("planes"), and behind single ones what they leave of A's diagonal and of P's, binary32 [mp]
+// each.  While X X^T is summed in parts, these lie where the next X comes.
 inline uint64_t ns_x_bytes(uint32_t mp, uint32_t np, int planes) { return uint64_t(mp) * np * 2 * planes; }
-inline uint64_t ns_item_bytes(uint32_t mp, uint32_t np, int planes) { return 2 * (ns_x_bytes(mp, np, planes) + ns_x_bytes(mp, mp, planes)); }
+inline uint64_t ns_rest_bytes(uint32_t mp, int planes) { return planes == 1 ? uint64_t(mp) * 4 : 0; }
+inline uint64_t ns_item_bytes(uint32_t mp, uint32_t np, int planes) {
+  return 2 * (ns_x_bytes(mp, np, planes) + ns_x_bytes(mp, mp, planes) + ns_rest_bytes(mp, planes));
+}
 
 // A matrix whose X, A and P fit a CU's LDS goes through all steps in one workgroup: rows padded to 32, 16 bytes behind
 // each of them.

@@ -10,6 +10,11 @@
 // results (a few 2^-12 of the result's norm); for float results a number is a pair of binary16, high and low half, of
 // which three products are taken (high high, high low, low high): 22 bits.
 //
+// With one binary16 a number the diagonals of A and P keep what it leaves of them, and the next product adds it: where n is much
+// more than m all singular values are alike and A is nearly its diagonal, so that its rounding is a relative error of every
+// singular value, and some steps' polynomials have slopes of ten there (without it 32 x 512 is 0.003 of the norm off and
+// 4 x 1024 0.006, with it 0.0007; square ones 0.0012 and 0.0009).
+//
 // A and P are symmetric: only tiles on and below the diagonal are computed, each written to both its places.
 // X stays row-major throughout: X X^T reads rows along their length, and P X reads X through the LDS's
 // transposing reads, so that no transposed copy of X is ever stored.
@@ -154,10 +159,6 @@ template <typename Out> __device__ __forceinline__ void put_result(const NsArray
 // so that 16 rows of a fragment begin in 16 different quarters of the banks.  Blocks of 32 x 32: those of A and P on and
 // below the diagonal are dealt to the waves (of A with one or three blocks several waves share one's k); of P X a wave
 // takes 32 columns of X, which nobody else reads, holds them in registers and writes their next values in their place.
-//
-// With one binary16 a number the diagonals of A and P keep what it leaves of them, and P X adds it: where n is much more
-// than m all of A's diagonal is nearly the same number, its rounding the same relative error of every singular value, and
-// some steps' polynomials have slopes of ten there (32 x 512: 0.003 of the norm off without, 0.0007 with).
 //
 // Numbers come and go in chunks of eight, a thread every 512th chunk: eight along X's row, 16 bytes of the LDS.  (Results of
 // a tall matrix leave as four columns of two rows, since half a wave would write 128 bytes of a row only.)  They are read
@@ -835,7 +836,9 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   constexpr int kFloatRow = (T + 4) * 4, kFloatTallRow = (kHalf + 4) * 4;
   constexpr int kFloats = kHalf * kFloatRow > T * kFloatTallRow ? kHalf * kFloatRow : T * kFloatTallRow;
   constexpr int kResult = KIND == kNsLast ? kFloats : kImage;
-  constexpr int kLds = kStages * kStage > kResult ? kStages * kStage : kResult;
+  constexpr bool kRests = PLANES == 1 && KIND != kNsGram;   // what is left of a diagonal is read
+  constexpr int kRestAt = kStages * kStage > kResult ? kStages * kStage : (kResult + 1023) / 1024 * 1024;
+  constexpr int kLds = kRestAt + (kRests ? (kApplies ? 1 : 2) * 1024 : 0);
   static_assert(kTurned <= 1024 && kLoads >= 1 && kLds <= 160 * 1024 && (kStages & (kStages - 1)) == 0, "tile");
   __shared__ __align__(1024) char lds[kLds];
 
@@ -848,6 +851,8 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   char* const x_next = buffers + (step & 1 ? 0 : x_bytes);
   char* const gram = buffers + 2 * x_bytes;
   char* const poly = gram + a_bytes;
+  float* const gram_rest = reinterpret_cast<float*>(poly + a_bytes);
+  float* const poly_rest = gram_rest + mp;
 
   // Tile (r0, c0) of the result, and where it is found in the operands.
   uint32_t r0, c0;
@@ -978,6 +983,12 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
       for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.r[0][i], f.c[0][j], acc[i][j], 0, 0, 0);
   };
 
+  // What is left of the diagonal, of the tile's columns and, for A^2, its rows: in front of all else, so that it has come with it.
+  if constexpr (kRests) {
+    const float* const rests = kApplies ? poly_rest : gram_rest;
+    if (wave == 0) load_to_lds(buffer_words(rests + c0, T * 4), lane * 16, 0, lds_at + kRestAt);
+    if (!kApplies && wave == 1) load_to_lds(buffer_words(rests + r0, T * 4), lane * 16, 0, lds_at + kRestAt + 1024);
+  }
   if (stages >= kStages) {
 #pragma unroll
     for (int i = 0; i < kStages; ++i) ask(i);
@@ -989,8 +1000,29 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   __builtin_amdgcn_s_barrier();
   Fragments even, odd;
   read(0, 0, even);
+  // P with its diagonal's rests R is P X + R X: R, whose numbers binary16 has room for, goes through the products as a block of
+  // its own where the stages hold the rows of X that are the tile's columns, 64 of them each.  (From memory, at the end, R X made P X
+  // of 2048 x 8192 11 % longer, this 2.5.)
+  constexpr bool kDiagonal = kRests && kApplies;
+  const uint32_t diagonal = c0 / kDepth, diagonal_end = diagonal + T / kDepth;
+  _Float16 left[NB];
+  if constexpr (kDiagonal) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) left[j] = static_cast<_Float16>(*reinterpret_cast<const float*>(lds + kRestAt + (wc * (T / WC) + j * 32 + fr) * 4));
+  }
+  auto multiply_rests = [&](const Fragments& f, uint32_t piece, int slice) {
+    static_assert(!kDiagonal || T / WC == 64 || (T == 64 && T / WC == 32), "a wave's columns are a stage's, or half of one's");
+    if (T / WC == 64 ? piece != wc : static_cast<uint32_t>(slice >> 1) != wc) return;
+    const int j = T / WC == 64 ? slice >> 1 : 0;
+    const uint32_t mine = fr - (slice & 1) * 16 - fk * 8;        // where the lane's row has its column's number, if it has
+    half8 d;
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) d[e] = e == mine ? left[j] : static_cast<_Float16>(0.f);
+#pragma unroll
+    for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.r[0][i], d, acc[i][j], 0, 0, 0);
+  };
   // The stages behind the last one that is asked for by themselves, so that nothing in the loop is conditional.
-  auto stage = [&](uint32_t s, auto ask_more, auto read_next) {
+  auto stage = [&](uint32_t s, auto ask_more, auto read_next, auto with_rests) {
 #pragma unroll
     for (int slice = 0; slice < kSlices; ++slice) {
       Fragments& now = slice & 1 ? odd : even;
@@ -1006,14 +1038,20 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
         if constexpr (ask_more) ask(s + kStages);
       }
       multiply(now);
+      if constexpr (kDiagonal && with_rests)
+        if (s >= diagonal && s < diagonal_end) multiply_rests(now, s - diagonal, slice);
       // the products of a slice stay behind its reads, which the compiler would put in front of the next barrier
       if constexpr (T == 256 && PLANES == 1) __builtin_amdgcn_sched_barrier(0);
     }
   };
   uint32_t s = 0;
-  for (; s + kStages < stages; ++s) stage(s, Yes{}, Yes{});
-  for (; s + 1 < stages; ++s) stage(s, No{}, Yes{});
-  stage(s, No{}, No{});
+  if constexpr (kDiagonal) {
+    for (; s + kStages < stages && s < diagonal; ++s) stage(s, Yes{}, Yes{}, No{});
+    for (; s + kStages < stages && s < diagonal_end; ++s) stage(s, Yes{}, Yes{}, Yes{});
+  }
+  for (; s + kStages < stages; ++s) stage(s, Yes{}, Yes{}, No{});
+  for (; s + 1 < stages; ++s) stage(s, No{}, Yes{}, Yes{});
+  stage(s, No{}, No{}, Yes{});
 
   if constexpr (kSplits) {
     if (cls.splits > 1) {       // a part, as the registers hold it
@@ -1028,31 +1066,91 @@ __global__ __launch_bounds__(WR * WC * 64) void ns_product(NsArgs args, NsArrays
   // A wave's results go through the LDS, half of the tile's columns at a time, and from there in whole lines.
   // Block (i, j), element e of a lane: r = 32 i + 8 (e / 4) + 4 fk + e % 4, c = 32 j + fr.
   const uint32_t r_of = wr * (T / WR) + 4 * fk, c_of = (wc % (WC / 2)) * (T / WC) + fr;
+  const uint32_t c_first = c0 + wc * (T / WC) + fr;
   if constexpr (KIND != kNsLast) {
     char* const to = KIND == kNsGram ? gram : (KIND == kNsSquare ? poly : x_next);
     const uint64_t to_ld = uint64_t(KIND == kNsApply ? np : mp) * 2 * PLANES;
     if constexpr (KIND == kNsSquare) {
       const float constant = ca * ns_unit_p(PLANES), linear = cb * (ns_unit_p(PLANES) / ns_unit_a(PLANES));
       const float square = cc * (ns_unit_p(PLANES) / (ns_unit_a(PLANES) * ns_unit_a(PLANES)));
+      if constexpr (PLANES == 1) {
+        // A's tile comes to the LDS, where nobody reads stages any more: rows of its transpose, which is itself, 16-byte chunk q of
+        // row c at q ^ c.  With its diagonal's rests R it is A + R, and its square A^2 + A R + R A.
+        constexpr int kRow = T * 2, kRows = 1024 / kRow;
+        static_assert(T * kRow <= kStages * kStage, "tile of A");
 #pragma unroll
-      for (int i = 0; i < MB; ++i)
+        for (int i = 0; i < T / kRows / kWaves; ++i) {
+          const uint32_t load = wave * (T / kRows / kWaves) + i, row = lane * 16 / kRow;
+          const uint32_t chunk = (lane * 16 % kRow / 16) ^ ((load * kRows + row) & (kRow / 16 - 1));
+          load_to_lds(first_buffer, row * first_ld + chunk * 16, (c0 + load * kRows) * first_ld + r0 * 2, lds_at + load * 1024);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        const float* const of_columns = reinterpret_cast<const float*>(lds + kRestAt);
+        float of_column[NB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
+        for (int j = 0; j < NB; ++j) of_column[j] = of_columns[wc * (T / WC) + j * 32 + fr];
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
-            const uint32_t r = r0 + r_of + i * 32 + e * 2, c = c0 + wc * (T / WC) + fr + j * 32;
-            // A is symmetric: its columns are read as rows, whose neighbouring numbers neighbouring lanes take
+            const uint32_t r = r_of + i * 32 + e * 2;
+            const float4v of_row = *reinterpret_cast<const float4v*>(of_columns + 256 + r);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const char* from = gram + (r + k) * to_ld + (PLANES == 1 ? c * 2 : (c / 32) * 128 + (c % 32) * 2);
-              float v = static_cast<float>(*reinterpret_cast<const _Float16*>(from));
-              if constexpr (PLANES == 2) v += static_cast<float>(*reinterpret_cast<const _Float16*>(from + 64));
-              acc[i][j][e + k] = square * acc[i][j][e + k] + linear * v + (r + k == c ? constant : 0.f);
+            for (int j = 0; j < NB; ++j) {
+              const uint32_t c = wc * (T / WC) + j * 32 + fr;
+              const float4v a = __builtin_convertvector(*reinterpret_cast<const half4*>(lds + c * kRow + (((r >> 3) ^ (c & (kRow / 16 - 1))) << 4) + fk * 8), float4v);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float v = acc[i][j][e + k] + a[k] * (of_row[k] + of_column[j]);
+                acc[i][j][e + k] = square * v + linear * a[k];
+              }
             }
           }
+      } else {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const uint32_t r = r0 + r_of + i * 32 + e * 2, c = c_first + j * 32;
+              // A is symmetric: its columns are read as rows, whose neighbouring numbers neighbouring lanes take
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const char* from = gram + (r + k) * to_ld + (c / 32) * 128 + (c % 32) * 2;
+                float v = static_cast<float>(*reinterpret_cast<const _Float16*>(from));
+                v += static_cast<float>(*reinterpret_cast<const _Float16*>(from + 64));
+                acc[i][j][e + k] = square * acc[i][j][e + k] + linear * v + (r + k == c ? constant : 0.f);
+              }
+            }
+      }
     }
     constexpr float kUnit = KIND == kNsGram ? ns_unit_a(PLANES) / (ns_unit_x(PLANES) * ns_unit_x(PLANES))
                                             : (KIND == kNsSquare ? 1.f : 1.f / ns_unit_p(PLANES));
+    if constexpr (!kApplies && PLANES == 1) {
+      // The diagonal: of a block on it, the lanes whose row is among their four hold one number each. A^2's is not whole yet, and
+      // of both goes what a binary16 leaves to memory.
+      if (r0 == c0) {
+        const int mine = (fr >> 2 & 1) == fk ? static_cast<int>((fr >> 3) * 4 + (fr & 3)) : -1;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) {
+            if (wr * (T / WR) + i * 32 != wc * (T / WC) + j * 32) continue;
+            const uint32_t c = wc * (T / WC) + j * 32 + fr;
+            float more = 0.f, v = 0.f;
+            if constexpr (KIND == kNsSquare)
+              more = ca * ns_unit_p(PLANES) + cb * (ns_unit_p(PLANES) / ns_unit_a(PLANES)) * *reinterpret_cast<const float*>(lds + kRestAt + c * 4);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              if constexpr (KIND == kNsSquare) acc[i][j][e] += e == mine ? more : 0.f;
+              v = e == mine ? acc[i][j][e] * kUnit : v;
+            }
+            if (mine >= 0) (KIND == kNsGram ? gram_rest : poly_rest)[c0 + c] = v - static_cast<float>(static_cast<_Float16>(v));
+          }
+      }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       __syncthreads();
@@ -1202,7 +1300,14 @@ __global__ __launch_bounds__(256) void ns_join(NsArgs args, int32_t step) {
   const uint64_t ld = uint64_t(cls.mp) * 2 * PLANES;
   auto spot = [](uint32_t i) { return PLANES == 1 ? i * 2 : (i / 32) * 128 + (i % 32) * 2; };
   const half4 high = __builtin_convertvector(sum, half4);
-  const half4 low = __builtin_convertvector(sum - __builtin_convertvector(high, float4v), half4);
+  const float4v left = sum - __builtin_convertvector(high, float4v);
+  const half4 low = __builtin_convertvector(left, half4);
+  if constexpr (PLANES == 1) {
+    float* const rests = reinterpret_cast<float*>(gram + 2 * ld * cls.mp);
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k)
+      if (r + k == c) rests[c] = left[k];
+  }
   *reinterpret_cast<half4*>(gram + c * ld + spot(r)) = high;
   if constexpr (PLANES == 2) *reinterpret_cast<half4*>(gram + c * ld + spot(r) + 64) = low;
   if (r0 != c0) {
