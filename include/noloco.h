@@ -375,6 +375,7 @@ noloco_status noloco_muon_plan_info(const noloco_muon_plan* plan, int64_t* eleme
  * Enqueued on hip_stream, not synchronised; allocates and copies nothing, so it may be captured into a HIP graph.
  * The plan owns the workspace: calls sharing one plan must not overlap in time.  Results are bit-identical
  * from run to run.  Every argument is checked before the first launch; after NOLOCO_ERR_DEVICE the output is undefined.
+ * The current device must be the plan's (NOLOCO_ERR_INVALID_ARG), as in all calls with a plan below.
  */
 noloco_status noloco_orthogonalize(const noloco_muon_plan* plan, const void* x, int32_t x_dtype, void* out,
                                    int32_t out_dtype, const noloco_newton_schulz* method, void* hip_stream);

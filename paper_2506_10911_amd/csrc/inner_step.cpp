@@ -37,6 +37,13 @@ uint64_t bytes_of(int32_t dtype) { return dtype == NOLOCO_BF16 ? 2 : 4; }
 
 uint32_t padded(int64_t v, int tile) { return static_cast<uint32_t>((v + tile - 1) / tile * tile); }
 
+// A plan's tables and workspace are in the memory of the GPU that was current when it was made.
+noloco_status check_device(int of_plan) {
+  int device = -1;
+  if (hipGetDevice(&device) != hipSuccess) return NOLOCO_ERR_DEVICE;
+  return device == of_plan ? NOLOCO_OK : NOLOCO_ERR_INVALID_ARG;
+}
+
 // Matrices of one shape.
 struct Shape {
   uint32_t rows, cols;      // as stored
@@ -394,6 +401,9 @@ noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, 
   // binary16).
   const bool one = method->products == NOLOCO_PRODUCTS_F16 || (method->products == NOLOCO_PRODUCTS_AUTO && arrays.out_bf16 && !plan->pairs);
   const int planes = one ? 1 : 2;
+  if (plan->batches[planes - 1].empty()) return NOLOCO_OK;
+  const noloco_status st = check_device(plan->device);
+  if (st != NOLOCO_OK) return st;
   noloco::NsSteps steps{};
   steps.count = method->steps;
   std::copy(method->coefficients, method->coefficients + 3 * method->steps, steps.k);
@@ -599,6 +609,8 @@ extern "C" noloco_status noloco_embed_lookup(const noloco_embedding_plan* plan, 
   const noloco_status st = embed_args(plan, table, table_dtype, out, out_dtype, tokens, token_type, num_tokens, scale, &args);
   if (st != NOLOCO_OK) return st;
   if (num_tokens == 0) return NOLOCO_OK;
+  const noloco_status there = check_device(plan->device);
+  if (there != NOLOCO_OK) return there;
   return noloco::launch_embed_lookup(args, hip_stream) == 0 ? NOLOCO_OK : NOLOCO_ERR_DEVICE;
 }
 
@@ -611,5 +623,7 @@ extern "C" noloco_status noloco_embed_gradient(const noloco_embedding_plan* plan
   if (st != NOLOCO_OK) return st;
   args.accumulate = accumulate;
   if (num_tokens == 0 && accumulate) return NOLOCO_OK;
+  const noloco_status there = check_device(plan->device);
+  if (there != NOLOCO_OK) return there;
   return noloco::launch_embed_gradient(args, hip_stream) == 0 ? NOLOCO_OK : NOLOCO_ERR_DEVICE;
 }

@@ -1,0 +1,80 @@
+// Host-only checks of inner_step.cpp (built and run by tests/test_inner_plans.py): the kernel launchers are stand-ins that
+// record what would be launched, device memory is host memory, the current device is whatever a check makes it.
+#include <hip/hip_runtime_api.h>
+
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <vector>
+
+#include "inner_internal.h"
+
+static int current_device = 0;
+extern "C" hipError_t hipGetDevice(int* device) { *device = current_device; return hipSuccess; }
+extern "C" hipError_t hipMalloc(void** ptr, size_t size) {
+  *ptr = std::malloc(size < (64u << 20) ? size : (64u << 20));      // what lies behind the tables only kernels touch
+  return hipSuccess;
+}
+extern "C" hipError_t hipFree(void* ptr) { std::free(ptr); return hipSuccess; }
+extern "C" hipError_t hipMemcpy(void* dst, const void* src, size_t size, hipMemcpyKind) { std::memcpy(dst, src, size); return hipSuccess; }
+
+namespace noloco {
+static int launched = 0;
+int launch_ns_sums(const NsArgs&, const NsArrays&, uint32_t, void*) { ++launched; return 0; }
+int launch_ns_start(const NsArgs&, const NsArrays&, int, uint32_t, void*) { ++launched; return 0; }
+int launch_ns_product(const NsArgs&, const NsArrays&, int, int, int, int, float, float, float, uint32_t, void*) { ++launched; return 0; }
+int launch_ns_small(const NsArgs&, const NsArrays&, const NsSteps&, int, uint32_t, uint32_t, void*) { ++launched; return 0; }
+int launch_embed_lookup(const EmbedArgs&, void*) { ++launched; return 0; }
+int launch_embed_gradient(const EmbedArgs&, void*) { ++launched; return 0; }
+}  // namespace noloco
+
+#define CHECK(cond) do { if (!(cond)) { std::printf("CHECK failed at line %d: %s\n", __LINE__, #cond); return 1; } } while (0)
+
+using namespace noloco;
+
+static const float kSteps[6] = {1.5f, -.5f, 0.f, 1.5f, -.5f, 0.f};
+static char* memory(size_t at) {
+  static char here[1 << 16] __attribute__((aligned(256)));
+  return here + at;
+}
+
+// A call on another GPU than its plan's would use that GPU's memory there.
+static int check_devices() {
+  const noloco_matrix matrix = {0, 4, 4, 4, 1.f};
+  const noloco_newton_schulz method = {2, kSteps, 0.f, NOLOCO_PRODUCTS_AUTO};
+  const noloco_muon_hparams hparams = {.1f, .9f, 0.f, 1};
+  noloco_muon_plan *plan = nullptr, *none = nullptr;
+  noloco_embedding_plan* table = nullptr;
+  current_device = 1;
+  CHECK(noloco_muon_plan_create(&matrix, 1, 64, 1, 0, &plan) == NOLOCO_OK);
+  CHECK(noloco_muon_plan_create(nullptr, 0, 64, 1, 0, &none) == NOLOCO_OK);
+  CHECK(noloco_embedding_plan_create(0, 4, 4, 64, 1, 8, &table) == NOLOCO_OK);
+  char *a = memory(0), *b = memory(4096), *c = memory(8192);
+  float* const momentum = reinterpret_cast<float*>(c);
+  for (int device : {1, 0, 1}) {
+    current_device = device;
+    launched = 0;
+    const noloco_status want = device == 1 ? NOLOCO_OK : NOLOCO_ERR_INVALID_ARG;
+    CHECK(noloco_orthogonalize(plan, a, NOLOCO_F32, b, NOLOCO_F32, &method, nullptr) == want);
+    CHECK(noloco_muon_step(plan, a, NOLOCO_F32, b, NOLOCO_F32, momentum, &hparams, &method, nullptr) == want);
+    CHECK(noloco_embed_lookup(table, a, NOLOCO_F32, b, NOLOCO_I32, 8, 1.f, c, NOLOCO_F32, nullptr) == want);
+    CHECK(noloco_embed_gradient(table, a, NOLOCO_F32, b, NOLOCO_I32, 8, 1.f, c, NOLOCO_F32, 0, nullptr) == want);
+    CHECK((launched > 0) == (device == 1));
+    // what launches nothing does not ask for the device
+    CHECK(noloco_orthogonalize(none, a, NOLOCO_F32, b, NOLOCO_F32, &method, nullptr) == NOLOCO_OK);
+    CHECK(noloco_embed_lookup(table, a, NOLOCO_F32, nullptr, NOLOCO_I32, 0, 1.f, nullptr, NOLOCO_F32, nullptr) == NOLOCO_OK);
+  }
+  CHECK(noloco_muon_plan_destroy(plan) == NOLOCO_OK && noloco_muon_plan_destroy(none) == NOLOCO_OK);
+  CHECK(noloco_embedding_plan_destroy(table) == NOLOCO_OK);
+  return 0;
+}
+
+int main(int argc, char** argv) {
+  const char* const what = argc > 1 ? argv[1] : "";
+  int failed = 1;
+  if (std::strcmp(what, "devices") == 0) failed = check_devices();
+  else std::printf("what to check?\n");
+  if (failed == 0) std::printf("ok\n");
+  return failed;
+}
