@@ -93,7 +93,8 @@ __global__ __launch_bounds__(256) void embed_lookup(EmbedArgs a) {
   const int64_t all = static_cast<int64_t>(a.W) * a.num_tokens;
   const uint32_t lane = threadIdx.x & 63;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t first = (static_cast<int64_t>(blockIdx.x) * 4 + wave) * kTokens;
+  static_assert(kLookupTokens == 4 * kTokens, "tokens of a workgroup");
+  const int64_t first = ((static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 4 + wave) * kTokens;
   if (first >= all) return;
   const uint32_t mine = first + lane < all && lane < kTokens ? token_at(a, first + lane) : a.vocab;
   const Table* from[kTokens];
@@ -441,8 +442,8 @@ __global__ __launch_bounds__(256) void embed_join(EmbedArgs a, const uint32_t* t
 }
 
 template <typename Table, typename Row, int N> int lookup(const EmbedArgs& a, void* stream) {
-  const int64_t all = static_cast<int64_t>(a.W) * a.num_tokens;
-  return enqueue(embed_lookup<Table, Row, N>, dim3(static_cast<uint32_t>((all + 15) / 16)), 256, 0, stream, a);
+  const LookupGrid grid = lookup_grid(static_cast<int64_t>(a.W) * a.num_tokens);
+  return enqueue(embed_lookup<Table, Row, N>, dim3(grid.x, grid.y), 256, 0, stream, a);
 }
 
 template <typename Table, typename Row, int N> int gradient(const EmbedArgs& a, void* stream) {

@@ -121,6 +121,14 @@ constexpr int kMergeWays = 16;          // sorted lists that one merge joins
 constexpr int kMergeChunk = kSortChunk * kMergeWays;      // tokens that the first one holds in the LDS
 constexpr int kSumChunk = 32;           // sorted positions that a workgroup sums
 
+// The lookup's workgroups: 256 threads, sixteen tokens each, all of which may be more than 2^32 threads in one dimension.
+constexpr int64_t kLookupTokens = 16;
+struct LookupGrid { uint32_t x, y; };
+inline LookupGrid lookup_grid(int64_t all) {
+  const int64_t groups = (all + kLookupTokens - 1) / kLookupTokens, rows = (groups + (1 << 23) - 1) >> 23;
+  return {static_cast<uint32_t>((groups + rows - 1) / rows), static_cast<uint32_t>(rows)};
+}
+
 struct EmbedArgs {
   void* table;            // first element of worker 0's table (or of its gradient)
   void* rows;             // out, or dout: [W][tokens][width]

@@ -70,10 +70,26 @@ static int check_devices() {
   return 0;
 }
 
+// Every number of tokens that a plan takes is a grid that HIP takes: less than 2^32 threads and at most 65536 workgroups in a
+// dimension.
+static int check_lookup_grid() {
+  for (int bit = 0; bit < 31; ++bit)
+    for (int64_t all : {(1ll << bit) - 1, 1ll << bit, (1ll << bit) + 1, (1ll << bit) + 12345, (2ll << bit) - 1}) {
+      if (all < 1 || all > 0x7fffffff) continue;
+      const LookupGrid grid = lookup_grid(all);
+      const uint64_t tokens = uint64_t(grid.x) * grid.y * kLookupTokens;
+      CHECK(uint64_t(grid.x) * 256 < 1ull << 32 && grid.x >= 1 && grid.y >= 1 && grid.y <= 65536);
+      CHECK(tokens >= uint64_t(all) && tokens - all < grid.y * uint64_t(kLookupTokens));
+      CHECK(all > 1 << 27 || grid.y == 1);
+    }
+  return 0;
+}
+
 int main(int argc, char** argv) {
   const char* const what = argc > 1 ? argv[1] : "";
   int failed = 1;
   if (std::strcmp(what, "devices") == 0) failed = check_devices();
+  else if (std::strcmp(what, "lookup_grid") == 0) failed = check_lookup_grid();
   else std::printf("what to check?\n");
   if (failed == 0) std::printf("ok\n");
   return failed;

@@ -25,3 +25,7 @@ def driver(tmp_path_factory):
 
 def test_calls_on_another_device_are_refused(driver):
     driver("devices")
+
+
+def test_lookup_of_any_number_of_tokens_is_a_grid_that_hip_takes(driver):
+    driver("lookup_grid")
