@@ -85,11 +85,27 @@ static int check_lookup_grid() {
   return 0;
 }
 
+// Arrays of nothing share no memory, wherever they begin.
+static int check_empty_arrays() {
+  noloco_embedding_plan* table = nullptr;
+  CHECK(noloco_embedding_plan_create(0, 4, 4, 64, 1, 8, &table) == NOLOCO_OK);
+  char* const a = memory(0);
+  CHECK(noloco_embed_lookup(table, a, NOLOCO_F32, a + 32, NOLOCO_I32, 0, 1.f, a + 64, NOLOCO_F32, nullptr) == NOLOCO_OK);
+  CHECK(noloco_embed_gradient(table, a + 64, NOLOCO_F32, a + 64, NOLOCO_I32, 0, 1.f, a, NOLOCO_F32, 1, nullptr) == NOLOCO_OK);
+  launched = 0;
+  CHECK(noloco_embed_gradient(table, a + 64, NOLOCO_F32, a + 64, NOLOCO_I32, 0, 1.f, a, NOLOCO_F32, 0, nullptr) == NOLOCO_OK && launched == 1);
+  CHECK(noloco_embed_lookup(table, a, NOLOCO_F32, a + 32, NOLOCO_I32, 1, 1.f, memory(4096), NOLOCO_F32, nullptr) == NOLOCO_ERR_INVALID_ARG);
+  CHECK(noloco_embed_lookup(table, a, NOLOCO_F32, memory(4096), NOLOCO_I32, 1, 1.f, a + 64, NOLOCO_F32, nullptr) == NOLOCO_ERR_INVALID_ARG);
+  CHECK(noloco_embedding_plan_destroy(table) == NOLOCO_OK);
+  return 0;
+}
+
 int main(int argc, char** argv) {
   const char* const what = argc > 1 ? argv[1] : "";
   int failed = 1;
   if (std::strcmp(what, "devices") == 0) failed = check_devices();
   else if (std::strcmp(what, "lookup_grid") == 0) failed = check_lookup_grid();
+  else if (std::strcmp(what, "empty_arrays") == 0) failed = check_empty_arrays();
   else std::printf("what to check?\n");
   if (failed == 0) std::printf("ok\n");
   return failed;

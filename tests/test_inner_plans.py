@@ -29,3 +29,7 @@ def test_calls_on_another_device_are_refused(driver):
 
 def test_lookup_of_any_number_of_tokens_is_a_grid_that_hip_takes(driver):
     driver("lookup_grid")
+
+
+def test_arrays_of_nothing_overlap_nothing(driver):
+    driver("empty_arrays")
