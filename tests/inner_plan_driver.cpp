@@ -2,6 +2,7 @@
 // record what would be launched, device memory is host memory, the current device is whatever a check makes it.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
@@ -21,10 +22,27 @@ extern "C" hipError_t hipMemcpy(void* dst, const void* src, size_t size, hipMemc
 
 namespace noloco {
 static int launched = 0;
+static bool say = false;          // print what is launched: the last step's products, tile by tile, and small matrices
+static void told(int tile, const NsArgs& args) {
+  uint32_t last = 0;
+  for (int i = 0; say && i < kNsClasses && args.table->end[i] != 0xffffffffu; ++i) {
+    const NsClass& c = args.table->cls[i];
+    std::printf("%d %u %u %u %u\n", tile, c.tall ? c.n : c.m, c.tall ? c.m : c.n, (args.table->end[i] - last) / c.per_item, c.splits);
+    last = args.table->end[i];
+  }
+}
 int launch_ns_sums(const NsArgs&, const NsArrays&, uint32_t, void*) { ++launched; return 0; }
 int launch_ns_start(const NsArgs&, const NsArrays&, int, uint32_t, void*) { ++launched; return 0; }
-int launch_ns_product(const NsArgs&, const NsArrays&, int, int, int, int, float, float, float, uint32_t, void*) { ++launched; return 0; }
-int launch_ns_small(const NsArgs&, const NsArrays&, const NsSteps&, int, uint32_t, uint32_t, void*) { ++launched; return 0; }
+int launch_ns_product(const NsArgs& args, const NsArrays&, int kind, int tile, int, int, float, float, float, uint32_t, void*) {
+  ++launched;
+  if (kind == kNsLast) told(tile, args);
+  return 0;
+}
+int launch_ns_small(const NsArgs& args, const NsArrays&, const NsSteps&, int, uint32_t, uint32_t, void*) {
+  ++launched;
+  told(0, args);
+  return 0;
+}
 int launch_embed_lookup(const EmbedArgs&, void*) { ++launched; return 0; }
 int launch_embed_gradient(const EmbedArgs&, void*) { ++launched; return 0; }
 }  // namespace noloco
@@ -100,12 +118,41 @@ static int check_empty_arrays() {
   return 0;
 }
 
+// Reads W, the products to take and matrices (offset, rows, cols, row_stride) from standard input, and prints for every shape of
+// matrices the tile they are planned for (0: in one workgroup), their rows and columns, how many there are, and
+// the parts of X X^T; then how many launches an orthogonalisation of two steps takes.
+static int print_plan() {
+  int W = 0, products = 0, count = 0;
+  CHECK(std::scanf("%d %d %d", &W, &products, &count) == 3);
+  std::vector<noloco_matrix> matrices(count);
+  int64_t end = 0;
+  for (noloco_matrix& m : matrices) {
+    long long v[4];
+    CHECK(std::scanf("%lld %lld %lld %lld", v, v + 1, v + 2, v + 3) == 4);
+    m = {v[0], v[1], v[2], v[3], 1.f};
+    end = std::max<int64_t>(end, v[0] + (v[1] - 1) * v[3] + v[2]);
+  }
+  const int64_t stride = (end + 63) / 64 * 64;
+  noloco_muon_plan* plan = nullptr;
+  CHECK(noloco_muon_plan_create(matrices.data(), count, stride, W, 0, &plan) == NOLOCO_OK);
+  const noloco_newton_schulz method = {2, kSteps, 0.f, products};
+  char* const x = memory(0);
+  char* const y = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(x) + uint64_t(W) * stride * 8 + 4096) / 256 * 256);
+  say = true;
+  launched = 0;
+  CHECK(noloco_orthogonalize(plan, x, NOLOCO_F32, y, NOLOCO_BF16, &method, nullptr) == NOLOCO_OK);
+  std::printf("launches %d\n", launched);
+  CHECK(noloco_muon_plan_destroy(plan) == NOLOCO_OK);
+  return 0;
+}
+
 int main(int argc, char** argv) {
   const char* const what = argc > 1 ? argv[1] : "";
   int failed = 1;
   if (std::strcmp(what, "devices") == 0) failed = check_devices();
   else if (std::strcmp(what, "lookup_grid") == 0) failed = check_lookup_grid();
   else if (std::strcmp(what, "empty_arrays") == 0) failed = check_empty_arrays();
+  else if (std::strcmp(what, "plan") == 0) failed = print_plan();
   else std::printf("what to check?\n");
   if (failed == 0) std::printf("ok\n");
   return failed;

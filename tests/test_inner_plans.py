@@ -4,6 +4,8 @@ import subprocess
 
 import pytest
 
+import paper_2506_10911_amd as nl
+import test_gpu_muon_general as general
 from conftest import ROOT
 
 
@@ -33,3 +35,29 @@ def test_lookup_of_any_number_of_tokens_is_a_grid_that_hip_takes(driver):
 
 def test_arrays_of_nothing_overlap_nothing(driver):
     driver("empty_arrays")
+
+
+def planned(driver, matrices, W, products):
+    """({(rows, cols): (tile, how many, parts of X X^T)}, launches of two steps) of a plan; tile 0: in one workgroup."""
+    text = f"{W} {products} {len(matrices)}\n" + "\n".join(" ".join(map(str, m[:4])) for m in matrices)
+    shapes, launches = {}, 0
+    for line in driver("plan", text=text).splitlines():
+        words = line.split()
+        if words[0] == "launches":
+            launches = int(words[1])
+        elif len(words) == 5:
+            tile, rows, cols, count, parts = map(int, words)
+            before = shapes.get((rows, cols), (tile, 0, parts))
+            assert before[0] == tile and before[2] == parts
+            shapes[rows, cols] = (tile, before[1] + count, parts)
+    return shapes, launches
+
+
+@pytest.mark.parametrize("products", [nl.PRODUCTS_F16, nl.PRODUCTS_PAIRS])
+@pytest.mark.parametrize("path", sorted(general.PATHS))
+def test_gpu_tests_of_the_general_path_reach_its_tiles(driver, path, products):
+    """A rule that moves a threshold may not leave a kernel without its test."""
+    matrices, _, W, tile, shared = general.path(path)
+    shapes, _ = planned(driver, matrices, W, products)
+    assert {s[0] for s in shapes.values()} == {tile}
+    assert any(s[2] > 1 for s in shapes.values()) == shared
