@@ -47,15 +47,17 @@ noloco_status check_device(int of_plan) {
 // Matrices of one shape.
 struct Shape {
   uint32_t rows, cols;      // as stored
-  int tile;
   uint32_t first_item, items;
-  bool alone[2];            // goes through all steps in one workgroup (one binary16 a number, pairs)
-  uint32_t parts[2];        // that X X^T is summed in, with one binary16 a number and with pairs
+  // with one binary16 a number, and with pairs
+  int tiles[2];
+  bool alone[2];            // goes through all steps in one workgroup
+  uint32_t parts[2];        // that X X^T is summed in
   uint32_t m() const { return std::min(rows, cols); }
   uint32_t n() const { return std::max(rows, cols); }
-  uint32_t mp() const { return padded(m(), tile); }
-  uint32_t np() const { return padded(n(), tile); }
-  uint64_t item_bytes(int planes) const { return noloco::ns_item_bytes(mp(), np(), planes); }
+  int tile(int planes) const { return tiles[planes - 1]; }
+  uint32_t mp(int planes) const { return padded(m(), tile(planes)); }
+  uint32_t np(int planes) const { return padded(n(), tile(planes)); }
+  uint64_t item_bytes(int planes) const { return noloco::ns_item_bytes(mp(planes), np(planes), planes); }
   uint64_t small_bytes(int planes) const { return noloco::ns_small_bytes(m(), n(), planes); }
   // Four rows of P are what a wave keeps of a column: 128.
   bool small(int planes) const { return alone[planes - 1]; }
@@ -79,7 +81,8 @@ struct Batch {
 // CUs: with less than two rounds of them smaller ones are ahead (eight of 2048^2 327 / 285, thirty-two 1060 / 1254), and below
 // 1024 rows too (96 of 768^2 in pairs 685 / 630; 48 of 768 x 3072 1091 / 971).  Tiles of 64 pay where there are less of 128
 // than CUs: one 1024 x 4096 39 / 70, four of 768^2 32 / 37, eight 44 / 48, sixteen (336 tiles) 72 / 74, one of 2048^2 76 / 76.
-// Tiles of X X^T are counted, of all matrices that go through launches together.
+// Tiles of X X^T are counted, of all matrices that go through launches together in the format that is asked for (256 of 128 x 256
+// in pairs: tiles of 64 249 us, of 128 221; 1152 1054 and 946).
 constexpr int64_t kTiles256 = 512, kTiles128 = 256, kRows256 = 1024, kJoined = 256;
 
 int64_t lower_tiles(int64_t m, int tile) {
@@ -87,10 +90,13 @@ int64_t lower_tiles(int64_t m, int tile) {
   return t * (t + 1) / 2;
 }
 
+// X has to be one buffer, whose offsets have 32 bits.
+bool one_buffer(int64_t m, int64_t n, int tile, int planes) { return noloco::ns_x_bytes(padded(m, tile), padded(n, tile), planes) >> 32 == 0; }
+
 // Padding to 256 may cost a tenth of the products.
-bool pads_well(int64_t m, int64_t n) {
+bool pads_well(int64_t m, int64_t n, int planes) {
   const double big = double(padded(m, 256)) * padded(m, 256) * padded(n, 256), less = double(padded(m, 128)) * padded(m, 128) * padded(n, 128);
-  return m >= kRows256 && big <= 1.1 * less && noloco::ns_x_bytes(padded(m, 256), padded(n, 256), 2) >> 32 == 0;
+  return m >= kRows256 && big <= 1.1 * less && one_buffer(m, n, 256, planes);
 }
 
 // X X^T of few rows is few tiles of long sums: where there are less tiles than twice the CUs the long side is shared out, as
@@ -99,38 +105,39 @@ bool pads_well(int64_t m, int64_t n) {
 // (eight of 64 x 4000) 193 / 121; with 512 (130 x 16384) 546 / 166; 16384 x 1 in bf16 507 / 116.
 constexpr int64_t kSplitGroups = 512, kSplitStages = 48, kShare = 8, kMostSplits = 64;
 
-void choose_tiles(std::vector<Shape>* shapes) {
+void choose_tiles(std::vector<Shape>* shapes, int planes) {
   int64_t big = 0, all = 0;
   for (const Shape& s : *shapes) {
-    if (s.fits_lds(1)) continue;
-    if (pads_well(s.m(), s.n())) big += s.items * lower_tiles(s.m(), 256);
+    if (s.fits_lds(planes)) continue;
+    if (pads_well(s.m(), s.n(), planes)) big += s.items * lower_tiles(s.m(), 256);
     all += s.items * lower_tiles(s.m(), 128);
   }
   for (Shape& s : *shapes) {
-    s.tile = all < kTiles128 ? 64 : (big >= kTiles256 && pads_well(s.m(), s.n()) ? 256 : 128);
-    if (noloco::ns_x_bytes(padded(s.m(), s.tile), padded(s.n(), s.tile), 2) >> 32 != 0) s.tile = 64;      // a buffer's offsets have 32 bits
+    int& tile = s.tiles[planes - 1];
+    tile = all < kTiles128 ? 64 : (big >= kTiles256 && pads_well(s.m(), s.n(), planes) ? 256 : 128);
+    if (!one_buffer(s.m(), s.n(), tile, planes)) tile = 64;
   }
-  // Small matrices beside others: the others' launches are there anyway, and up to kJoined tiles of P X more cost them less than
-  // a launch of their own, which lasts as long as its slowest workgroup (ragged float matrices, 32 small ones 41 us of 212).
-  for (int planes = 1; planes <= 2; ++planes) {
-    bool others = false;
-    int64_t tiles = 0;
-    for (const Shape& s : *shapes) {
-      if (!s.fits_lds(planes)) others = true;
-      else tiles += int64_t(s.items) * (s.mp() / s.tile) * (s.np() / s.tile);
-    }
-    for (Shape& s : *shapes) s.alone[planes - 1] = s.fits_lds(planes) && !(others && tiles <= kJoined);
-    int64_t grams = 0;
-    for (const Shape& s : *shapes)
-      if (!s.alone[planes - 1]) grams += s.items * lower_tiles(s.m(), s.tile);
-    for (Shape& s : *shapes) {
-      s.parts[planes - 1] = 1;
-      if (s.alone[planes - 1] || s.tile != noloco::kNsSplitTile) continue;
-      const int64_t stages = (s.n() + 64 / planes - 1) / (64 / planes);
-      if (stages < kSplitStages) continue;
-      const int64_t room = noloco::ns_x_bytes(s.mp(), s.np(), planes) / (lower_tiles(s.m(), s.tile) * noloco::kNsSplitBytes);
-      s.parts[planes - 1] = static_cast<uint32_t>(std::max<int64_t>(1, std::min({kSplitGroups / grams, stages / kShare, room, kMostSplits})));
-    }
+  // Small matrices beside others of their tile: the others' launches are there anyway, and up to kJoined tiles of P X more cost them
+  // less than a launch of their own, which lasts as long as its slowest workgroup (ragged float matrices, 32 small ones 41 us of
+  // 212).  Beside others of another tile they would need launches of their own for each product.
+  bool others[257] = {};
+  int64_t tiles = 0;
+  for (const Shape& s : *shapes) {
+    if (!s.fits_lds(planes)) others[s.tile(planes)] = true;
+    else tiles += int64_t(s.items) * (s.mp(planes) / s.tile(planes)) * (s.np(planes) / s.tile(planes));
+  }
+  int64_t grams = 0;
+  for (Shape& s : *shapes) {
+    s.alone[planes - 1] = s.fits_lds(planes) && !(others[s.tile(planes)] && tiles <= kJoined);
+    if (!s.alone[planes - 1]) grams += s.items * lower_tiles(s.m(), s.tile(planes));
+  }
+  for (Shape& s : *shapes) {
+    s.parts[planes - 1] = 1;
+    if (s.alone[planes - 1] || s.tile(planes) != noloco::kNsSplitTile) continue;
+    const int64_t stages = (s.n() + 64 / planes - 1) / (64 / planes);
+    if (stages < kSplitStages) continue;
+    const int64_t room = noloco::ns_x_bytes(s.mp(planes), s.np(planes), planes) / (lower_tiles(s.m(), s.tile(planes)) * noloco::kNsSplitBytes);
+    s.parts[planes - 1] = static_cast<uint32_t>(std::max<int64_t>(1, std::min({kSplitGroups / grams, stages / kShare, room, kMostSplits})));
   }
 }
 
@@ -203,7 +210,7 @@ uint32_t make_batches(std::vector<Shape> shapes, int planes, uint64_t room, std:
   std::stable_sort(shapes.begin(), shapes.end(), [&](const Shape& a, const Shape& b) {
     const bool as = a.small(planes), bs = b.small(planes);
     if (as != bs) return bs;
-    return as ? a.small_bytes(planes) > b.small_bytes(planes) : a.tile > b.tile;
+    return as ? a.small_bytes(planes) > b.small_bytes(planes) : a.tile(planes) > b.tile(planes);
   });
   size_t shape = 0;
   uint32_t done = 0, most = 0;      // of that shape's items; of a batch
@@ -211,7 +218,7 @@ uint32_t make_batches(std::vector<Shape> shapes, int planes, uint64_t room, std:
     const Shape& head = shapes[shape];
     const bool small = head.small(planes);
     Batch b{};
-    b.tile = small ? 0 : head.tile;
+    b.tile = small ? 0 : head.tile(planes);
     b.lds = small ? static_cast<uint32_t>(head.small_bytes(planes)) : 0;
     b.first_table = static_cast<uint32_t>(tables->size());
     NsTable table[kTables];
@@ -224,11 +231,11 @@ uint32_t make_batches(std::vector<Shape> shapes, int planes, uint64_t room, std:
     int classes = 0;
     while (shape < shapes.size() && classes < noloco::kNsClasses) {
       const Shape& s = shapes[shape];
-      if (s.small(planes) != small || (small ? sharing(s) != sharing(head) : s.tile != b.tile)) break;
+      if (s.small(planes) != small || (small ? sharing(s) != sharing(head) : s.tile(planes) != b.tile)) break;
       const uint64_t each = small ? 0 : s.item_bytes(planes), elements = uint64_t(s.rows) * s.cols;
-      const uint32_t mt = s.mp() / s.tile, nt = s.np() / s.tile;
+      const uint32_t mt = s.mp(planes) / s.tile(planes), nt = s.np(planes) / s.tile(planes);
       const uint32_t chunks = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>((elements + noloco::kNsChunkElems - 1) / noloco::kNsChunkElems, 1), noloco::kNsChunks));
-      const uint32_t per[kTables] = {small ? 1 : chunks, s.mp() / 64 * (s.np() / 64), mt * (mt + 1) / 2, mt * nt};
+      const uint32_t per[kTables] = {small ? 1 : chunks, s.mp(planes) / 64 * (s.np(planes) / 64), mt * (mt + 1) / 2, mt * nt};
       uint64_t fit = s.items - done;
       if (!small) fit = std::min<uint64_t>(fit, (room - used) / each);
       for (int k = 0; k < (small ? 1 : kTables); ++k) {
@@ -243,8 +250,8 @@ uint32_t make_batches(std::vector<Shape> shapes, int planes, uint64_t room, std:
       c.first_sum = items;
       c.m = s.m();
       c.n = s.n();
-      c.mp = s.mp();
-      c.np = s.np();
+      c.mp = s.mp(planes);
+      c.np = s.np(planes);
       c.tall = s.rows > s.cols ? 1 : 0;
       c.splits = s.parts[planes - 1];
       b.splits = std::max(b.splits, c.splits);
@@ -315,11 +322,10 @@ noloco_status create_muon_plan(const noloco_matrix* given, int32_t num, int64_t 
       ++end;
     }
     s.items = static_cast<uint32_t>(items.size()) - s.first_item;
-    s.tile = 64;
     shapes.push_back(s);
     i = end;
   }
-  choose_tiles(&shapes);
+  for (int planes = 1; planes <= 2; ++planes) choose_tiles(&shapes, planes);
   plan->pairs = std::all_of(shapes.begin(), shapes.end(), [](const Shape& s) { return s.fits_lds(2) || (s.m() <= 64 && !s.fits_lds(1)); });
 
   uint64_t all[2] = {0, 0}, largest = 0;

@@ -61,3 +61,36 @@ def test_gpu_tests_of_the_general_path_reach_its_tiles(driver, path, products):
     shapes, _ = planned(driver, matrices, W, products)
     assert {s[0] for s in shapes.values()} == {tile}
     assert any(s[2] > 1 for s in shapes.values()) == shared
+
+
+def side_by_side(*shapes):
+    """(offset, rows, cols, row_stride) of `count` matrices of each shape (count, rows, cols), one after the other."""
+    found, at = [], 0
+    for count, rows, cols in shapes:
+        for _ in range(count):
+            found.append((at, rows, cols, cols))
+            at += rows * cols
+    return found
+
+
+@pytest.mark.parametrize("products", [nl.PRODUCTS_F16, nl.PRODUCTS_PAIRS])
+def test_small_matrices_go_along_in_launches_of_their_tile_only(driver, products):
+    """Two steps: sums, start and six products of the large ones. Small ones beside tiles of 64 or 128 go along, beside tiles of 256
+    alone, where they would need eight launches of their own, they take one."""
+    for large, tile in (((2, 260, 516), 64), ((14, 768, 768), 128)):
+        shapes, launches = planned(driver, side_by_side(large, (2, 64, 64)), 1, products)
+        assert (shapes[64, 64][0], shapes[large[1:]][0], launches) == (tile, tile, 8)
+    shapes, launches = planned(driver, side_by_side((8, 4096, 4096), (2, 64, 64)), 1, products)
+    assert (shapes[64, 64][0], shapes[4096, 4096][0], launches) == (0, 256, 9)
+    # with others of 128 beside those of 256 they go along again
+    shapes, launches = planned(driver, side_by_side((8, 4096, 4096), (1, 768, 768), (2, 64, 64)), 1, products)
+    assert (shapes[64, 64][0], shapes[768, 768][0], shapes[4096, 4096][0], launches) == (128, 128, 256, 16)
+
+
+def test_tiles_are_counted_in_the_format_that_is_asked_for(driver):
+    """128 x 256 fits one workgroup in single binary16 and goes through launches in pairs, where 256 tiles of 128 and more take these."""
+    matrices = side_by_side((255, 128, 256))
+    assert planned(driver, matrices, 1, nl.PRODUCTS_PAIRS)[0][128, 256][:2] == (64, 255)
+    matrices = side_by_side((256, 128, 256))
+    assert planned(driver, matrices, 1, nl.PRODUCTS_F16)[0][128, 256][:2] == (0, 256)
+    assert planned(driver, matrices, 1, nl.PRODUCTS_PAIRS)[0][128, 256][:2] == (128, 256)
