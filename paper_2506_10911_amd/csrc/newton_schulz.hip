@@ -336,11 +336,14 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
 #pragma unroll
   for (uint32_t w = 0; w < kWaves; ++w) squares += part[w];
   const double norm = sqrt(squares) + static_cast<double>(arrays.eps);
+  float near;
   {
     // X_0 = u * ns_unit_x / norm, the factor as a number near 1 and a power of two, which float has room for whatever the norm.
-    // A matrix of zeros stays one.
+    // A matrix of zeros stays one.  Single binary16 are rounded already, and so that X_0 is not rounded twice it stays without
+    // the number near 1 (0.5 to 1), which the first step's polynomial takes in.
     int power = 0;
-    const float near = norm == 0. ? 0.f : static_cast<float>(frexp(static_cast<double>(ns_unit_x(PLANES)) / norm, &power));
+    near = norm == 0. ? 0.f : static_cast<float>(frexp(static_cast<double>(ns_unit_x(PLANES)) / norm, &power));
+    if (!(norm <= 1.7976931348623157e308)) near = __builtin_nanf("");
     const Number<0> way;           // in the LDS both ways are the same
     Walk walk = walk_of(way);
 #pragma unroll 2
@@ -351,7 +354,7 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
         const int chunk_power = power + static_cast<int>(c.there ? powers[done + thread] : 0) - 127 - 14;
         const half8 h = __builtin_bit_cast(half8, get(way, c, 0));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) high[e] = static_cast<_Float16>(ldexpf(static_cast<float>(h[e]) * near, chunk_power));
+        for (int e = 0; e < 8; ++e) high[e] = static_cast<_Float16>(ldexpf(static_cast<float>(h[e]), chunk_power));
       } else {
         const ushort8 hi = get(way, c, 0), lo = get(way, c, 1);
 #pragma unroll
@@ -493,8 +496,12 @@ __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArray
   };
 
   for (int step = 0; step < steps.count; ++step) {
-    const float constant = steps.k[3 * step] * ns_unit_p(PLANES), linear = steps.k[3 * step + 1] * (ns_unit_p(PLANES) / ns_unit_a(PLANES));
-    const float square = steps.k[3 * step + 2] * (ns_unit_p(PLANES) / (ns_unit_a(PLANES) * ns_unit_a(PLANES)));
+    // X_0 is `missing` times what the LDS holds, A its square times
+    const float missing = PLANES == 1 && step == 0 ? near : 1.f;
+    const float constant = steps.k[3 * step] * ns_unit_p(PLANES) * missing;
+    const float linear = steps.k[3 * step + 1] * (ns_unit_p(PLANES) / ns_unit_a(PLANES)) * (missing * missing * missing);
+    const float square = steps.k[3 * step + 2] * (ns_unit_p(PLANES) / (ns_unit_a(PLANES) * ns_unit_a(PLANES))) *
+                         (missing * missing * missing * missing * missing);
     symmetric(x, x_row, np / 16, gram, blocks <= 2, [&](uint32_t, uint32_t, uint32_t, float4v d) { return d * kUnitGram; });
     symmetric(gram, a_row, mp / 16, poly, false, [&](uint32_t bi, uint32_t bj, uint32_t quad, float4v d) {
       const uint32_t row = bj * 32 + quad * 8 + half * 4, col = bi * 32 + of32;

@@ -290,3 +290,62 @@ def test_graph_of_an_update(name):
         torch.cuda.synchronize()
         nl.muon_step(plan, e_theta, nl.F32, x, nl.F32, e_moved, (0.1, 0.9, 0.1))
         assert same_bits(theta.cpu(), e_theta.cpu()) and same_bits(moved.cpu(), e_moved.cpu())
+
+
+def test_small_matrices_round_their_first_x_once():
+    """One step of 2 x^5, whose slope is five times itself: X_0 is off by one rounding, 2^-11, and X and the result's store by
+    another. The number and the row's length are such that two roundings of X_0 go the same way (to 0.0019 together)."""
+    n, w = 989, 1.0004663467407227
+    signs = torch.randint(0, 2, (1, n), generator=torch.Generator().manual_seed(81)) * 2.0 - 1.0
+    x = torch.zeros((1, 1024))
+    x[:, :n] = signs * w
+    plan = nl.MuonPlan([(0, 1, n), (1023, 1, 1)], 1024, 1)
+    got = torch.zeros((1, 1024), device="cuda")
+    nl.orthogonalize(plan, x.cuda(), nl.F32, got, nl.F32, coefficients=((0.0, 0.0, 2.0),), eps=0.0, products=nl.PRODUCTS_F16)
+    want = 2.0 * signs.double() / n ** 0.5
+    off = (got[:, :n].cpu().double() / want - 1.0).abs().max().item()
+    assert off <= 6 * 2.0 ** -11 * 1.01, f"{off:.5f}"
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-7])
+def test_bad_numbers_of_small_matrices_in_binary16(eps):
+    matrices, stride = layout([(70, 70), (9, 200), (200, 9), (64, 64)], gap=4)
+    x = filled(matrices, 3, stride, torch.float32, seed=82).cuda()
+    plan = nl.MuonPlan(matrices, stride, 3)
+
+    def run(into):
+        out = torch.zeros((3, stride), device="cuda")
+        nl.orthogonalize(plan, into, nl.F32, out, nl.F32, eps=eps, products=nl.PRODUCTS_F16)
+        return out
+
+    clean, bad = run(x), x.clone()
+    plain.view(bad, *matrices[0][:4])[1].zero_()
+    plain.view(bad, *matrices[1][:4])[0, 8, 199] = float("inf")
+    plain.view(bad, *matrices[2][:4])[1, 0, 0] = float("-inf")
+    plain.view(bad, *matrices[3][:4])[2, 63, 3] = float("nan")
+    bad_rows = plain.view(bad, *matrices[3][:4])[0]
+    bad_rows.zero_()
+    bad_rows[5, 7] = float("inf")                        # everything else is zero
+    got = run(bad)
+    for k, m in enumerate(matrices):
+        for w in range(3):
+            part = plain.view(got, *m[:4])[w]
+            if (k, w) == (0, 1):
+                assert (part == 0).all()
+            elif (k, w) in ((1, 0), (2, 1), (3, 2), (3, 0)):
+                assert part.isnan().all()
+            else:
+                assert same_bits(part, plain.view(clean, *m[:4])[w])
+    assert same_bits(run(x), clean)
+
+
+def test_sizes_of_numbers_do_not_matter_to_small_matrices_in_binary16():
+    matrices, stride = layout([(30, 70), (64, 600)])
+    x = filled(matrices, 1, stride, torch.float32, seed=83)
+    plan = nl.MuonPlan(matrices, stride, 1)
+    for factor in (1.0, 2.0 ** -100, 2.0 ** 100):
+        got = torch.zeros((1, stride), device="cuda")
+        nl.orthogonalize(plan, (x * factor).cuda(), nl.F32, got, nl.F32, eps=0.0, products=nl.PRODUCTS_F16)
+        for m in matrices:
+            exact, bound = plain.newton_schulz_bound(plain.view(x, *m[:4])[0].double(), "f16", torch.float32, eps=0.0)
+            assert (plain.view(got.cpu(), *m[:4])[0].double() - exact).norm().item() <= bound
