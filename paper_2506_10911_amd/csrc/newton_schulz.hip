@@ -39,7 +39,8 @@ typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 // 16 bytes a lane from a buffer to the LDS, at `to` + 16 times the lane, past the registers.  The compiler does not count
 // these loads (it would wait for all of them in front of every transposing read): who reads what they bring waits for
-// vmcnt itself.
+// vmcnt itself.  m0 is a register that the compiler keeps nothing in and that a clobber list may not name; its own
+// instructions that read it, each behind a write of its own, are none in these kernels.
 __device__ __forceinline__ uint4v buffer_words(const void* p, uint32_t bytes) {
   const uint64_t at = reinterpret_cast<uint64_t>(p);
   auto same = [](uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v))); };

@@ -1,5 +1,6 @@
 """Host code of the inner step's operators against stand-ins for the HIP runtime and the kernel launchers."""
 import os
+import re
 import subprocess
 
 import pytest
@@ -94,3 +95,27 @@ def test_tiles_are_counted_in_the_format_that_is_asked_for(driver):
     matrices = side_by_side((256, 128, 256))
     assert planned(driver, matrices, 1, nl.PRODUCTS_F16)[0][128, 256][:2] == (0, 256)
     assert planned(driver, matrices, 1, nl.PRODUCTS_PAIRS)[0][128, 256][:2] == (128, 256)
+
+
+def test_only_the_loads_to_the_lds_use_m0(tmp_path):
+    """They write it in inline assembly, which cannot say so: m0 is reserved. So nothing else may count on what it holds."""
+    with open(nl.library_path(), "rb") as f:
+        data = f.read()
+    kernels, at = 0, data.find(b"\x7fELF", 4)
+    while at >= 0:
+        if int.from_bytes(data[at + 18:at + 20], "little") == 224:                  # AMDGPU
+            table, entry, count = (int.from_bytes(data[at + a:at + b], "little") for a, b in ((40, 48), (58, 60), (60, 62)))
+            image = tmp_path / "gfx950.elf"
+            image.write_bytes(data[at:at + table + entry * count])
+            objdump = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "llvm-objdump")
+            text = subprocess.run([objdump, "-d", "--no-show-raw-insn", str(image)], check=True, capture_output=True, text=True).stdout
+            for body in re.findall(r"<[^>]*ns_product[^>]*>:\n(.*?)\n\n", text + "\n\n", re.S):
+                lines = [line.split("//")[0].strip() for line in body.splitlines()]
+                kernels += 1
+                for i, line in enumerate(lines):
+                    if re.search(r"\bm0\b", line):
+                        assert re.match(r"s_mov_b32 m0, s\d+$", line) and lines[i + 1] == "s_nop 0" and lines[i + 2].endswith("offen lds")
+                    elif line.endswith(" lds"):
+                        assert lines[i - 2].startswith("s_mov_b32 m0")
+        at = data.find(b"\x7fELF", at + 4)
+    assert kernels == 3 * 2 * 5                                                     # tiles, formats, kinds (the last with two results)
