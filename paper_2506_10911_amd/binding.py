@@ -289,7 +289,8 @@ def replica_spread_noalloc(plan: LaunchPlan, x, x_dtype: int, out_std, stream=No
 
 class MuonPlan:
     """noloco_muon_plan_create / _destroy / _info: the matrices of every worker's row, each (offset, rows, cols) or
-    (offset, rows, cols, row_stride) or (offset, rows, cols, row_stride, scale)."""
+    (offset, rows, cols, row_stride) or (offset, rows, cols, row_stride, scale). info() counts batches with single binary16
+    (bf16_batches) and with pairs (f32_batches)."""
 
     def __init__(self, matrices, worker_stride: int, W: int, workspace_bytes: int = 0):
         self._handle, self._address = C.c_void_p(0), 0

@@ -16,9 +16,6 @@
 namespace noloco {
 namespace {
 
-typedef float float4v __attribute__((ext_vector_type(4)));
-typedef uint16_t ushort4v __attribute__((ext_vector_type(4)));
-
 template <typename T> struct same { typedef T type; };
 template <typename... KArgs>
 int enqueue(void (*kernel)(KArgs...), dim3 grid, uint32_t block, uint32_t lds, void* stream, typename same<KArgs>::type... args) {

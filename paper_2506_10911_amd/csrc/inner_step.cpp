@@ -400,11 +400,11 @@ noloco_status check_method(const noloco_newton_schulz* method) {
 }
 
 noloco_status run_batches(const noloco_muon_plan* plan, const NsArrays& arrays, const noloco_newton_schulz* method, void* stream) {
-  // One binary16 a number leaves an error below a bf16 result's own rounding (0.0007 to 0.0016 of the norm, the rounding 0.0017),
-  // the more the less numbers average it.  The smallest matrices, whose step waits more than it computes, take pairs (us, binary16
-  // and pairs: eight of 16 x 64 15.9 / 15.7, 32 of 64 x 64 18.2 / 21.6) and have the rounding alone.  So have long ones of few
-  // rows that go through launches: their singular values are so alike that one rounding is in all of them (4 x 6000: 0.0067 in
-  // binary16).
+  // One binary16 a number leaves an error below a bf16 result's own rounding (0.0005 to 0.0011 of the norm, the rounding 0.0017),
+  // the more the fewer numbers average it and the smaller the least singular value is (4 x 4 and 8 x 8 of noise 0.0014, one in a
+  // hundred 0.006).  Small matrices, whose step waits more than it computes, take pairs (us, binary16 and pairs: eight of 16 x 64
+  // 16.4 / 15.6, 32 of 64 x 64 19.0 / 21.7) and have the rounding alone.  So have long ones of few rows that go through launches
+  // (4 x 6000 beside nothing larger 94 / 113, eight of 64 x 4000 95 / 119, errors 0.0017 either way).
   const bool one = method->products == NOLOCO_PRODUCTS_F16 || (method->products == NOLOCO_PRODUCTS_AUTO && arrays.out_bf16 && !plan->pairs);
   const int planes = one ? 1 : 2;
   if (plan->batches[planes - 1].empty()) return NOLOCO_OK;

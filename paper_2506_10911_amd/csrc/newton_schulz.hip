@@ -32,7 +32,6 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef float float4v __attribute__((ext_vector_type(4)));
-typedef uint16_t ushort4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 #define lds_memory __attribute__((address_space(3)))
@@ -168,8 +167,9 @@ template <typename Out> __device__ __forceinline__ void put_result(const NsArray
 //
 // What bounds it: each workgroup waits for its own chain.  1152 matrices of 64 x 768 in binary16, float in and bf16 out, take
 // 257 us (1.3 TB/s): four and a half rounds, in each of which all CUs load at once (14 us), then compute (six to seven us a
-// step), then write.  Two steps of loads and products side by side would need two matrices' LDS; asking for the next matrix
-// before the steps needs registers that are not there.  With launches for each product instead: 637 us.  24 matrices of
+// step), then write.  The matrix cores are busy 10 % of the cycles, the LDS 32 %.  A second workgroup a CU has no room while X
+// is in the LDS; asking for the next matrix before the steps needs registers that are not there.  (X in registers, 48 a lane at
+// 64 x 768, would leave room for two: not built.)  With launches for each product instead: 637 us.  24 matrices of
 // 64 x 64 to 64 x 256 in pairs: 34 us, with launches 99.
 template <int PLANES, bool BF16, bool MOMENTUM, typename Out>
 __global__ __launch_bounds__(kNsSmallThreads) void ns_small(NsArgs args, NsArrays arrays, NsSteps steps) {
@@ -814,13 +814,14 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t block
 // of the products that use them, across the stage's end too: the barrier in front of the last slice's products tells that
 // the next stage has come and that this one's buffer is free.
 //
-// What bounds it: a stage of 64 KiB takes 1.55 us of a CU when all CUs are at it, 1.0 of them its products at the clock
-// that the power leaves (1.8 of 2.4 GHz); stages of half the depth, four to five of them, were 2 to 10 % slower, so it is the
-// loads' rate and not their way that the rest is spent on.  P X of 4096 x 16384: 1170 to 1340 TFLOP/s by the card (a large library
-// product 1220 to 1480), X X^T 900 to 950 of those it computes.  In pairs (768 x 768 to 768 x 3072, tiles of 128) 900 and 930,
-// three products a number counted.  A symmetric product ends with both its images, from registers the one and through
-// the LDS the other (tiles of 256: gram 6 us of a workgroup's 60, square 13), the last P X with the update of theta in the same
-// way (19 us, of theta's reads mostly).
+// What bounds it: in tiles of 256 the clock, which falls to 1.63 to 1.75 of 2.4 GHz under these products, and the stages' way to
+// the LDS: the matrix cores are busy 68 % of that clock's cycles in P X of 4096 x 4096 to 4096 x 16384, 60 % at 2048, 48 to 54 %
+// in the symmetric products.  (Stages of half the depth, four to five of them, were 2 to 10 % slower.)  P X at 4096 1165
+// TFLOP/s, at 2048 1043, X X^T 916 and 838, A^2 923 and 794, symmetric ones counted by half; a large library product 1220 to
+// 1480.  In pairs (768 x 768 to 768 x 3072, tiles of 128) 905, 808 and 627, three products a number counted, with the matrix cores
+// busy 53, 56 and 40 % at 1.66 to 1.8 GHz: two stages of 32 KiB bring too little work for each of their waits.  A symmetric
+// product ends with both its images, from registers the one and through the LDS the other, the last P X with the update of theta
+// in the same way (2048 wide, bf16: 2205 us beside 1581 of the other P X).
 //
 // Rows of 128 bytes: 16-byte chunk q of row r lies at q ^ (r >> 1 & 7), so that the 16 lanes that read at once meet
 // 16 different quarters of the 64 banks.  Rows of X in the transposed operand: chunk q of row k at q ^ (k & 3) << 2
