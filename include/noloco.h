@@ -447,6 +447,171 @@ noloco_status noloco_embed_gradient(const noloco_embedding_plan* plan, const voi
                                     int32_t grad_dtype, int32_t accumulate, void* hip_stream);
 
 /*
+ * Layer norm, matrices and loss of the inner step: what a replica runs through between the table's lookup and its gradient.
+ * Weights are read from the W stacked rows (theta) and their gradients go to the same places of an array of the same
+ * layout (grad); activations are [W][num_tokens][width], one worker's behind the other's without gaps.  A plan lists all layers
+ * of its kind that the rows have; a call names one by its number in that list.
+ *   theta, grad   device, [W][worker_stride] float or bf16, NOLOCO_BASE_ALIGN_BYTES-aligned; of grad only the layer's
+ *                 elements are written
+ *   activations   device, float or bf16, 16-byte-aligned
+ *   num_tokens    0 <= num_tokens <= max_tokens
+ *   accumulate    0: gradients of weights are written, 1: added to what is there
+ * Arithmetic is binary32, results are rounded once to their type.  Arrays that a call writes must not overlap any other one
+ * of the call (NOLOCO_ERR_INVALID_ARG), but for those that an entry point names.  Calls are enqueued on hip_stream, not
+ * synchronised, allocate and copy nothing and may be captured into a HIP graph.  A plan owns its workspace: calls that share
+ * one must not overlap in time, replays of graphs among them.  Results are bit-identical from run to run.  The current
+ * device must be the plan's (NOLOCO_ERR_INVALID_ARG).  Every argument is checked before the first launch.
+ */
+
+/* One layer norm of every worker's row: `width` weights from element `weight` of the row on, as many biases from `bias` on;
+ * bias -1: none. */
+typedef struct noloco_norm {
+  int64_t weight;
+  int64_t bias;
+  int64_t width;
+} noloco_norm;
+
+/*
+ * Plan for the layer norms of an arena's rows, with the workspace of noloco_layer_norm_gradient (one hipMalloc: sums of the
+ * weights' gradients, 8 bytes for each element of the widest norm and up to 1024 groups of tokens, W workers).
+ * Errors: NOLOCO_ERR_SEGMENT_OVERLAP (weight and bias of a norm share an element, or one leaves the row),
+ * NOLOCO_ERR_INVALID_ARG, NOLOCO_ERR_ALIGNMENT, NOLOCO_ERR_UNSUPPORTED (width above 2^20, max_tokens above 2^27,
+ * W * max_tokens above 2^31 - 1), NOLOCO_ERR_DEVICE.  On error *out is null.
+ */
+typedef struct noloco_layer_norm_plan noloco_layer_norm_plan;
+noloco_status noloco_layer_norm_plan_create(const noloco_norm* norms, int32_t num_norms, int64_t worker_stride, int32_t W,
+                                            int64_t max_tokens, noloco_layer_norm_plan** out);
+noloco_status noloco_layer_norm_plan_destroy(noloco_layer_norm_plan* plan);
+
+/*
+ * out[w][t] = (x[w][t] - mean) * rstd * weight_w + bias_w, with mean the row's, rstd = 1 / sqrt(variance + eps), and the
+ * variance the mean of the squared distances from the mean.
+ *   eps     >= 0
+ *   stats   device, out, float[W][num_tokens][2], 16-byte-aligned: mean and rstd, which the gradient takes; may be null
+ * A NaN or an infinity in a row of x makes that row NaN, and no other.
+ */
+noloco_status noloco_layer_norm(const noloco_layer_norm_plan* plan, int32_t norm, const void* x, int32_t x_dtype,
+                                const void* theta, int32_t theta_dtype, int64_t num_tokens, float eps, void* out,
+                                int32_t out_dtype, float* stats, void* hip_stream);
+
+/*
+ * With xh = (x - mean) * rstd and g = dout * weight:
+ *   dx     = add + rstd * (g - mean(g) - xh * mean(g * xh))
+ *   weight's gradient = sum over the worker's tokens of dout * xh,  bias's = sum of dout
+ *   stats  what noloco_layer_norm left for x
+ *   add    of dx's type, [W][num_tokens][width], may be null (nothing is added) and may be dx itself
+ *   grad   may be null: no gradients of weights
+ * Sums over tokens are taken in an order that depends on the sizes alone.
+ */
+noloco_status noloco_layer_norm_gradient(const noloco_layer_norm_plan* plan, int32_t norm, const void* dout, int32_t dout_dtype,
+                                         const void* x, int32_t x_dtype, const void* theta, int32_t theta_dtype,
+                                         const float* stats, int64_t num_tokens, const void* add, void* dx, int32_t dx_dtype,
+                                         void* grad, int32_t grad_dtype, int32_t accumulate, void* hip_stream);
+
+/* One matrix of every worker's row with its bias: element (i, o) of M, input i and output o, is `offset + i * row_stride + o`
+ * elements into the row, or `offset + o * row_stride + i` if it is transposed (as an embedding table is, used as output
+ * head).  `outputs` biases from element `bias` on; -1: none. */
+typedef struct noloco_linear_layer {
+  int64_t offset;
+  int64_t inputs, outputs;
+  int64_t row_stride;      /* >= outputs, or >= inputs if transposed */
+  int64_t bias;
+  int32_t transposed;      /* 0 or 1 */
+} noloco_linear_layer;
+
+/* What noloco_linear applies to z: z; max(z, 0); z Phi(z) with the normal distribution Phi; the same by
+ * (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 for Phi; z / (1 + exp(-z)). */
+typedef enum noloco_activation {
+  NOLOCO_ACT_NONE = 0, NOLOCO_ACT_RELU = 1, NOLOCO_ACT_GELU = 2, NOLOCO_ACT_GELU_TANH = 3, NOLOCO_ACT_SILU = 4
+} noloco_activation;
+
+/*
+ * Plan for the matrices of an arena's rows, with a workspace (one hipMalloc) for gradients before the activation and for
+ * sums that are taken in parts.  A gradient goes through the workers in batches that fit it.
+ *   workspace_bytes  most bytes for the workspace; 0: 4 GiB.  Never more than all workers need at once, and never less than
+ *                    one worker needs by itself (4 bytes for each of the largest layer's max_tokens x outputs, and less)
+ * Errors: NOLOCO_ERR_SEGMENT_OVERLAP (a matrix and its own bias share an element, or one leaves the row),
+ * NOLOCO_ERR_INVALID_ARG, NOLOCO_ERR_ALIGNMENT, NOLOCO_ERR_UNSUPPORTED (a side above 2^22; max_tokens above 2^24; matrix,
+ * x or out of one worker of more than 2^30 numbers, row_stride counted), NOLOCO_ERR_DEVICE.  On error *out is null.
+ */
+typedef struct noloco_linear_plan noloco_linear_plan;
+noloco_status noloco_linear_plan_create(const noloco_linear_layer* layers, int32_t num_layers, int64_t worker_stride,
+                                        int32_t W, int64_t max_tokens, int64_t workspace_bytes, noloco_linear_plan** out);
+noloco_status noloco_linear_plan_destroy(noloco_linear_plan* plan);
+
+/*
+ * z = x M + bias;  out = act(z) + residual
+ *   residual   of out's type, [W][num_tokens][outputs], may be null (nothing is added) and may be out itself
+ *   before     of out's type, [W][num_tokens][outputs]: z, which the gradient takes; may be null
+ * How products take their operands goes by the result: for a bf16 result float operands are rounded to bf16; for a float
+ * result they keep their 24 bits (three bf16 each, and the products of these that binary32 can tell).  Sums are binary32.
+ * A NaN or an infinity in x or M makes NaN or infinite what depends on it.
+ */
+noloco_status noloco_linear(const noloco_linear_plan* plan, int32_t layer, const void* x, int32_t x_dtype, const void* theta,
+                            int32_t theta_dtype, int64_t num_tokens, int32_t activation, const void* residual, void* before,
+                            void* out, int32_t out_dtype, void* hip_stream);
+
+/*
+ * dz = dout * act'(before);  dx = add + dz M^T;  M's gradient = x^T dz, bias's = sum of dz over the worker's tokens
+ *   before     of dout's type, [W][num_tokens][outputs]: what noloco_linear left; may be null for NOLOCO_ACT_NONE
+ *   add        of dx's type, [W][num_tokens][inputs], may be null (nothing is added) and may be dx itself
+ *   dx, grad   either may be null: not computed.  x may be null where grad is
+ * Products take their operands by the result's type as above; dz is rounded to bf16 only where a bf16 result takes it.
+ */
+noloco_status noloco_linear_gradient(const noloco_linear_plan* plan, int32_t layer, const void* dout, int32_t dout_dtype,
+                                     const void* x, int32_t x_dtype, const void* theta, int32_t theta_dtype, int64_t num_tokens,
+                                     int32_t activation, const void* before, const void* add, void* dx, int32_t dx_dtype,
+                                     void* grad, int32_t grad_dtype, int32_t accumulate, void* hip_stream);
+
+/* Most alternatives of a position. */
+#define NOLOCO_MAX_TOP 32
+
+/*
+ * Plan for logits [W][max_tokens][row_stride], of which the first `vocab` of a row count (the rest is neither read nor
+ * written), with the workspace of noloco_token_log_probs (one hipMalloc, a few MB).
+ *   max_top  most alternatives that a call asks for, up to NOLOCO_MAX_TOP (NOLOCO_ERR_UNSUPPORTED beyond)
+ * Errors: NOLOCO_ERR_INVALID_ARG (row_stride < vocab among them), NOLOCO_ERR_UNSUPPORTED (vocab above 2^24, W * max_tokens
+ * above 2^31 - 1, or W * max_tokens * row_stride above 2^60), NOLOCO_ERR_DEVICE.  On error *out is null.
+ */
+typedef struct noloco_log_prob_plan noloco_log_prob_plan;
+noloco_status noloco_log_prob_plan_create(int64_t vocab, int64_t row_stride, int32_t W, int64_t max_tokens, int32_t max_top,
+                                          noloco_log_prob_plan** out);
+noloco_status noloco_log_prob_plan_destroy(noloco_log_prob_plan* plan);
+
+/*
+ * Of every row l of logits, with n = log(sum over v of exp(l[v])) and p[v] = exp(l[v] - n):
+ *   log_probs        l[token] - n; 0 where the token is negative or not below vocab (padding)
+ *   entropy          -sum over v of p[v] log p[v]
+ *   norms            n, which the gradient takes
+ *   top_tokens, top_log_probs   the `top` tokens with the largest logits and their l[v] - n, largest first, the lower token first
+ *                    where logits are equal; -1 and -infinity behind the last of a vocabulary that is smaller
+ *   logits           device, [W][num_tokens][row_stride] float or bf16, 16-byte-aligned (rows need not be)
+ *   tokens           device, [W][num_tokens] of token_type
+ *   log_probs, entropy, norms   device, float[W][num_tokens], the last two may be null
+ *   top              0 <= top <= max_top; top_tokens int32 [W][num_tokens][top], top_log_probs float, unused where top is 0
+ * Logits of -infinity have no probability.  Where nothing else is in a row, n and the log probabilities are -infinity and the
+ * entropy is 0.  A NaN or +infinity in a row makes its norm, log probabilities and entropy NaN; a NaN is ranked as -infinity.
+ */
+noloco_status noloco_token_log_probs(const noloco_log_prob_plan* plan, const void* logits, int32_t logits_dtype,
+                                     const void* tokens, int32_t token_type, int64_t num_tokens, float* log_probs,
+                                     float* entropy, float* norms, int32_t top, int32_t* top_tokens, float* top_log_probs,
+                                     void* hip_stream);
+
+/*
+ * dlogits[v] = dlog_prob * ([v = token] - p[v]) - dentropy * p[v] * (log p[v] + entropy)
+ *   norms, entropy   what noloco_token_log_probs left (entropy may be null where dentropy is)
+ *   dlog_probs       device, float[W][num_tokens]; not read where the token is padding
+ *   dentropy         device, float[W][num_tokens], may be null: no gradient of the entropy
+ *   dlogits          device, [W][num_tokens][row_stride] float or bf16, 16-byte-aligned; may be logits itself where the types
+ *                    agree.  Elements behind vocab are left as they are
+ * A row whose norm is -infinity has a gradient of zeros, and so has padding where dentropy is null.
+ */
+noloco_status noloco_token_log_probs_gradient(const noloco_log_prob_plan* plan, const void* logits, int32_t logits_dtype,
+                                              const void* tokens, int32_t token_type, int64_t num_tokens, const float* norms,
+                                              const float* dlog_probs, const float* dentropy, const float* entropy, void* dlogits,
+                                              int32_t dlogits_dtype, void* hip_stream);
+
+/*
  * Latency model (section "Latency results", appendix "Latency analysis").  Host only, seeded
  * Monte-Carlo; no GPU work.  Message and step times are LogNormal(mu, sigma^2), sigma >= 0.
  *

@@ -6,11 +6,13 @@ it libnoloco.so, is loaded on first use of any name below, so that
 `python -m paper_2506_10911_amd.build` can run before the library exists. There is no
 fallback: if the library is missing, that first use raises.
 """
-_NAMES = ("BF16", "EmbeddingPlan", "F32", "I32", "I64", "LaunchPlan", "MuonPlan", "NEWTON_SCHULZ", "NolocoError",
+_NAMES = ("ACT_GELU", "ACT_GELU_TANH", "ACT_NONE", "ACT_RELU", "ACT_SILU", "BF16", "EmbeddingPlan", "F32", "I32", "I64",
+          "LaunchPlan", "LayerNormPlan", "LinearPlan", "LogProbPlan", "MuonPlan", "NEWTON_SCHULZ", "NolocoError",
           "PRODUCTS_AUTO", "PRODUCTS_F16", "PRODUCTS_PAIRS", "copy_probe", "embed_gradient", "embed_lookup", "fill_probe",
-          "library_path", "merge_segments", "muon_step", "orthogonalize", "outer_step", "plan_groups", "plan_routes",
-          "read_probe", "replica_spread", "replica_spread_noalloc", "sim_tree_vs_pair", "sim_barrier_penalty", "strerror",
-          "binding")
+          "layer_norm", "layer_norm_gradient", "library_path", "linear", "linear_gradient", "merge_segments", "muon_step",
+          "orthogonalize", "outer_step", "plan_groups", "plan_routes", "read_probe", "replica_spread",
+          "replica_spread_noalloc", "sim_tree_vs_pair", "sim_barrier_penalty", "strerror", "token_log_probs",
+          "token_log_probs_gradient", "binding")
 
 
 def __getattr__(name):

@@ -14,6 +14,7 @@ import numpy as np
 F32, BF16 = 0, 1
 I32, I64 = 2, 3                                          # types of token ids
 PRODUCTS_AUTO, PRODUCTS_F16, PRODUCTS_PAIRS = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 # Five steps that take singular values from 0.003 to 1 to between 0.7 and 1.2.
 NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 MAX_GROUP = 256
@@ -50,6 +51,15 @@ class _Tuning(C.Structure):
 class _Matrix(C.Structure):
     _fields_ = [("offset", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64), ("row_stride", C.c_int64),
                 ("scale", C.c_float)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("weight", C.c_int64), ("bias", C.c_int64), ("width", C.c_int64)]
+
+
+class _LinearLayer(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("inputs", C.c_int64), ("outputs", C.c_int64), ("row_stride", C.c_int64),
+                ("bias", C.c_int64), ("transposed", C.c_int32)]
 
 
 def _load():
@@ -103,6 +113,16 @@ def _load():
     L.noloco_embedding_plan_create.argtypes = [C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int64, C.POINTER(C.c_void_p)]
     L.noloco_embedding_plan_destroy.restype = C.c_int
     L.noloco_embedding_plan_destroy.argtypes = [C.c_void_p]
+    L.noloco_layer_norm_plan_create.restype = C.c_int
+    L.noloco_layer_norm_plan_create.argtypes = [C.POINTER(_Norm), C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.POINTER(C.c_void_p)]
+    L.noloco_linear_plan_create.restype = C.c_int
+    L.noloco_linear_plan_create.argtypes = [C.POINTER(_LinearLayer), C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_int64,
+                                            C.POINTER(C.c_void_p)]
+    L.noloco_log_prob_plan_create.restype = C.c_int
+    L.noloco_log_prob_plan_create.argtypes = [C.c_int64, C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.POINTER(C.c_void_p)]
+    for destroy in (L.noloco_layer_norm_plan_destroy, L.noloco_linear_plan_destroy, L.noloco_log_prob_plan_destroy):
+        destroy.restype = C.c_int
+        destroy.argtypes = [C.c_void_p]
     L.noloco_copy_probe.restype = C.c_int
     L.noloco_copy_probe.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
     L.noloco_read_probe.restype = C.c_int
@@ -132,6 +152,9 @@ def _load_calls():
     _calls.bind(*(C.cast(f, C.c_void_p).value for f in functions), _int32)
     inner = (_lib.noloco_orthogonalize, _lib.noloco_muon_step, _lib.noloco_embed_lookup, _lib.noloco_embed_gradient)
     _calls.bind_inner(*(C.cast(f, C.c_void_p).value for f in inner))
+    model = (_lib.noloco_layer_norm, _lib.noloco_layer_norm_gradient, _lib.noloco_linear, _lib.noloco_linear_gradient,
+             _lib.noloco_token_log_probs, _lib.noloco_token_log_probs_gradient)
+    _calls.bind_model(*(C.cast(f, C.c_void_p).value for f in model))
     return _calls
 
 
@@ -142,7 +165,10 @@ EXPORTS = ("noloco_plan_groups", "noloco_plan_routes", "noloco_merge_segments", 
            "noloco_outer_step", "noloco_replica_spread", "noloco_replica_spread_noalloc",
            "noloco_muon_plan_create", "noloco_muon_plan_destroy", "noloco_muon_plan_info", "noloco_orthogonalize",
            "noloco_muon_step", "noloco_embedding_plan_create", "noloco_embedding_plan_destroy", "noloco_embed_lookup",
-           "noloco_embed_gradient", "noloco_sim_tree_vs_pair",
+           "noloco_embed_gradient", "noloco_layer_norm_plan_create", "noloco_layer_norm_plan_destroy", "noloco_layer_norm",
+           "noloco_layer_norm_gradient", "noloco_linear_plan_create", "noloco_linear_plan_destroy", "noloco_linear",
+           "noloco_linear_gradient", "noloco_log_prob_plan_create", "noloco_log_prob_plan_destroy", "noloco_token_log_probs",
+           "noloco_token_log_probs_gradient", "noloco_sim_tree_vs_pair",
            "noloco_sim_barrier_penalty", "noloco_copy_probe", "noloco_read_probe", "noloco_fill_probe",
            "noloco_strerror")
 
@@ -378,6 +404,129 @@ def embed_gradient(plan: EmbeddingPlan, dout, dout_dtype: int, tokens, token_typ
                                    accumulate, _stream(stream))
     if status != 0:
         raise NolocoError(status, "noloco_embed_gradient")
+
+
+class _ModelPlan:
+    """What the plans of layer norm, matrices and log probabilities share."""
+
+    _handle, _address, _destroy = C.c_void_p(0), 0, None
+
+    def destroy(self):
+        if self._handle:
+            handle, self._handle, self._address = self._handle, C.c_void_p(0), 0
+            _check(getattr(_lib, self._destroy)(handle), self._destroy)
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+class LayerNormPlan(_ModelPlan):
+    """noloco_layer_norm_plan_create / _destroy: the layer norms of every worker's row, each (weight, bias, width) with the
+    places of its weights and biases in the row (bias -1 or None: none), for up to max_tokens tokens a worker."""
+
+    _destroy = "noloco_layer_norm_plan_destroy"
+
+    def __init__(self, norms, worker_stride: int, W: int, max_tokens: int):
+        self._handle = C.c_void_p(0)
+        arr = (_Norm * max(len(norms), 1))()
+        for slot, (weight, bias, width) in zip(arr, norms):
+            slot.weight, slot.bias, slot.width = int(weight), -1 if bias is None else int(bias), int(width)
+        _check(_lib.noloco_layer_norm_plan_create(arr, len(norms), int(worker_stride), int(W), int(max_tokens),
+                                                  C.byref(self._handle)), "noloco_layer_norm_plan_create")
+        self._address = self._handle.value
+
+
+def layer_norm(plan: LayerNormPlan, norm: int, x, x_dtype: int, theta, theta_dtype: int, num_tokens: int, eps: float, out,
+               out_dtype: int, stats=None, stream=None):
+    """noloco_layer_norm: out <- (x - mean) rstd weight + bias with the plan's norm number `norm`; stats: float [W, num_tokens, 2]."""
+    status = _calls.layer_norm(plan._address, norm, x, x_dtype, theta, theta_dtype, num_tokens, eps, out, out_dtype, stats,
+                               _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_layer_norm")
+
+
+def layer_norm_gradient(plan: LayerNormPlan, norm: int, dout, dout_dtype: int, x, x_dtype: int, theta, theta_dtype: int, stats,
+                        num_tokens: int, dx, dx_dtype: int, grad, grad_dtype: int, accumulate: bool = False, add=None, stream=None):
+    """noloco_layer_norm_gradient: dx <- (add +) the norm's gradient, and those of its weights in grad (None: not wanted)."""
+    status = _calls.layer_norm_gradient(plan._address, norm, dout, dout_dtype, x, x_dtype, theta, theta_dtype, stats, num_tokens,
+                                        add, dx, dx_dtype, grad, grad_dtype, accumulate, _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_layer_norm_gradient")
+
+
+class LinearPlan(_ModelPlan):
+    """noloco_linear_plan_create / _destroy: the matrices of every worker's row, each (offset, inputs, outputs) or (offset,
+    inputs, outputs, bias) or (offset, inputs, outputs, bias, transposed) or (offset, inputs, outputs, bias, transposed,
+    row_stride), bias -1 or None: none, for up to max_tokens tokens a worker."""
+
+    _destroy = "noloco_linear_plan_destroy"
+
+    def __init__(self, layers, worker_stride: int, W: int, max_tokens: int, workspace_bytes: int = 0):
+        self._handle = C.c_void_p(0)
+        arr = (_LinearLayer * max(len(layers), 1))()
+        for slot, m in zip(arr, layers):
+            slot.offset, slot.inputs, slot.outputs = int(m[0]), int(m[1]), int(m[2])
+            slot.bias = int(m[3]) if len(m) > 3 and m[3] is not None else -1
+            slot.transposed = int(m[4]) if len(m) > 4 else 0
+            slot.row_stride = int(m[5]) if len(m) > 5 else (slot.inputs if slot.transposed else slot.outputs)
+        _check(_lib.noloco_linear_plan_create(arr, len(layers), int(worker_stride), int(W), int(max_tokens), int(workspace_bytes),
+                                              C.byref(self._handle)), "noloco_linear_plan_create")
+        self._address = self._handle.value
+
+
+def linear(plan: LinearPlan, layer: int, x, x_dtype: int, theta, theta_dtype: int, num_tokens: int, out, out_dtype: int,
+           activation: int = ACT_NONE, residual=None, before=None, stream=None):
+    """noloco_linear: out <- act(x M + bias) + residual with the plan's layer number `layer`; before <- x M + bias."""
+    status = _calls.linear(plan._address, layer, x, x_dtype, theta, theta_dtype, num_tokens, activation, residual, before, out,
+                           out_dtype, _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_linear")
+
+
+def linear_gradient(plan: LinearPlan, layer: int, dout, dout_dtype: int, x, x_dtype: int, theta, theta_dtype: int, num_tokens: int,
+                    dx, dx_dtype: int, grad, grad_dtype: int, activation: int = ACT_NONE, before=None, accumulate: bool = False,
+                    add=None, stream=None):
+    """noloco_linear_gradient: dx <- (add +) dz M^T and M's and the bias's gradients in grad, with dz = dout act'(before);
+    dx or grad None: not wanted."""
+    status = _calls.linear_gradient(plan._address, layer, dout, dout_dtype, x, x_dtype, theta, theta_dtype, num_tokens, activation,
+                                    before, add, dx, dx_dtype, grad, grad_dtype, accumulate, _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_linear_gradient")
+
+
+class LogProbPlan(_ModelPlan):
+    """noloco_log_prob_plan_create / _destroy: logits [W, up to max_tokens, row_stride], of which `vocab` count (row_stride
+    None: all), with up to max_top alternatives a position."""
+
+    _destroy = "noloco_log_prob_plan_destroy"
+
+    def __init__(self, vocab: int, W: int, max_tokens: int, row_stride=None, max_top: int = 0):
+        self._handle = C.c_void_p(0)
+        _check(_lib.noloco_log_prob_plan_create(int(vocab), int(vocab if row_stride is None else row_stride), int(W), int(max_tokens),
+                                                int(max_top), C.byref(self._handle)), "noloco_log_prob_plan_create")
+        self._address = self._handle.value
+
+
+def token_log_probs(plan: LogProbPlan, logits, logits_dtype: int, tokens, token_type: int, num_tokens: int, log_probs, entropy=None,
+                    norms=None, top: int = 0, top_tokens=None, top_log_probs=None, stream=None):
+    """noloco_token_log_probs: log_probs[w, t] <- log softmax(logits[w, t])[tokens[w, t]], 0 where the token is none of the
+    vocabulary; entropy, norms (log sum exp) and the `top` likeliest tokens where they are asked for."""
+    status = _calls.token_log_probs(plan._address, logits, logits_dtype, tokens, token_type, num_tokens, log_probs, entropy, norms,
+                                    top, top_tokens, top_log_probs, _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_token_log_probs")
+
+
+def token_log_probs_gradient(plan: LogProbPlan, logits, logits_dtype: int, tokens, token_type: int, num_tokens: int, norms,
+                             dlog_probs, dlogits, dlogits_dtype: int, dentropy=None, entropy=None, stream=None):
+    """noloco_token_log_probs_gradient: dlogits <- the gradient from those of the log probabilities and of the entropy."""
+    status = _calls.token_log_probs_gradient(plan._address, logits, logits_dtype, tokens, token_type, num_tokens, norms, dlog_probs,
+                                             dentropy, entropy, dlogits, dlogits_dtype, _stream(stream))
+    if status != 0:
+        raise NolocoError(status, "noloco_token_log_probs_gradient")
 
 
 def copy_probe(dst, src, nbytes: int, stream=None):

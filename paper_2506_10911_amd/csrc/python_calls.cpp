@@ -326,6 +326,140 @@ PyObject* bind_inner(PyObject*, PyObject* const* args, Py_ssize_t count) {
   Py_RETURN_NONE;
 }
 
+decltype(&noloco_layer_norm) layer_norm_fn = nullptr;
+decltype(&noloco_layer_norm_gradient) layer_norm_gradient_fn = nullptr;
+decltype(&noloco_linear) linear_fn = nullptr;
+decltype(&noloco_linear_gradient) linear_gradient_fn = nullptr;
+decltype(&noloco_token_log_probs) log_probs_fn = nullptr;
+decltype(&noloco_token_log_probs_gradient) log_probs_gradient_fn = nullptr;
+
+// The arguments of a call, one after the other, as the types they are taken as.
+struct Arguments {
+  PyObject* const* args;
+  bool take(void** out) { return address_of(*args++, out); }
+  bool take(float** out) { return take(reinterpret_cast<void**>(out)); }
+  bool take(int32_t** out) { return take(reinterpret_cast<void**>(out)); }
+  bool take(int32_t* out) { return int32_of(*args++, out); }
+  bool take(float* out) { return float_of(*args++, out); }
+  bool take(int64_t* out) {
+    *out = PyLong_AsLongLong(*args++);
+    return !PyErr_Occurred();
+  }
+  template <typename... T> bool all(T*... out) { return (take(out) && ...); }
+};
+
+template <typename Call> PyObject* status_of(const Call& call) {
+  noloco_status status;
+  Py_BEGIN_ALLOW_THREADS
+  status = call();
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// layer_norm(plan, norm, x, x_dtype, theta, theta_dtype, num_tokens, eps, out, out_dtype, stats, stream)
+PyObject* layer_norm(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  void *plan, *x, *theta, *out, *stream;
+  float *stats, eps;
+  int32_t norm, x_dtype, theta_dtype, out_dtype;
+  int64_t tokens;
+  if (!counted(count, 12) || !Arguments{args}.all(&plan, &norm, &x, &x_dtype, &theta, &theta_dtype, &tokens, &eps, &out, &out_dtype, &stats, &stream))
+    return nullptr;
+  return status_of([&] {
+    return layer_norm_fn(static_cast<noloco_layer_norm_plan*>(plan), norm, x, x_dtype, theta, theta_dtype, tokens, eps, out, out_dtype, stats, stream);
+  });
+}
+
+// layer_norm_gradient(plan, norm, dout, dout_dtype, x, x_dtype, theta, theta_dtype, stats, num_tokens, add, dx, dx_dtype, grad, grad_dtype,
+//                     accumulate, stream)
+PyObject* layer_norm_gradient(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  void *plan, *dout, *x, *theta, *add, *dx, *grad, *stream;
+  float* stats;
+  int32_t norm, dout_dtype, x_dtype, theta_dtype, dx_dtype, grad_dtype, accumulate;
+  int64_t tokens;
+  if (!counted(count, 17) || !Arguments{args}.all(&plan, &norm, &dout, &dout_dtype, &x, &x_dtype, &theta, &theta_dtype, &stats, &tokens, &add, &dx,
+                                                  &dx_dtype, &grad, &grad_dtype, &accumulate, &stream))
+    return nullptr;
+  return status_of([&] {
+    return layer_norm_gradient_fn(static_cast<noloco_layer_norm_plan*>(plan), norm, dout, dout_dtype, x, x_dtype, theta, theta_dtype, stats, tokens,
+                                  add, dx, dx_dtype, grad, grad_dtype, accumulate, stream);
+  });
+}
+
+// linear(plan, layer, x, x_dtype, theta, theta_dtype, num_tokens, activation, residual, before, out, out_dtype, stream)
+PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  void *plan, *x, *theta, *residual, *before, *out, *stream;
+  int32_t layer, x_dtype, theta_dtype, activation, out_dtype;
+  int64_t tokens;
+  if (!counted(count, 13) || !Arguments{args}.all(&plan, &layer, &x, &x_dtype, &theta, &theta_dtype, &tokens, &activation, &residual, &before, &out,
+                                                  &out_dtype, &stream))
+    return nullptr;
+  return status_of([&] {
+    return linear_fn(static_cast<noloco_linear_plan*>(plan), layer, x, x_dtype, theta, theta_dtype, tokens, activation, residual, before, out,
+                     out_dtype, stream);
+  });
+}
+
+// linear_gradient(plan, layer, dout, dout_dtype, x, x_dtype, theta, theta_dtype, num_tokens, activation, before, add, dx, dx_dtype, grad,
+//                 grad_dtype, accumulate, stream)
+PyObject* linear_gradient(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  void *plan, *dout, *x, *theta, *before, *add, *dx, *grad, *stream;
+  int32_t layer, dout_dtype, x_dtype, theta_dtype, activation, dx_dtype, grad_dtype, accumulate;
+  int64_t tokens;
+  if (!counted(count, 18) || !Arguments{args}.all(&plan, &layer, &dout, &dout_dtype, &x, &x_dtype, &theta, &theta_dtype, &tokens, &activation, &before,
+                                                  &add, &dx, &dx_dtype, &grad, &grad_dtype, &accumulate, &stream))
+    return nullptr;
+  return status_of([&] {
+    return linear_gradient_fn(static_cast<noloco_linear_plan*>(plan), layer, dout, dout_dtype, x, x_dtype, theta, theta_dtype, tokens, activation,
+                              before, add, dx, dx_dtype, grad, grad_dtype, accumulate, stream);
+  });
+}
+
+// token_log_probs(plan, logits, logits_dtype, tokens, token_type, num_tokens, log_probs, entropy, norms, top, top_tokens, top_log_probs, stream)
+PyObject* token_log_probs(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  void *plan, *logits, *tokens, *stream;
+  float *log_probs, *entropy, *norms, *top_log_probs;
+  int32_t logits_dtype, token_type, top, *top_tokens;
+  int64_t num_tokens;
+  if (!counted(count, 13) || !Arguments{args}.all(&plan, &logits, &logits_dtype, &tokens, &token_type, &num_tokens, &log_probs, &entropy, &norms, &top,
+                                                  &top_tokens, &top_log_probs, &stream))
+    return nullptr;
+  return status_of([&] {
+    return log_probs_fn(static_cast<noloco_log_prob_plan*>(plan), logits, logits_dtype, tokens, token_type, num_tokens, log_probs, entropy, norms, top,
+                        top_tokens, top_log_probs, stream);
+  });
+}
+
+// token_log_probs_gradient(plan, logits, logits_dtype, tokens, token_type, num_tokens, norms, dlog_probs, dentropy, entropy, dlogits,
+//                          dlogits_dtype, stream)
+PyObject* token_log_probs_gradient(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  void *plan, *logits, *tokens, *dlogits, *stream;
+  float *norms, *dlog_probs, *dentropy, *entropy;
+  int32_t logits_dtype, token_type, dlogits_dtype;
+  int64_t num_tokens;
+  if (!counted(count, 13) || !Arguments{args}.all(&plan, &logits, &logits_dtype, &tokens, &token_type, &num_tokens, &norms, &dlog_probs, &dentropy,
+                                                  &entropy, &dlogits, &dlogits_dtype, &stream))
+    return nullptr;
+  return status_of([&] {
+    return log_probs_gradient_fn(static_cast<noloco_log_prob_plan*>(plan), logits, logits_dtype, tokens, token_type, num_tokens, norms, dlog_probs,
+                                 dentropy, entropy, dlogits, dlogits_dtype, stream);
+  });
+}
+
+// bind_model(addresses of noloco_layer_norm, _layer_norm_gradient, _linear, _linear_gradient, _token_log_probs, _token_log_probs_gradient)
+PyObject* bind_model(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  if (!counted(count, 6)) return nullptr;
+  void* fn[6];
+  for (int i = 0; i < 6; ++i)
+    if (!address_of(args[i], &fn[i])) return nullptr;
+  layer_norm_fn = reinterpret_cast<decltype(layer_norm_fn)>(fn[0]);
+  layer_norm_gradient_fn = reinterpret_cast<decltype(layer_norm_gradient_fn)>(fn[1]);
+  linear_fn = reinterpret_cast<decltype(linear_fn)>(fn[2]);
+  linear_gradient_fn = reinterpret_cast<decltype(linear_gradient_fn)>(fn[3]);
+  log_probs_fn = reinterpret_cast<decltype(log_probs_fn)>(fn[4]);
+  log_probs_gradient_fn = reinterpret_cast<decltype(log_probs_gradient_fn)>(fn[5]);
+  Py_RETURN_NONE;
+}
+
 template <typename F> PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
 PyMethodDef methods[] = {
@@ -339,6 +473,13 @@ PyMethodDef methods[] = {
     {"muon_step", fast(muon_step), METH_FASTCALL, nullptr},
     {"embed_lookup", fast(embed_lookup), METH_FASTCALL, nullptr},
     {"embed_gradient", fast(embed_gradient), METH_FASTCALL, nullptr},
+    {"bind_model", fast(bind_model), METH_FASTCALL, nullptr},
+    {"layer_norm", fast(layer_norm), METH_FASTCALL, nullptr},
+    {"layer_norm_gradient", fast(layer_norm_gradient), METH_FASTCALL, nullptr},
+    {"linear", fast(linear), METH_FASTCALL, nullptr},
+    {"linear_gradient", fast(linear_gradient), METH_FASTCALL, nullptr},
+    {"token_log_probs", fast(token_log_probs), METH_FASTCALL, nullptr},
+    {"token_log_probs_gradient", fast(token_log_probs_gradient), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
