@@ -22,7 +22,8 @@ OUT = os.path.join(PKG, "libnoloco.so")
 CALLS = os.path.join(PKG, "_calls.so")       # CPython module of the binding
 OBJ = os.path.join(PKG, "_build")
 HOST_SOURCES = ["api.cpp", "planner.cpp", "launch_plan.cpp", "latency_model.cpp", "inner_step.cpp", "model_step.cpp"]   # no device code
-DEVICE_SOURCES = ["kernels.hip", "newton_schulz.hip", "embedding.hip", "layer_norm.hip", "linear.hip", "log_probs.hip"]
+DEVICE_SOURCES = ["kernels.hip", "newton_schulz.hip", "embedding.hip", "layer_norm.hip", "products.hip", "linear.hip",
+                  "log_probs.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ROCM = os.path.dirname(os.path.dirname(os.path.realpath(HIPCC)))

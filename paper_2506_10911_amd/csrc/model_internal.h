@@ -69,7 +69,50 @@ struct ProductArgs {
   void* before;               // the same
 };
 
-int launch_product(const ProductArgs& args, void* stream);
+constexpr double kSmallWork = double(1 << 28);  // multiplications of all workers that make a product a large one
+
+// How a product goes out, by its sizes and types alone (but for the alignment of its operands).  Offsets are into the workspace.
+struct ProductPlan {
+  int32_t tile;               // 0: product_any, 256, 128, or 32 (32 x 256)
+  int32_t f16;                // operands packed to binary16 times powers of two
+  int32_t packed[2], parts[2];
+  uint32_t splits;            // parts that k is shared out in
+  uint64_t packed_at[2], largest_at, exponents_at, parts_at, bytes;      // bytes: of the workspace
+};
+
+// `room`: bytes that there are; sums in parts take what packing leaves of it.
+ProductPlan plan_product(const ProductArgs& args, uint64_t room);
+// Most bytes that packing a product takes for each worker, whatever its types.
+uint64_t pack_bytes(int64_t m, int64_t n, int64_t k);
+constexpr uint64_t kPartsRoom = 64 << 20;      // and for sums in parts, for all workers
+
+struct DirectArgs {
+  const void *a, *b;          // 16-bit numbers, part 0 of worker 0
+  int64_t a_worker, a_ld, a_part, b_worker, b_ld, b_part;
+  uint32_t a_parts, b_parts;  // two bits a segment: which part it takes
+  uint32_t segments, splits;
+  uint32_t tiles_m, tiles_n, run;
+  const int32_t* exponents;   // [W][2]
+  float* parts;               // [splits][W][m][parts_ld], or null
+  int64_t parts_ld;
+};
+
+constexpr int kPackParts = 64;
+struct PackOperand {
+  const void* p;
+  void* out;                  // [parts][W][rows][wide rounded up to eight]; null: not packed
+  int64_t worker_stride, ld;
+  uint32_t rows, wide;
+  int32_t bf16, parts, eights;      // eights: p is at a multiple of 16 bytes
+};
+struct PackArgs {
+  PackOperand operand[2];
+  float* largest;             // [W][2][kPackParts]
+  int32_t* exponents;
+  int32_t f16, W;
+};
+
+int launch_product(const ProductArgs& args, const ProductPlan& plan, char* room, void* stream);
 
 struct SlopeArgs {
   const void* dout;           // [W][tokens][outputs]

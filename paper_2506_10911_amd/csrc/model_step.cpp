@@ -1,5 +1,5 @@
 // C ABI of layer norm, matrices and log probabilities: argument checking, plans, and the split of a call into kernel
-// launches.  All arithmetic is in layer_norm.hip, linear.hip and log_probs.hip.
+// launches.  All arithmetic is in layer_norm.hip, products.hip, linear.hip and log_probs.hip.
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
@@ -14,7 +14,7 @@
 
 namespace {
 
-constexpr int64_t kDefaultWorkspace = 4ll << 30;
+constexpr int64_t kDefaultWorkspace = 1ll << 30;
 constexpr int64_t kMostWidth = 1 << 20, kMostNormTokens = 1 << 27, kMostRows = std::numeric_limits<int32_t>::max();
 constexpr int64_t kMostSide = 1 << 22, kMostTokens = 1 << 24, kMostNumbers = 1 << 30, kMostVocab = 1 << 24;
 
@@ -229,10 +229,83 @@ extern "C" noloco_status noloco_layer_norm_gradient(const noloco_layer_norm_plan
 // Matrices
 // ---------------------------------------------------------------------------
 
+namespace noloco {
+
+namespace {
+
+constexpr uint64_t kMostGroups = 1u << 22;      // workgroups of a launch
+constexpr int64_t kMostRow = 1 << 22;           // numbers from one row of an operand to the next: 256 of them have 32-bit offsets
+
+// Does the operand lie as product_direct loads it?
+bool lies_well(const Operand& o, uint32_t k) {
+  return o.bf16 && aligned(o.p, 16) && o.ld <= kMostRow && ((o.ld | o.worker_stride) & 7) == 0 && (!o.along_k || k % 8 == 0);
+}
+
+uint64_t tiles_of(uint64_t v, uint64_t tile) { return (v + tile - 1) / tile; }
+
+}  // namespace
+
+uint64_t pack_bytes(int64_t m, int64_t n, int64_t k) {
+  auto most = [k](int64_t size) { return static_cast<uint64_t>(std::max(size * ((k + 7) / 8 * 8), k * ((size + 7) / 8 * 8))) * 4; };
+  return whole(most(m)) + whole(most(n)) + 2048;
+}
+
+ProductPlan plan_product(const ProductArgs& args, uint64_t room) {
+  ProductPlan plan{};
+  plan.parts[0] = plan.parts[1] = 1;
+  plan.splits = 1;
+  const uint64_t W = args.W, m = args.m, n = args.n, k = args.k;
+  if (k == 0 || m == 0 || n == 0 || double(W) * m * n * k < kSmallWork) return plan;
+  // Padding to 256 may cost a tenth of the products.
+  const uint64_t big = tiles_of(m, 256) * tiles_of(n, 256) * W, small = tiles_of(m, 128) * tiles_of(n, 128) * W;
+  uint64_t tiles, target;
+  if (m <= 32 && args.a.along_k) {
+    plan.tile = 32;
+    tiles = tiles_of(n, 256) * W;
+    target = 256;
+  } else if (big >= 256 && big * 4 <= small + small / 10) {
+    plan.tile = 256;
+    tiles = big;
+    target = 256;
+  } else {
+    plan.tile = 128;
+    tiles = small;
+    target = 512;
+  }
+  if (tiles > kMostGroups || W * m * ((n + 7) / 8) > kMostGroups * 256 * 64) return ProductPlan{};
+  const int floats = (args.a.bf16 ? 0 : 1) + (args.b.bf16 ? 0 : 1);
+  plan.f16 = args.out_bf16 ? floats == 2 : floats > 0;
+  uint64_t at = 0;
+  for (int i = 0; i < 2; ++i) {
+    const Operand& o = i == 0 ? args.a : args.b;
+    const uint64_t size = i == 0 ? m : n, rows = o.along_k ? size : k, wide = tiles_of(o.along_k ? k : size, 8) * 8;
+    plan.packed[i] = plan.f16 || !lies_well(o, args.k);
+    plan.parts[i] = plan.f16 && !args.out_bf16 && !o.bf16 ? 2 : 1;
+    plan.packed_at[i] = at;
+    if (plan.packed[i]) at += whole(W * rows * wide * 2 * plan.parts[i]);
+  }
+  plan.largest_at = at;
+  at += plan.f16 ? whole(W * 2 * kPackParts * sizeof(float)) : 0;
+  plan.exponents_at = at;
+  at += plan.f16 ? whole(W * 2 * sizeof(int32_t)) : 0;
+  plan.parts_at = at;
+  const uint64_t segments = plan.parts[0] + plan.parts[1] - 1, stages = tiles_of(k, 64) * segments;
+  const uint64_t part = W * m * (tiles_of(n, 8) * 8) * sizeof(float), left = room > at ? std::min(room - at, kPartsRoom) : 0;
+  plan.splits = static_cast<uint32_t>(std::max<uint64_t>(1, std::min({target / std::max<uint64_t>(tiles, 1), stages / 8, left / part, uint64_t(32)})));
+  if (plan.splits > 1) at += plan.splits * part;
+  plan.bytes = at;
+  return plan;
+}
+
+}  // namespace noloco
+
 namespace {
 
 // Workspace that one worker's gradient needs: dz in binary32, and the bias's sums.
 uint64_t dz_bytes(const noloco_linear_layer& l, int64_t tokens) { return whole(static_cast<uint64_t>(tokens) * l.outputs * sizeof(float)); }
+uint64_t packed_bytes(const noloco_linear_layer& l, int64_t tokens) {
+  return std::max({noloco::pack_bytes(tokens, l.outputs, l.inputs), noloco::pack_bytes(tokens, l.inputs, l.outputs), noloco::pack_bytes(l.inputs, l.outputs, tokens)});
+}
 uint64_t sums_bytes(const noloco_linear_layer& l, int64_t tokens) { return whole(static_cast<uint64_t>(noloco::slope_groups(tokens)) * l.outputs * sizeof(float)); }
 
 // Does a run of `count` elements from `at` on share one with a matrix of `rows` rows of `cols`?
@@ -268,11 +341,14 @@ extern "C" noloco_status noloco_linear_plan_create(const noloco_linear_layer* la
   noloco_status st = check_rows(num_layers, layers, worker_stride, W, max_tokens);
   if (st != NOLOCO_OK) return st;
   if (max_tokens > kMostTokens) return NOLOCO_ERR_UNSUPPORTED;
-  uint64_t one = 0;
+  uint64_t one = 0, parts = 0;
   for (int32_t i = 0; i < num_layers; ++i) {
-    st = check_layer(layers[i], worker_stride, max_tokens);
+    const noloco_linear_layer& l = layers[i];
+    st = check_layer(l, worker_stride, max_tokens);
     if (st != NOLOCO_OK) return st;
-    one = std::max(one, dz_bytes(layers[i], max_tokens) + sums_bytes(layers[i], max_tokens));
+    one = std::max(one, dz_bytes(l, max_tokens) + sums_bytes(l, max_tokens) + packed_bytes(l, max_tokens));
+    const double numbers = double(W) * std::max({double(max_tokens) * l.inputs, double(max_tokens) * l.outputs, double(l.inputs) * l.outputs});
+    parts = std::max(parts, static_cast<uint64_t>(std::min(numbers * 32 * sizeof(float), double(noloco::kPartsRoom))));
   }
   try {
     std::unique_ptr<noloco_linear_plan> plan(new noloco_linear_plan);
@@ -281,7 +357,7 @@ extern "C" noloco_status noloco_linear_plan_create(const noloco_linear_layer* la
     plan->max_tokens = max_tokens;
     plan->W = W;
     const uint64_t asked = workspace_bytes > 0 ? workspace_bytes : kDefaultWorkspace;
-    plan->room = std::max(one, std::min(one * W, asked));
+    plan->room = std::max(one, std::min(one * W, asked)) + whole(parts);
     if (!plan->block.allocate(plan->room)) return NOLOCO_ERR_DEVICE;
     *out = plan.release();
     return NOLOCO_OK;
@@ -302,6 +378,26 @@ char* offset(void* p, int64_t elements, int32_t dtype) { return static_cast<char
 // Activations [tokens][width] as an operand whose k runs along the width, or along the tokens.
 noloco::Operand rows_operand(const void* p, int64_t tokens, int64_t width, int32_t dtype, bool along_width) {
   return {p, tokens * width, width, along_width ? 1 : 0, dtype == NOLOCO_BF16 ? 1 : 0};
+}
+
+// A product, in batches of workers whose packed operands fit `bytes` of the workspace from `room` on.
+bool run_product(noloco::ProductArgs args, char* room, uint64_t bytes, int32_t W, void* stream) {
+  for (int32_t w = 0; w < W; w += args.W) {
+    args.W = W - w;
+    noloco::ProductPlan plan = noloco::plan_product(args, bytes);
+    while (plan.bytes > bytes && args.W > 1) {
+      args.W = (args.W + 1) / 2;
+      plan = noloco::plan_product(args, bytes);
+    }
+    if (noloco::launch_product(args, plan, room, stream) != 0) return false;
+    for (noloco::Operand* o : {&args.a, &args.b}) o->p = static_cast<const char*>(o->p) + args.W * o->worker_stride * (o->bf16 ? 2 : 4);
+    const int32_t out_dtype = args.out_bf16 ? NOLOCO_BF16 : NOLOCO_F32;
+    args.out = offset(args.out, args.W * args.out_stride, out_dtype);
+    if (args.more != nullptr) args.more = offset(args.more, args.W * args.out_stride, out_dtype);
+    if (args.before != nullptr) args.before = offset(args.before, args.W * args.out_stride, out_dtype);
+    if (args.bias != nullptr) args.bias = offset(args.bias, args.W * args.bias_stride, args.bias_bf16 ? NOLOCO_BF16 : NOLOCO_F32);
+  }
+  return true;
 }
 
 noloco_status check_linear(const noloco_linear_plan* plan, int32_t layer, int64_t num_tokens, int32_t activation) {
@@ -348,7 +444,7 @@ extern "C" noloco_status noloco_linear(const noloco_linear_plan* plan, int32_t l
   args.before = before;
   const noloco_status there = check_device(plan->block.device);
   if (there != NOLOCO_OK) return there;
-  return noloco::launch_product(args, hip_stream) == 0 ? NOLOCO_OK : NOLOCO_ERR_DEVICE;
+  return run_product(args, plan->block.memory, plan->room, plan->W, hip_stream) ? NOLOCO_OK : NOLOCO_ERR_DEVICE;
 }
 
 extern "C" noloco_status noloco_linear_gradient(const noloco_linear_plan* plan, int32_t layer, const void* dout, int32_t dout_dtype,
@@ -377,15 +473,20 @@ extern "C" noloco_status noloco_linear_gradient(const noloco_linear_plan* plan, 
   const noloco_status there = check_device(plan->block.device);
   if (there != NOLOCO_OK) return there;
 
-  // dz is kept in binary32 where a float result takes it, unless it is dout itself, or zeros in places of it.
-  const bool fine = (dx != nullptr && dx_dtype == NOLOCO_F32) || (grad != nullptr && grad_dtype == NOLOCO_F32);
+  // dz is kept in binary32 where a float result takes it, or a product with a float operand (one of two operands may be rounded to
+  // bf16, as the result is), unless it is dout itself, or zeros in places of it.
+  const bool fine = (dx != nullptr && (dx_dtype == NOLOCO_F32 || theta_dtype == NOLOCO_F32)) ||
+                    (grad != nullptr && (grad_dtype == NOLOCO_F32 || x_dtype == NOLOCO_F32)) ||
+                    double(plan->W) * T * l.inputs * l.outputs < noloco::kSmallWork;
   const int32_t dz_dtype = !acts || activation == NOLOCO_ACT_RELU ? dout_dtype : (fine ? NOLOCO_F32 : NOLOCO_BF16);
   const bool sums = grad != nullptr && l.bias >= 0;
   const uint64_t room_dz = acts ? whole(static_cast<uint64_t>(T) * l.outputs * bytes_of(dz_dtype)) : 0, room_sums = sums ? sums_bytes(l, T) : 0;
-  const int32_t batch = room_dz + room_sums == 0 ? plan->W : static_cast<int32_t>(std::min<uint64_t>(plan->W, plan->room / (room_dz + room_sums)));
+  const uint64_t packed = packed_bytes(l, T);
+  const int32_t batch = room_dz + room_sums == 0 ? plan->W : static_cast<int32_t>(std::min<uint64_t>(plan->W, (plan->room - packed) / (room_dz + room_sums)));
   for (int32_t w = 0; w < plan->W; w += batch) {
     const int32_t W = std::min(batch, plan->W - w);
     char* const dz_room = plan->block.memory;
+    const uint64_t used = W * (room_dz + room_sums);
     const void* dz = offset(dout, w * T * l.outputs, dout_dtype);
     if (acts || sums) {
       noloco::SlopeArgs args{};
@@ -420,7 +521,7 @@ extern "C" noloco_status noloco_linear_gradient(const noloco_linear_plan* plan, 
       args.out_ld = l.inputs;
       args.out_bf16 = dx_dtype == NOLOCO_BF16;
       args.more = add == nullptr ? nullptr : offset(add, w * T * l.inputs, dx_dtype);
-      if (noloco::launch_product(args, hip_stream) != 0) return NOLOCO_ERR_DEVICE;
+      if (!run_product(args, dz_room + used, plan->room - used, W, hip_stream)) return NOLOCO_ERR_DEVICE;
     }
     if (grad != nullptr) {
       noloco::ProductArgs args{};
@@ -437,7 +538,7 @@ extern "C" noloco_status noloco_linear_gradient(const noloco_linear_plan* plan, 
       args.out_ld = l.row_stride;
       args.out_bf16 = grad_dtype == NOLOCO_BF16;
       args.accumulate = accumulate;
-      if (noloco::launch_product(args, hip_stream) != 0) return NOLOCO_ERR_DEVICE;
+      if (!run_product(args, dz_room + used, plan->room - used, W, hip_stream)) return NOLOCO_ERR_DEVICE;
     }
   }
   return NOLOCO_OK;

@@ -1,0 +1,736 @@
+// Products sum over k of A(m, k) B(n, k) with bias, activation and residual in their end (kernels and their launchers):
+// what matrices do forward (z = x M + bias, out = act(z) + residual) and backward (dx = dz M^T + add, M's gradient x^T dz).
+// Operands lie with their numbers along k or along m (n) next to each other; the matrix cores take 16-bit ones.
+//
+// Large products (product_direct) load bf16 operands past the registers to the LDS as they lie.  Others are packed first, to
+// rows that begin at multiples of 16 bytes:
+//   bf16 result, one float operand     that one rounded to bf16, which costs as much as the result's own rounding
+//   bf16 result, two float operands    both rounded to binary16 (11 bits), each times a power of two of its worker
+//   float result, float operands       a float one as a pair of binary16 (22 bits), a bf16 one as one, times powers of two; the
+//                                      products of two pairs but that of their low halves.  What a pair leaves of a number is
+//                                      2^-22 of it or 2^-40 of the operand's largest.
+// Small products (product_any), which packing would make longer, take any operands through the registers and a float one apart
+// into bf16: two of them, 16 bits, for a bf16 result; three, which together are the number, for a float one, and the products of
+// parts that reach 2^-16 of the largest.
+#include <type_traits>
+
+#include "activations.h"
+#include "device_numbers.h"
+#include "model_internal.h"
+
+namespace noloco {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef uint16_t ushort8 __attribute__((ext_vector_type(8)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+
+#define lds_memory __attribute__((address_space(3)))
+
+// The end of a product for N neighbouring numbers of a row.
+template <int N> __device__ __forceinline__ void finish(const ProductArgs& a, int64_t w, uint32_t m, uint32_t n, float* v) {
+  const int64_t at = w * a.out_stride + m * a.out_ld + n;
+  if (a.bias != nullptr) {
+    float bias[N];
+    load_numbers<N>(a.bias, w * a.bias_stride + n, a.bias_bf16, bias);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += bias[i];
+  }
+  if (a.before != nullptr) store_numbers<N>(a.before, at, a.out_bf16, v);
+  if (a.activation != NOLOCO_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = activate(a.activation, v[i]);
+  }
+  if (a.more != nullptr || a.accumulate) {
+    float more[N];
+    load_numbers<N>(a.accumulate ? a.out : a.more, at, a.out_bf16, more);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += more[i];
+  }
+  store_numbers<N>(a.out, at, a.out_bf16, v);
+}
+
+// Do N neighbouring numbers (four or eight) of everything that the end of a product touches lie at a multiple of their vectors' size?
+template <int N> __device__ __forceinline__ bool ends_in(const ProductArgs& a) {
+  auto fits = [](const void* p, int32_t bf16) { return reinterpret_cast<uintptr_t>(p) % (bf16 ? 2 * N : 16) == 0; };
+  return ((a.out_stride | a.out_ld) & (N - 1)) == 0 && fits(a.out, a.out_bf16) && fits(a.more, a.out_bf16) && fits(a.before, a.out_bf16) &&
+         (a.bias == nullptr || ((a.bias_stride & (N - 1)) == 0 && fits(a.bias, a.bias_bf16)));
+}
+
+// ---------------------------------------------------------------------------
+// Small products, and any operands
+// ---------------------------------------------------------------------------
+
+constexpr int kTile = 128, kDepth = 32;
+constexpr int kPlane = kTile * kDepth * 2;       // bytes of one part of an operand's stage
+
+// Sixteen neighbouring numbers of an operand, as they come from memory; those that are not there are zeros.
+template <typename E> struct Sixteen {
+  E v[16];
+  __device__ __forceinline__ void load(const E* p, int there, bool whole) {
+    if (whole) {
+      constexpr int kVector = 16 / sizeof(E);
+      typedef E vector __attribute__((ext_vector_type(kVector)));
+#pragma unroll
+      for (int i = 0; i < 16; i += kVector) {
+        const vector x = *reinterpret_cast<const vector*>(p + i);
+#pragma unroll
+        for (int k = 0; k < kVector; ++k) v[i + k] = x[k];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = i < there ? p[i] : E(0);
+    }
+  }
+  // Part `part` of PARTS of numbers first .. first + 7.
+  template <int PARTS> __device__ __forceinline__ ushort8 part(int part, int first) const {
+    ushort8 out;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(E) == 2) {
+        out[i] = v[first + i];
+      } else if constexpr (PARTS == 1) {
+        out[i] = narrow(v[first + i]);
+      } else {
+        // cut, not rounded: each rest is exact, and the third has at most eight bits
+        float x = v[first + i];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          if (k < part) x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+        out[i] = part == PARTS - 1 ? narrow(x) : static_cast<uint16_t>(__float_as_uint(x) >> 16);
+      }
+    }
+    return out;
+  }
+};
+
+// 128 x 128 of the result by four waves, each 64 x 64 in blocks of 32 x 32.  Operands come through registers, where they are
+// taken apart, one stage of 32 k ahead of the products.
+//
+// Numbers along k: rows of 64 bytes, 16-byte chunk q of row r at q ^ (r >> 2 & 3), so that 16 lanes meet 16 quarters of the
+// LDS's banks.  Numbers along m: rows of 256 bytes, one k each, chunk q of row k at q ^ (k & 3) << 2, turned by the LDS's
+// transposing reads.
+template <typename TA, typename TB, bool ALONG_A, bool ALONG_B, int PA, int PB>
+__global__ __launch_bounds__(256) void product_any(ProductArgs a) {
+  __shared__ __align__(1024) char lds[(PA + PB) * kPlane];
+  const uint32_t thread = threadIdx.x, lane = thread & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  const uint32_t wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+  const uint32_t tiles_m = (a.m + kTile - 1) / kTile;
+  const uint32_t m0 = blockIdx.x % tiles_m * kTile, n0 = blockIdx.x / tiles_m * kTile;
+  const int64_t w = blockIdx.y;
+  const TA* const pa = static_cast<const TA*>(a.a.p) + w * a.a.worker_stride;
+  const TB* const pb = static_cast<const TB*>(a.b.p) + w * a.b.worker_stride;
+
+  auto load = [&](auto& into, const auto* p, int64_t ld, auto along, uint32_t first, uint32_t size, uint32_t k0) {
+    typedef typename std::remove_reference<decltype(*p)>::type E;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(p) | static_cast<uint64_t>(ld) * sizeof(E)) & 15) == 0;
+    const uint32_t row = first + (along ? thread >> 1 : (thread & 7) * 16), k = k0 + (along ? (thread & 1) * 16 : thread >> 3);
+    const int64_t there = along ? (row < size ? static_cast<int64_t>(a.k) - k : 0) : (k < a.k ? static_cast<int64_t>(size) - row : 0);
+    const int64_t at = along ? row * ld + k : k * ld + row;
+    into.load(p + (there > 0 ? at : 0), static_cast<int>(there < 0 ? 0 : there < 16 ? there : 16), aligned && there >= 16);
+  };
+  auto put = [&](const auto& from, auto along, auto parts, char* to) {
+    constexpr int P = decltype(parts)::value;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t row = along ? thread >> 1 : thread >> 3, q = along ? (thread & 1) * 2 + h : (thread & 7) * 2 + h;
+        const uint32_t at = along ? row * 64 + ((q ^ (row >> 2 & 3)) << 4) : row * 256 + ((q ^ (row & 3) << 2) << 4);
+        *reinterpret_cast<ushort8*>(to + p * kPlane + at) = from.template part<P>(p, h * 8);
+      }
+  };
+  // Fragment: number lane % 32 of a block of 32, eight k from 8 (lane / 32) on.
+  const uint32_t of32 = lane & 31, half = lane >> 5;
+  auto fragment = [&](const char* plane, auto along, uint32_t first, int slice) {
+    if (along) {
+      const uint32_t row = first + of32, q = slice * 2 + half;
+      return *reinterpret_cast<const bf16x8*>(plane + row * 64 + ((q ^ (row >> 2 & 3)) << 4));
+    } else {
+      const uint32_t k = slice * 16 + half * 8 + (lane >> 2 & 3), byte = first * 2 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+      const char* const at = plane + k * 256 + (((byte >> 4) ^ (k & 3) << 2) << 4) + (byte & 15);
+      const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(at));
+      const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(at + 4 * 256));
+      return __builtin_bit_cast(bf16x8, static_cast<short8v>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
+    }
+  };
+  typedef typename std::conditional<ALONG_A, Yes, No>::type AlongA;
+  typedef typename std::conditional<ALONG_B, Yes, No>::type AlongB;
+  Sixteen<TA> next_a;
+  Sixteen<TB> next_b;
+  float16v acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  if (a.k > 0) {
+    load(next_a, pa, a.a.ld, AlongA{}, m0, a.m, 0);
+    load(next_b, pb, a.b.ld, AlongB{}, n0, a.n, 0);
+  }
+  for (uint32_t k0 = 0; k0 < a.k; k0 += kDepth) {
+    put(next_a, AlongA{}, Number<PA>{}, lds);
+    put(next_b, AlongB{}, Number<PB>{}, lds + PA * kPlane);
+    __syncthreads();
+    if (k0 + kDepth < a.k) {
+      load(next_a, pa, a.a.ld, AlongA{}, m0, a.m, k0 + kDepth);
+      load(next_b, pb, a.b.ld, AlongB{}, n0, a.n, k0 + kDepth);
+    }
+#pragma unroll
+    for (int slice = 0; slice < kDepth / 16; ++slice) {
+      bf16x8 fa[PA][2], fb[PB][2];
+#pragma unroll
+      for (int p = 0; p < PA; ++p)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fa[p][i] = fragment(lds + p * kPlane, AlongA{}, wm + i * 32, slice);
+#pragma unroll
+      for (int p = 0; p < PB; ++p)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) fb[p][j] = fragment(lds + (PA + p) * kPlane, AlongB{}, wn + j * 32, slice);
+      // the small products first
+#pragma unroll
+      for (int both = PA > 2 || PB > 2 ? 2 : 1; both >= 0; --both)
+#pragma unroll
+        for (int p = 0; p <= both; ++p) {
+          if (p >= PA || both - p >= PB) continue;
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[both - p][j], fa[p][i], acc[i][j], 0, 0, 0);
+        }
+    }
+    __syncthreads();
+  }
+
+  // Block (i, j), element e of a lane: m = 32 i + of32, n = 32 j + 8 (e / 4) + 4 half + e % 4.
+  const bool fours = ends_in<4>(a);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const uint32_t m = m0 + wm + i * 32 + of32, n = n0 + wn + j * 32 + e * 2 + half * 4;
+        if (m >= a.m || n >= a.n) continue;
+        float v[4] = {acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        if (fours && n + 4 <= a.n) {
+          finish<4>(a, w, m, n, v);
+        } else {
+#pragma unroll 1
+          for (uint32_t c = 0; c < 4 && n + c < a.n; ++c) {
+            float one = c == 0 ? v[0] : (c == 1 ? v[1] : (c == 2 ? v[2] : v[3]));
+            finish<1>(a, w, m, n + c, &one);
+          }
+        }
+      }
+}
+
+// ---------------------------------------------------------------------------
+// Large products
+// ---------------------------------------------------------------------------
+
+// 16 bytes a lane from a buffer to the LDS, at `to` + 16 times the lane, past the registers; zeros for what lies behind the buffer's
+// last byte.  The compiler does not count these loads: who reads what they bring waits for vmcnt itself.  m0 is a register that the
+// compiler keeps nothing in and that a clobber list may not name; its own instructions that read it, each behind a write of
+// its own, are none in these kernels.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v))); }
+__device__ __forceinline__ uint4v buffer_words(uint64_t at, uint32_t bytes) {
+  return uint4v{uniform(static_cast<uint32_t>(at)), uniform(static_cast<uint32_t>(at >> 32) & 0xffffu), uniform(bytes), 0x00020000u};
+}
+__device__ __forceinline__ void load_to_lds(uint4v buffer, uint32_t lane_offset, uint32_t to) {
+  to = uniform(to);
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" :: "v"(lane_offset), "s"(buffer), "s"(to) : "memory");
+}
+
+// Workgroups are dealt to the 8 XCDs in turn; each XCD takes runs of `run` consecutive tiles, which share rows and columns in
+// its L2: 32 of 256 x 256, one round of its CUs, 64 of the smaller ones, of which two share a CU.
+__device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t blocks, uint32_t run) {
+  const uint32_t whole = blocks / (8 * run) * (8 * run);
+  if (block >= whole) return block;
+  const uint32_t xcd = block & 7u, slot = block >> 3, k = slot / run;
+  return (k * 8 + xcd) * run + (slot - k * run);
+}
+
+constexpr uint32_t kBehind = 0xfffffff0u;       // an offset behind every buffer
+
+// How one operand's stages of 64 k come to the LDS and are read from it: T numbers along m (or n), by WAVES waves.
+//   ALONG  rows of 128 bytes, one number of m each: 16-byte chunk q of row r lies at q ^ (r >> 1 & 7), so that the 16 lanes that read
+//          at once meet 16 different quarters of the 64 banks
+//   else   rows of 2 T bytes, one k each: chunk q of row k at q ^ (k & 3) << 2 (128-byte rows: q ^ (k >> 1 & 1) << 2), since four lanes of
+//          a group of 16 read each of four rows; turned by the LDS's transposing reads
+template <int T, int WAVES, bool ALONG> struct Stages {
+  static constexpr int kBytes = T * 128, kLoads = T / 8 / WAVES, kRow = ALONG ? 128 : T * 2, kRows = 1024 / kRow;
+  static_assert(kLoads >= 1 && kRow <= 1024, "tile");
+  uint64_t base;             // of the tile's first number, k = 0, part 0
+  uint64_t k_bytes, part_bytes;      // from one stage of 64 k, and from one part, to the next
+  uint32_t ld_bytes, rows;   // ALONG: rows of the tile that there are; else: numbers of a row from the tile's first on
+  uint32_t offset[kLoads];   // of the lane's 16 bytes of each load
+  uint32_t chunk[2];         // ALONG: which eight k they are, of even and odd loads
+  __device__ __forceinline__ void open(const void* p, int64_t worker, int64_t ld, int64_t part, uint32_t first, uint32_t size, uint32_t lane, uint32_t wave) {
+    base = reinterpret_cast<uint64_t>(p) + 2 * static_cast<uint64_t>(worker + (ALONG ? first * ld : static_cast<int64_t>(first)));
+    ld_bytes = static_cast<uint32_t>(2 * ld);
+    k_bytes = ALONG ? 128 : 64ull * ld_bytes;
+    part_bytes = 2 * part;
+    rows = ALONG ? (size - first < T ? size - first : T) : size - first;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t load = wave * kLoads + i;
+      if constexpr (ALONG) {
+        const uint32_t q = (lane & 7) ^ (((load & 1) << 2 | lane >> 4) & 7);
+        chunk[i & 1] = q;
+        offset[i] = (load * 8 + (lane >> 3)) * ld_bytes + q * 16;
+      } else {
+        const uint32_t in_row = lane * 16 % kRow, k = load * kRows + lane * 16 / kRow;
+        const uint32_t turn = kRow >= 256 ? (k & 3) << 2 : (kRow == 128 ? (k >> 1 & 1) << 2 : 0);
+        offset[i] = k * ld_bytes + ((in_row >> 4) ^ turn) * 16;
+      }
+    }
+  }
+  // Asks for the stage that begins at k = 64 `stage`, of which `k_left` there are.
+  __device__ __forceinline__ void ask(uint32_t part, uint32_t stage, uint32_t k_left, uint32_t to, uint32_t wave) const {
+    const uint64_t at = base + part * part_bytes + stage * k_bytes;
+    const uint32_t deep = k_left < 64 ? k_left : 64;
+    // up to the end of the last vector that holds a number: what is not there whole comes as zeros
+    const uint32_t last = ((ALONG ? k_left : rows) + 7) / 8 * 16, bytes = ((ALONG ? rows : deep) - 1) * ld_bytes + last;
+    const uint4v buffer = buffer_words(at, bytes < kBehind ? bytes : kBehind);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      uint32_t from = offset[i];
+      if constexpr (ALONG) {
+        if (k_left < 64) from = chunk[i & 1] * 8 < k_left ? from : kBehind;
+      }
+      load_to_lds(buffer, from, to + (wave * kLoads + i) * 1024);
+    }
+  }
+  // Where a lane's fragments of blocks of 32 numbers, `first` and on, lie in a stage.
+  template <int BLOCKS> struct Reader {
+    uint32_t at[ALONG ? 1 : BLOCKS], row;
+    __device__ __forceinline__ void open(uint32_t first, uint32_t lane) {
+      if constexpr (ALONG) {
+        row = first + (lane & 31);
+        at[0] = row * 128;
+      } else {
+        const uint32_t k = (lane >> 5) * 8 + (lane >> 2 & 3);
+        const uint32_t turn = kRow >= 256 ? (k & 3) << 2 : (kRow == 128 ? (k >> 1 & 1) << 2 : 0);
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+          const uint32_t byte = (first + i * 32) * 2 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+          at[i] = k * kRow + (((byte >> 4) ^ turn) << 4) + (byte & 15);
+        }
+      }
+    }
+    __device__ __forceinline__ short8v read(const char* stage, int block, int slice, uint32_t lane) const {
+      if constexpr (ALONG) {
+        const uint32_t q = ((slice * 2 + (lane >> 5)) ^ ((lane & 31) >> 1 & 7)) * 16;
+        return *reinterpret_cast<const short8v*>(stage + at[0] + block * 32 * 128 + q);
+      } else {
+        const char* const from = stage + at[block] + slice * 16 * kRow;
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(from));
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(from + 4 * kRow));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    }
+  };
+};
+
+template <bool F16> __device__ __forceinline__ float16v multiply(short8v a, short8v b, float16v d) {
+  if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), d, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), d, 0, 0, 0);
+}
+
+// TM x TN of the result by WM x WN waves, each (TM / WM) x (TN / WN) in blocks of 32 x 32.  Operands come to the LDS past the registers,
+// STAGES stages of 64 k deep.  Fragments are read one slice of 16 k ahead of the products that use them, across the stage's end too:
+// the barrier in front of the last slice's products tells that the next stage has come and that this one's buffer is free.
+template <int TM, int TN, int WM, int WN, bool ALONG_A, bool ALONG_B, bool F16, int STAGES>
+__global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, DirectArgs d) {
+  constexpr int kWaves = WM * WN, kThreads = kWaves * 64, MB = TM / WM / 32, NB = TN / WN / 32, kSlices = 4;
+  typedef Stages<TM, kWaves, ALONG_A> A;
+  typedef Stages<TN, kWaves, ALONG_B> B;
+  constexpr int kStage = A::kBytes + B::kBytes, kLoads = A::kLoads + B::kLoads;
+  constexpr int kImageRow = TN * 4 + 16, kImageRows = WM * 32, kImage = kImageRow * kImageRows;
+  constexpr int kLds = STAGES * kStage > kImage ? STAGES * kStage : kImage;
+  static_assert(kLds <= 160 * 1024 && (STAGES & (STAGES - 1)) == 0 && STAGES * kLoads < 64, "stages");
+  __shared__ __align__(1024) char lds[kLds];
+  const uint32_t thread = threadIdx.x, lane = thread & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  const uint32_t wm = wave / WN, wn = wave % WN;
+
+  // four tiles of m by all of n
+  const uint32_t tiles = d.tiles_m * d.tiles_n, tile = tile_of_block(blockIdx.x, gridDim.x, d.run);
+  const uint32_t w = tile / tiles, of_worker = tile - w * tiles, band = 4 * d.tiles_n, group = of_worker / band, in = of_worker - group * band;
+  const uint32_t high = d.tiles_m - group * 4 < 4 ? d.tiles_m - group * 4 : 4;
+  const uint32_t m0 = (group * 4 + in % high) * TM, n0 = in / high * TN;
+
+  const uint32_t deep = (a.k + 63) / 64, all = deep * d.segments;
+  const uint32_t s0 = static_cast<uint32_t>(static_cast<uint64_t>(all) * blockIdx.y / d.splits);
+  const uint32_t stages = static_cast<uint32_t>(static_cast<uint64_t>(all) * (blockIdx.y + 1) / d.splits) - s0;
+  A of_a;
+  B of_b;
+  of_a.open(d.a, w * d.a_worker, d.a_ld, d.a_part, m0, a.m, lane, wave);
+  of_b.open(d.b, w * d.b_worker, d.b_ld, d.b_part, n0, a.n, lane, wave);
+  uint32_t segment = s0 / deep, stage_k = s0 - segment * deep, asked = 0;
+  const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_memory char*)lds));
+  auto ask = [&] {
+    const uint32_t to = lds_at + (asked & (STAGES - 1)) * kStage, k_left = a.k - stage_k * 64;
+    of_a.ask(d.a_parts >> segment * 2 & 3, stage_k, k_left, to, wave);
+    of_b.ask(d.b_parts >> segment * 2 & 3, stage_k, k_left, to + A::kBytes, wave);
+    ++asked;
+    if (++stage_k == deep) {
+      stage_k = 0;
+      ++segment;
+    }
+  };
+  typename A::template Reader<MB> read_a;
+  typename B::template Reader<NB> read_b;
+  read_a.open(wm * (TM / WM), lane);
+  read_b.open(wn * (TN / WN), lane);
+  struct Fragments { short8v a[MB], b[NB]; };
+  auto read = [&](uint32_t stage, int slice, Fragments& f) {
+    const char* const from = lds + (stage & (STAGES - 1)) * kStage;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) f.a[i] = read_a.read(from, i, slice, lane);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) f.b[j] = read_b.read(from + A::kBytes, j, slice, lane);
+  };
+  float16v acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  if (stages >= STAGES) {
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) ask();
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * kLoads) : "memory");
+  } else {
+    for (uint32_t i = 0; i < stages; ++i) ask();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  __builtin_amdgcn_s_barrier();
+  Fragments even, odd;
+  read(0, 0, even);
+  // The stages behind the last one that is asked for by themselves, so that nothing in the loop is conditional.
+  auto stage = [&](uint32_t s, auto ask_more, auto read_next) {
+#pragma unroll
+    for (int slice = 0; slice < kSlices; ++slice) {
+      Fragments& now = slice & 1 ? odd : even;
+      Fragments& next = slice & 1 ? even : odd;
+      if (slice + 1 < kSlices) {
+        read(s, slice + 1, next);
+      } else {
+        // the next stage has come, those behind it may be on their way
+        if constexpr (ask_more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        if constexpr (read_next) read(s + 1, 0, next);
+        if constexpr (ask_more) ask();
+      }
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = multiply<F16>(now.b[j], now.a[i], acc[i][j]);
+      // the products of a slice stay behind its reads, which the compiler would put in front of the next barrier
+      if constexpr (TM == 256) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  uint32_t s = 0;
+  for (; s + STAGES < stages; ++s) stage(s, Yes{}, Yes{});
+  for (; s + 1 < stages; ++s) stage(s, No{}, Yes{});
+  stage(s, No{}, No{});
+
+  if constexpr (F16) {
+    const int by = -(d.exponents[2 * w] + d.exponents[2 * w + 1]);
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = ldexpf(acc[i][j][e], by);
+  }
+
+  // Results go through the LDS, 32 rows of every wave at a time, and from there in whole lines.  Block (i, j), element e of a lane:
+  // m = 32 i + lane % 32, n = 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4.
+  const bool eights = ends_in<8>(a);
+  const uint32_t of32 = lane & 31, half = lane >> 5;
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    __syncthreads();
+    char* const mine = lds + (wm * 32 + of32) * kImageRow + (wn * (TN / WN) + half * 4) * 4;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<float4v*>(mine + j * 128 + e * 8) = float4v{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+    __syncthreads();
+    auto row_of = [&](uint32_t row) { return m0 + row / 32 * (TM / WM) + i * 32 + row % 32; };
+    if (d.parts != nullptr || eights) {
+      for (uint32_t v = thread; v < kImageRows * (TN / 8); v += kThreads) {
+        const uint32_t row = v / (TN / 8), col = v % (TN / 8) * 8, m = row_of(row), n = n0 + col;
+        if (m >= a.m || n >= a.n) continue;
+        const float4v* const from = reinterpret_cast<const float4v*>(lds + row * kImageRow + col * 4);
+        const float4v lo = from[0], hi = from[1];
+        if (d.parts != nullptr) {
+          float4v* const to = reinterpret_cast<float4v*>(d.parts + ((static_cast<uint64_t>(blockIdx.y) * a.W + w) * a.m + m) * d.parts_ld + n);
+          to[0] = lo;
+          to[1] = hi;
+          continue;
+        }
+        float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        if (n + 8 <= a.n) {
+          finish<8>(a, w, m, n, x);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (n + e < a.n) finish<1>(a, w, m, n + e, x + e);
+        }
+      }
+    } else {
+      for (uint32_t v = thread; v < kImageRows * TN; v += kThreads) {
+        const uint32_t row = v / TN, col = v % TN, m = row_of(row), n = n0 + col;
+        if (m >= a.m || n >= a.n) continue;
+        float x = *reinterpret_cast<const float*>(lds + row * kImageRow + col * 4);
+        finish<1>(a, w, m, n, &x);
+      }
+    }
+  }
+}
+
+// The parts of a product whose k is shared out, in their order, and its end: a thread takes eight neighbouring numbers.
+__global__ __launch_bounds__(256) void product_join(ProductArgs a, DirectArgs d) {
+  const uint32_t wide = (a.n + 7) / 8;
+  const uint64_t v = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x, rows = static_cast<uint64_t>(a.W) * a.m;
+  if (v >= rows * wide) return;
+  const uint64_t row = v / wide, w = row / a.m;
+  const uint32_t n = static_cast<uint32_t>(v - row * wide) * 8, m = static_cast<uint32_t>(row - w * a.m);
+  float x[8] = {};
+  const float* const from = d.parts + row * d.parts_ld + n;
+#pragma unroll 4
+  for (uint32_t s = 0; s < d.splits; ++s) {
+    float part[8];
+    Stored<float, 8>::load(from + s * rows * d.parts_ld, part);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] += part[e];
+  }
+  if (n + 8 <= a.n && ends_in<8>(a)) {
+    finish<8>(a, w, m, n, x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (n + e < a.n) finish<1>(a, w, m, n + e, x + e);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Operands as large products take them
+// ---------------------------------------------------------------------------
+
+// The largest finite number of an operand, or of what one of kPackParts workgroups takes of it.
+__global__ __launch_bounds__(256) void product_largest(PackArgs p) {
+  const PackOperand& o = p.operand[blockIdx.z];
+  if (o.out == nullptr) return;
+  const int64_t w = blockIdx.y, numbers = static_cast<int64_t>(o.rows) * o.wide;
+  float most = 0.f;
+  auto take = [&](float v) {
+    v = fabsf(v);
+    most = v < __builtin_inff() ? fmaxf(most, v) : most;
+  };
+  const int64_t at = w * o.worker_stride;
+  const bool vectors = o.eights && ((o.worker_stride | o.ld | o.wide) & 7) == 0;
+  if (vectors) {
+    for (int64_t v = blockIdx.x * 256 + threadIdx.x; v < numbers / 8; v += kPackParts * 256) {
+      const int64_t row = v * 8 / o.wide, col = v * 8 - row * o.wide;
+      float x[8];
+      load_numbers<8>(o.p, at + row * o.ld + col, o.bf16, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) take(x[e]);
+    }
+  } else {
+    for (int64_t v = blockIdx.x * 256 + threadIdx.x; v < numbers; v += kPackParts * 256) {
+      const int64_t row = v / o.wide, col = v - row * o.wide;
+      float x;
+      load_numbers<1>(o.p, at + row * o.ld + col, o.bf16, &x);
+      take(x);
+    }
+  }
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
+  __shared__ float waves[4];
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    p.largest[(w * 2 + blockIdx.z) * kPackParts + blockIdx.x] = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+}
+
+// Rows of `wide` numbers to rows of a multiple of eight, zeros behind their ends: bf16, or one or two binary16 of the numbers times a power
+// of two that takes the largest of the worker's operand to between 2^14 and 2^15.
+__global__ __launch_bounds__(256) void product_pack(PackArgs p) {
+  const PackOperand& o = p.operand[blockIdx.z];
+  if (o.out == nullptr) return;
+  const int64_t w = blockIdx.y;
+  int by = 0;
+  if (p.f16) {
+    static_assert(kPackParts == 64, "a lane each");
+    float most = p.largest[(w * 2 + blockIdx.z) * kPackParts + (threadIdx.x & 63)];
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
+    if (most > 0.f) {
+      int power;
+      (void)frexpf(most, &power);      // most = 0.5 to 1 times 2^power
+      by = 15 - power;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.exponents[w * 2 + blockIdx.z] = by;
+  }
+  const uint32_t vectors = static_cast<uint32_t>((o.wide + 7) / 8);
+  const int64_t all = static_cast<int64_t>(o.rows) * vectors;
+  const bool whole = o.eights && ((o.worker_stride | o.ld | o.wide) & 7) == 0;
+  for (int64_t v = blockIdx.x * 256 + threadIdx.x; v < all; v += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t row = v / vectors;
+    const uint32_t col = static_cast<uint32_t>(v - row * vectors) * 8;
+    const int64_t from = w * o.worker_stride + row * o.ld + col;
+    float x[8];
+    if (whole) {
+      load_numbers<8>(o.p, from, o.bf16, x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = 0.f;
+        if (col + e < o.wide) load_numbers<1>(o.p, from + e, o.bf16, x + e);
+      }
+    }
+    uint16_t* const to = static_cast<uint16_t*>(o.out) + (w * o.rows + row) * (vectors * 8ll) + col;
+    ushort8 first, second;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (p.f16) {
+        const float y = ldexpf(x[e], by);
+        const _Float16 high = static_cast<_Float16>(y);
+        first[e] = __builtin_bit_cast(uint16_t, high);
+        second[e] = __builtin_bit_cast(uint16_t, static_cast<_Float16>(y - static_cast<float>(high)));
+      } else {
+        first[e] = narrow(x[e]);
+      }
+    }
+    *reinterpret_cast<ushort8*>(to) = first;
+    if (o.parts == 2) *reinterpret_cast<ushort8*>(to + static_cast<int64_t>(p.W) * o.rows * (vectors * 8ll)) = second;
+  }
+}
+
+}  // namespace
+
+namespace {
+
+int launch_any(const ProductArgs& args, void* stream) {
+  const dim3 grid((args.m + kTile - 1) / kTile * ((args.n + kTile - 1) / kTile), args.W);
+  auto with_layout = [&](auto ta, auto tb, auto pa, auto pb) {
+    typedef decltype(ta) TA;
+    typedef decltype(tb) TB;
+    constexpr int PA = decltype(pa)::value, PB = decltype(pb)::value;
+    if (args.a.along_k) {
+      return args.b.along_k ? enqueue(product_any<TA, TB, true, true, PA, PB>, grid, 256, 0, stream, args)
+                            : enqueue(product_any<TA, TB, true, false, PA, PB>, grid, 256, 0, stream, args);
+    }
+    return enqueue(product_any<TA, TB, false, false, PA, PB>, grid, 256, 0, stream, args);
+  };
+  const uint16_t half = 0;
+  const float whole = 0.f;
+  const Number<1> one;
+  const Number<2> two;
+  const Number<3> three;
+  if (args.a.bf16) {
+    if (args.b.bf16) return with_layout(half, half, one, one);
+    return args.out_bf16 ? with_layout(half, whole, one, two) : with_layout(half, whole, one, three);
+  }
+  if (args.b.bf16) return args.out_bf16 ? with_layout(whole, half, two, one) : with_layout(whole, half, three, one);
+  return args.out_bf16 ? with_layout(whole, whole, two, two) : with_layout(whole, whole, three, three);
+}
+
+}  // namespace
+
+int launch_product(const ProductArgs& args, const ProductPlan& plan, char* room, void* stream) {
+  if (args.m == 0 || args.n == 0) return 0;
+  if (plan.tile == 0) return launch_any(args, stream);
+  DirectArgs d{};
+  PackArgs pack{};
+  pack.f16 = plan.f16;
+  pack.W = args.W;
+  pack.largest = reinterpret_cast<float*>(room + plan.largest_at);
+  pack.exponents = reinterpret_cast<int32_t*>(room + plan.exponents_at);
+  uint64_t most = 0;
+  for (int i = 0; i < 2; ++i) {
+    const Operand& o = i == 0 ? args.a : args.b;
+    const uint32_t size = i == 0 ? args.m : args.n;
+    const void* p = o.p;
+    int64_t worker = o.worker_stride, ld = o.ld, part = 0;
+    if (plan.packed[i]) {
+      PackOperand& to = pack.operand[i];
+      to = {o.p, room + plan.packed_at[i], o.worker_stride, o.ld, o.along_k ? size : args.k, o.along_k ? args.k : size, o.bf16, plan.parts[i],
+            reinterpret_cast<uintptr_t>(o.p) % 16 == 0};
+      p = to.out;
+      ld = (to.wide + 7ll) / 8 * 8;
+      worker = to.rows * ld;
+      part = worker * args.W;
+      most = std::max<uint64_t>(most, to.rows * static_cast<uint64_t>(ld) / 8);
+    }
+    (i == 0 ? d.a : d.b) = p;
+    (i == 0 ? d.a_worker : d.b_worker) = worker;
+    (i == 0 ? d.a_ld : d.b_ld) = ld;
+    (i == 0 ? d.a_part : d.b_part) = part;
+  }
+  if (most > 0) {
+    int st = 0;
+    if (plan.f16) st = enqueue(product_largest, dim3(kPackParts, args.W, 2), 256, 0, stream, pack);
+    if (st == 0) st = enqueue(product_pack, dim3(static_cast<uint32_t>(std::min<uint64_t>((most + 255) / 256, 4096)), args.W, 2), 256, 0, stream, pack);
+    if (st != 0) return st;
+  }
+  // the small products first: low high, high low, high high
+  d.segments = 1;
+  if (plan.parts[0] == 2 && plan.parts[1] == 2) {
+    d.segments = 3;
+    d.a_parts = 1;
+    d.b_parts = 1 << 2;
+  } else if (plan.parts[0] == 2 || plan.parts[1] == 2) {
+    d.segments = 2;
+    (plan.parts[0] == 2 ? d.a_parts : d.b_parts) = 1;
+  }
+  d.exponents = pack.exponents;
+  d.splits = plan.splits;
+  d.parts = plan.splits > 1 ? reinterpret_cast<float*>(room + plan.parts_at) : nullptr;
+  d.parts_ld = (args.n + 7) / 8 * 8;
+  auto tiles = [&](uint32_t tm, uint32_t tn, uint32_t run) {
+    d.tiles_m = (args.m + tm - 1) / tm;
+    d.tiles_n = (args.n + tn - 1) / tn;
+    d.run = run;
+    return dim3(d.tiles_m * d.tiles_n * args.W, d.splits);
+  };
+  const bool aa = args.a.along_k, ab = args.b.along_k;
+  int st;
+#define NOLOCO_PRODUCT(TM, TN, WM, WN, STAGES, AA, AB) \
+  (plan.f16 ? enqueue(product_direct<TM, TN, WM, WN, AA, AB, true, STAGES>, grid, WM * WN * 64, 0, stream, args, d) \
+            : enqueue(product_direct<TM, TN, WM, WN, AA, AB, false, STAGES>, grid, WM * WN * 64, 0, stream, args, d))
+  if (plan.tile == 256) {
+    const dim3 grid = tiles(256, 256, 32);
+    st = !aa ? NOLOCO_PRODUCT(256, 256, 2, 4, 2, false, false) : (ab ? NOLOCO_PRODUCT(256, 256, 2, 4, 2, true, true) : NOLOCO_PRODUCT(256, 256, 2, 4, 2, true, false));
+  } else if (plan.tile == 128) {
+    const dim3 grid = tiles(128, 128, 64);
+    st = !aa ? NOLOCO_PRODUCT(128, 128, 2, 2, 2, false, false) : (ab ? NOLOCO_PRODUCT(128, 128, 2, 2, 2, true, true) : NOLOCO_PRODUCT(128, 128, 2, 2, 2, true, false));
+  } else {
+    const dim3 grid = tiles(32, 256, 64);
+    st = ab ? NOLOCO_PRODUCT(32, 256, 1, 4, 4, true, true) : NOLOCO_PRODUCT(32, 256, 1, 4, 4, true, false);
+  }
+#undef NOLOCO_PRODUCT
+  if (st != 0 || d.splits == 1) return st;
+  const uint64_t vectors = static_cast<uint64_t>(args.W) * args.m * ((args.n + 7) / 8);
+  return enqueue(product_join, dim3(static_cast<uint32_t>((vectors + 255) / 256)), 256, 0, stream, args, d);
+}
+
+}  // namespace noloco

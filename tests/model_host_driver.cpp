@@ -44,7 +44,31 @@ int launch_layer_norm_gradient(const NormArgs& a, void*) {
   EXPECT(a.groups >= 1 && inside(a.partial, uint64_t(a.W) * a.groups * 2 * a.width * 4));
   return launch();
 }
-int launch_product(const ProductArgs& a, void*) { products.push_back(a); return launch(); }
+int launch_product(const ProductArgs& a, const ProductPlan& p, char* at, void*) {
+  products.push_back(a);
+  EXPECT(inside(at, p.bytes));
+  EXPECT(p.splits >= 1 && p.splits <= 32 && (p.tile == 0 || p.tile == 32 || p.tile == 128 || p.tile == 256));
+  const uint64_t sizes[2] = {a.m, a.n};
+  uint64_t end = 0;
+  for (int i = 0; i < 2; ++i) {
+    const Operand& o = i == 0 ? a.a : a.b;
+    if (p.tile == 0) continue;
+    const uint64_t rows = o.along_k ? sizes[i] : a.k, wide = ((o.along_k ? a.k : sizes[i]) + 7) / 8 * 8;
+    EXPECT(p.packed[i] || (o.bf16 && o.ld % 8 == 0 && o.worker_stride % 8 == 0 && reinterpret_cast<uint64_t>(o.p) % 16 == 0 && (!o.along_k || a.k % 8 == 0)));
+    EXPECT(!p.packed[i] || p.packed_at[i] >= end);
+    if (p.packed[i]) end = p.packed_at[i] + uint64_t(a.W) * rows * wide * 2 * p.parts[i];
+  }
+  if (p.f16) {
+    EXPECT(p.largest_at >= end && p.exponents_at >= p.largest_at + uint64_t(a.W) * 2 * kPackParts * 4);
+    end = p.exponents_at + uint64_t(a.W) * 8;
+  }
+  if (p.splits > 1) {
+    EXPECT(p.parts_at >= end && p.splits <= (uint64_t(a.k) + 63) / 64 * (p.parts[0] + p.parts[1] - 1));
+    end = p.parts_at + p.splits * uint64_t(a.W) * a.m * ((a.n + 7) / 8 * 8) * 4;
+  }
+  EXPECT(end <= p.bytes);
+  return launch();
+}
 int launch_slope(const SlopeArgs& a, void*) {
   slopes.push_back(a);
   const uint64_t numbers = uint64_t(a.W) * a.tokens * a.outputs * (a.dz_bf16 ? 2 : 4), sums = uint64_t(a.W) * a.groups * a.outputs * 4;
@@ -133,8 +157,15 @@ static int matrices() {
       const noloco_linear_layer& l = given[layer];
       products.clear();
       CHECK(noloco_linear(plan, layer, at(1), t[0], at(2), t[1], T, act, nullptr, at(7), at(3), t[2], nullptr) == NOLOCO_OK);
-      CHECK(products.size() == (T > 0 ? 1u : 0u));
-      if (T > 0) CHECK(products[0].m == T && products[0].n == l.outputs && products[0].k == l.inputs && products[0].W == 7 && products[0].b.along_k == l.transposed);
+      int64_t of_out = 0;
+      for (const ProductArgs& p : products) {
+        CHECK(p.m == T && p.n == l.outputs && p.k == l.inputs && p.b.along_k == l.transposed);
+        CHECK(p.out == at(3) + of_out * T * l.outputs * (t[2] ? 2 : 4) && p.before == at(7) + of_out * T * l.outputs * (t[2] ? 2 : 4));
+        CHECK(p.a.p == at(1) + of_out * T * l.inputs * (t[0] ? 2 : 4) && p.b.p == at(2) + (l.offset + of_out * 150016) * (t[1] ? 2 : 4));
+        CHECK(l.bias < 0 || p.bias == at(2) + (l.bias + of_out * 150016) * (t[1] ? 2 : 4));
+        of_out += p.W;
+      }
+      CHECK(of_out == (T > 0 ? 7 : 0));
       products.clear();
       slopes.clear();
       const bool dx = gen() & 1, grad = gen() & 1;

@@ -90,15 +90,21 @@ def off_activation(z):
 
 def product(a, b, out_dtype):
     """(a @ b, bound) for a [.., m, k], b [.., k, n] as they are stored. A bf16 result: float operands are rounded to bf16. A float
-    one: three parts a float operand, of which products of 2^-24 are left out, and as many additions as there are products."""
+    one: three bf16 a float operand, of whose products those of 2^-24 are left out, or two binary16 (2^-22 of a number, or 2^-40 of
+    its worker's largest), of whose products that of the low halves, 2^-22, is left out; as many additions as there are products."""
     sizes = a.double().abs() @ b.double().abs()
     floats = [t.dtype == torch.float32 for t in (a, b)]
     k = a.shape[-1]
     if out_dtype == torch.bfloat16:
         rel = sum(STORED[torch.bfloat16] for f in floats if f) * SLACK + (k + 4) * U
+        least = 0.0
     else:
-        rel = ({0: 1, 1: 3, 2: 6}[sum(floats)] * k + 4) * U + (4 * U if all(floats) else 0)
-    return a.double() @ b.double(), rel * sizes * SLACK + TINY * k
+        rel = ({0: 1, 1: 3, 2: 6}[sum(floats)] * k + 4) * U + 4 * U * sum(floats) + (4 * U if all(floats) else 0)
+        least = 0.0
+        if any(floats):
+            largest = [t.double().abs().amax((-2, -1), keepdim=True) for t in (a, b)]
+            least = 2.0 ** -40 * (largest[0] * b.double().abs().sum(-2, keepdim=True) + largest[1] * a.double().abs().sum(-1, keepdim=True))
+    return a.double() @ b.double(), (rel * sizes + least) * SLACK + TINY * k
 
 
 def linear(x, matrix, bias, act, residual, out_dtype):
@@ -116,7 +122,7 @@ def linear(x, matrix, bias, act, residual, out_dtype):
 
 def linear_gradient(dout, x, matrix, before, act, add, dx_dtype, grad_dtype):
     """((dx, bound), (matrix's gradient, bound), (bias's, bound))"""
-    dz, off = dout.double(), torch.zeros(())
+    dz, off = dout.double(), torch.zeros((), dtype=torch.float64)
     if act != "none":
         slope = activation(act, before.double())[1]
         dz = dz * slope
@@ -128,14 +134,11 @@ def linear_gradient(dout, x, matrix, before, act, add, dx_dtype, grad_dtype):
         pair = [a, b]
         pair[which] = dz
         exact = pair[0].double() @ pair[1].double()
-        pair[which] = kept
-        types = [t.dtype for t in pair]
-        sized = [t.double().abs() for t in (dz if which == 0 else a, dz if which == 1 else b)]
-        rel = product(torch.ones((1, sized[0].shape[-1]), dtype=types[0]), torch.ones((sized[0].shape[-1], 1), dtype=types[1]), out_dtype)[1]
-        bound = (sized[0] @ sized[1]) * (rel / sized[0].shape[-1]).item()
-        offs = [sized[0], sized[1]]
+        pair[which] = dz.to(kept.dtype)           # off by a rounding of binary32 at most, which `off` has
+        bound = product(*pair, out_dtype)[1]
+        offs = [t.double().abs() for t in pair]
         offs[which] = off.expand_as(dz)
-        return exact, bound + offs[0].double() @ offs[1].double() + TINY
+        return exact, bound * SLACK + offs[0] @ offs[1] + TINY
 
     dx, dx_bound = through(dout, matrix.mT, 0, dx_dtype)
     if add is not None:

@@ -208,10 +208,59 @@ def test_gradient_through_activations(act, types, accumulate, with_add):
     check_gradient((2, 70, 40, 72, {}), types, act, with_add, accumulate)
 
 
+# Large products: what is packed and what is not, every tile, k shared out, edges within a tile, a stage and a vector.
+LARGE = [  # W, T, inputs, outputs, more of Layer
+    (1, 1, 16392, 16408, {}), (2, 20, 2600, 2704, dict(transposed=True)), (1, 31, 3001, 2999, {}), (1, 300, 1000, 1000, dict(gap=1)), (1, 520, 712, 776, {}),
+    (2, 130, 1064, 1048, dict(transposed=True, apart=8)), (4, 2041, 72, 2056, {}), (1, 4099, 4100, 64, dict(bias=False)), (1, 64, 2056, 2072, {}),
+    (3, 333, 515, 517, dict(transposed=True)),
+]
+
+
+@pytest.mark.parametrize("types", TYPES, ids=str)
+@pytest.mark.parametrize("size", LARGE, ids=str)
+def test_large_linear(size, types):
+    check_forward(size, types, "none" if size[1] % 2 else "gelu", with_residual=size[1] % 2 == 0)
+
+
+@pytest.mark.parametrize("types", [("f32", "f32", "f32", "f32", "f32"), ("bf16", "bf16", "f32", "bf16", "f32"), ("bf16", "bf16", "bf16", "bf16", "bf16")], ids=str)
+@pytest.mark.parametrize("size", LARGE, ids=str)
+def test_large_gradient(size, types):
+    check_gradient(size, types, "none" if size[1] % 2 else "silu", with_add=size[1] % 2 == 0, accumulate=size[2] % 2 == 0)
+
+
+@pytest.mark.parametrize("types", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f32", "f32", "bf16")], ids=str)
+def test_large_products_keep_bad_numbers_to_their_row_and_column(types):
+    layer = Layer(2, 712, 776)
+    x, theta, out = (DTYPES[t] for t in types)
+    a, x = layer.array(theta), randn((2, 300, 712), 2, x)
+    x[0, 7, 3] = math.nan
+    x[1, 299, 711] = math.inf
+    layer.matrix(a)[0, 711, 775] = math.nan
+    got, _ = forward(layer, layer.plan(300), x, a, "none", None, out)
+    bad = torch.zeros(got.shape, dtype=torch.bool)
+    bad[0, 7] = bad[1, 299] = True
+    bad[0, :, 775] = True
+    assert not got[bad].isfinite().any() and got[~bad].isfinite().all()
+
+
+def test_large_products_of_any_size():
+    """Float operands of every size that binary32 has room for, and of sizes that lie far apart."""
+    layer = Layer(1, 712, 776, bias=False)
+    for size in (1e-15, 1e15):
+        a, x = layer.array(torch.float32) * size, randn((1, 520, 712), 2) * size
+        x[:, ::3] *= 1e-3
+        got, _ = forward(layer, layer.plan(520), x, a, "none", None, torch.float32)
+        within(got, *plain.product(x, layer.matrix(a), torch.float32))
+    zero, _ = forward(layer, layer.plan(520), torch.zeros((1, 520, 712)), a, "none", None, torch.float32)
+    assert (zero == 0).all()
+
+
 def test_gradient_in_batches_of_workers():
     """A workspace that has room for one worker, or for two of five."""
     check_gradient((5, 70, 40, 72, {}), GRADIENT_TYPES[0], "gelu", True, True, room=1)
-    check_gradient((5, 70, 40, 72, {}), GRADIENT_TYPES[1], "silu", True, False, room=2 * (70 * 72 * 4 + 4096))
+    check_gradient((5, 70, 40, 72, {}), GRADIENT_TYPES[1], "silu", True, False, room=4 * (70 * 72 * 4 + 4096))
+    check_gradient((5, 300, 520, 456, {}), GRADIENT_TYPES[0], "gelu", True, False, room=1)
+    check_gradient((5, 300, 520, 456, {}), GRADIENT_TYPES[1], "gelu", True, False, room=8 << 20)
 
 
 def test_gradient_of_activations_is_that_of_differences():
