@@ -77,11 +77,25 @@ template <int N> __device__ __forceinline__ void store_numbers(void* p, int64_t 
   else Stored<float, N>::store(static_cast<float*>(p) + at, v);
 }
 
-// Sums over the lanes of a wave, the same in all of them.
+// Sums and largest numbers over the lanes of a wave, the same in all of them: within sixteen lanes by moves between lanes (pairs,
+// fours, eights mirrored, sixteens mirrored), then over the four sixteens.  Through the LDS (__shfl_xor) a sum is six round trips.
+template <int CONTROL> __device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 15, 15, true));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  v += moved<0xB1>(v);
+  v += moved<0x4E>(v);
+  v += moved<0x141>(v);
+  v += moved<0x140>(v);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+__device__ __forceinline__ float wave_largest(float v) {
+  v = fmaxf(v, moved<0xB1>(v));
+  v = fmaxf(v, moved<0x4E>(v));
+  v = fmaxf(v, moved<0x141>(v));
+  v = fmaxf(v, moved<0x140>(v));
+  return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
 }
 
 // v[0], v[1] summed over the workgroup's L threads (a wave, or whole waves: then `shared` has 2 * L / 64 floats and is free

@@ -47,7 +47,41 @@ template <int N, int K, int L> struct Row {
   }
 };
 
-template <int N, int K, int L>
+// A row on its way: as it lies in memory, so that nobody waits for it before it is widened.  Where types differ (E is void) it is
+// widened as it comes.
+template <typename E, int N, int K, int L> struct Coming {
+  static constexpr int kVector = Stored<E, N>::kVector;
+  typedef E vector __attribute__((ext_vector_type(kVector)));
+  vector raw[K][N / kVector];
+  __device__ __forceinline__ void ask(const void* p, int64_t at, bool, uint32_t lane, uint32_t width) {
+    const E* const from = static_cast<const E*>(p) + at;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!Row<N, K, L>::there(lane, k, width)) continue;
+#pragma unroll
+      for (int i = 0; i < N / kVector; ++i) raw[k][i] = *reinterpret_cast<const vector*>(from + (lane + k * L) * N + i * kVector);
+    }
+  }
+  // The row as numbers; zeros where the thread has none.
+  __device__ __forceinline__ void take(Row<N, K, L>& row, uint32_t lane, uint32_t width) const {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        float x;
+        if constexpr (sizeof(E) == 2) x = widen(raw[k][i / kVector][i % kVector]); else x = raw[k][i / kVector][i % kVector];
+        row.v[k * N + i] = Row<N, K, L>::there(lane, k, width) ? x : 0.f;
+      }
+  }
+};
+template <int N, int K, int L> struct Coming<void, N, K, L> {
+  Row<N, K, L> row;
+  __device__ __forceinline__ void ask(const void* p, int64_t at, bool bf16, uint32_t lane, uint32_t width) { row.load(p, at, bf16, lane, width); }
+  __device__ __forceinline__ void take(Row<N, K, L>& to, uint32_t, uint32_t) const { to = row; }
+};
+
+// E: the type of x and out (and of dout), or void.
+template <typename E, int N, int K, int L>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void layer_norm_held(NormArgs a) {
   typedef Row<N, K, L> R;
   constexpr uint32_t kThreads = L < 256 ? 256 : L, kRows = kThreads / L;
@@ -57,7 +91,8 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void layer_norm_held(NormArgs a)
   int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / L;
   if (t >= a.tokens) return;              // whole waves, and whole workgroups where these hold a row
   R weight, bias, x;
-  x.load(a.x, (first + t) * width, a.x_bf16, lane, width);
+  Coming<E, N, K, L> coming;
+  coming.ask(a.x, (first + t) * width, a.x_bf16, lane, width);
   weight.load(a.theta, w * a.stride + a.weight, a.theta_bf16, lane, width);
   if (a.bias >= 0) {
     bias.load(a.theta, w * a.stride + a.bias, a.theta_bf16, lane, width);
@@ -67,8 +102,8 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void layer_norm_held(NormArgs a)
   }
   const float count = static_cast<float>(width);
   for (; t < a.tokens; t += step) {
-    R next;
-    if (t + step < a.tokens) next.load(a.x, (first + t + step) * width, a.x_bf16, lane, width);
+    coming.take(x, lane, width);
+    if (t + step < a.tokens) coming.ask(a.x, (first + t + step) * width, a.x_bf16, lane, width);
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < R::kNumbers; ++i) sum += x.v[i];
@@ -92,7 +127,6 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void layer_norm_held(NormArgs a)
       a.stats[(first + t) * 2] = mean;
       a.stats[(first + t) * 2 + 1] = rstd;
     }
-    x = next;
   }
 }
 
@@ -132,7 +166,7 @@ __global__ __launch_bounds__(1024) void layer_norm_wide(NormArgs a) {
   }
 }
 
-template <int N, int K, int L>
+template <typename E, int N, int K, int L>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void layer_norm_gradient_held(NormArgs a) {
   typedef Row<N, K, L> R;
   constexpr uint32_t kThreads = L < 256 ? 256 : L, kRows = kThreads / L;
@@ -145,25 +179,37 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void layer_norm_gradient_held(No
   for (int i = 0; i < R::kNumbers; ++i) of_weight.v[i] = of_bias.v[i] = 0.f;
   const float count = static_cast<float>(width);
   int turn = 0;
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + sub; t < a.tokens; t += step) {
+  Coming<E, N, K, L> coming_x, coming_d, coming_add;
+  float mean = 0.f, rstd = 0.f;
+  auto ask = [&](int64_t t) {
     const int64_t at = (first + t) * width;
+    coming_x.ask(a.x, at, a.x_bf16, lane, width);
+    coming_d.ask(a.dout, at, a.dout_bf16, lane, width);
+    if (a.add != nullptr) coming_add.ask(a.add, at, a.out_bf16, lane, width);
+    mean = a.stats[(first + t) * 2];
+    rstd = a.stats[(first + t) * 2 + 1];
+  };
+  int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + sub;
+  if (t < a.tokens) ask(t);
+  for (; t < a.tokens; t += step) {
     R x, d, add;
-    x.load(a.x, at, a.x_bf16, lane, width);
-    d.load(a.dout, at, a.dout_bf16, lane, width);
+    coming_x.take(x, lane, width);
+    coming_d.take(d, lane, width);
     if (a.add != nullptr) {
-      add.load(a.add, at, a.out_bf16, lane, width);
+      coming_add.take(add, lane, width);
     } else {
 #pragma unroll
       for (int i = 0; i < R::kNumbers; ++i) add.v[i] = 0.f;
     }
-    const float mean = a.stats[(first + t) * 2], rstd = a.stats[(first + t) * 2 + 1];
+    const float mine = mean, scale = rstd;
+    if (t + step < a.tokens) ask(t + step);
     float sums[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int e = k * N + i;
-        x.v[e] = R::there(lane, k, width) ? (x.v[e] - mean) * rstd : 0.f;
+        x.v[e] = R::there(lane, k, width) ? (x.v[e] - mine) * scale : 0.f;
         of_weight.v[e] += d.v[e] * x.v[e];
         of_bias.v[e] += d.v[e];
         d.v[e] *= weight.v[e];
@@ -175,8 +221,8 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void layer_norm_gradient_held(No
     sums[0] /= count;
     sums[1] /= count;
 #pragma unroll
-    for (int i = 0; i < R::kNumbers; ++i) x.v[i] = add.v[i] + rstd * (d.v[i] - sums[0] - x.v[i] * sums[1]);
-    x.store(a.out, at, a.out_bf16, lane, width);
+    for (int i = 0; i < R::kNumbers; ++i) x.v[i] = add.v[i] + scale * (d.v[i] - sums[0] - x.v[i] * sums[1]);
+    x.store(a.out, (first + t) * width, a.out_bf16, lane, width);
   }
   if (a.grad == nullptr) return;
   // The workgroup's rows together, in their order.
@@ -313,11 +359,15 @@ template <int MOST, typename Launch> int with_shape(const NormArgs& a, const Lau
 }  // namespace
 
 int launch_layer_norm(const NormArgs& args, void* stream) {
-  const dim3 grid(args.groups, args.W);
+  // eight workgroups of 256 threads a CU, which take as many rows each as there are
+  const int64_t rows = args.width <= 1024 ? 4 : 1, most = std::max<int64_t>(1, (args.width > 4096 ? 512 : 2048) / args.W);
+  const dim3 grid(static_cast<uint32_t>(std::min((args.tokens + rows - 1) / rows, most)), args.W);
   if (args.width > kNormHeld) return enqueue(layer_norm_wide, grid, 1024, 0, stream, args);
   return with_shape<16>(args, [&](auto n, auto k, auto threads) {
     constexpr int N = decltype(n)::value, K = decltype(k)::value, L = decltype(threads)::value;
-    return enqueue(layer_norm_held<N, K, L>, grid, L < 256 ? 256 : L, 0, stream, args);
+    auto with = [&](auto kernel) { return enqueue(kernel, grid, L < 256 ? 256 : L, 0, stream, args); };
+    if (args.x_bf16 != args.out_bf16) return with(layer_norm_held<void, N, K, L>);
+    return args.x_bf16 ? with(layer_norm_held<uint16_t, N, K, L>) : with(layer_norm_held<float, N, K, L>);
   });
 }
 
@@ -332,7 +382,9 @@ int launch_layer_norm_gradient(const NormArgs& args, void* stream) {
     } else {
       st = with_shape<8>(args, [&](auto n, auto k, auto threads) {
         constexpr int N = decltype(n)::value, K = decltype(k)::value, L = decltype(threads)::value;
-        return enqueue(layer_norm_gradient_held<N, K, L>, grid, L < 256 ? 256 : L, 0, stream, args);
+        auto with = [&](auto kernel) { return enqueue(kernel, grid, L < 256 ? 256 : L, 0, stream, args); };
+        if (args.x_bf16 != args.out_bf16 || args.x_bf16 != args.dout_bf16) return with(layer_norm_gradient_held<void, N, K, L>);
+        return args.x_bf16 ? with(layer_norm_gradient_held<uint16_t, N, K, L>) : with(layer_norm_gradient_held<float, N, K, L>);
       });
     }
     if (st != 0) return st;

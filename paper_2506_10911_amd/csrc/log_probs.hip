@@ -59,8 +59,8 @@ __device__ __forceinline__ RowEnd finish_row(const LogProbArgs& a, int64_t row, 
   return end;
 }
 
-// L threads take a part of a row; where that is a wave, four waves take four rows.
-template <typename E, int L, bool TOP>
+// L threads take a part of a row; where that is a wave, four waves take four rows.  SPREAD: the entropy is asked for.
+template <typename E, int L, bool TOP, bool SPREAD>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs a) {
   constexpr int V = 16 / sizeof(E);          // logits of a load
   constexpr int kAhead = 4;                  // loads of a thread on their way
@@ -81,8 +81,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
     }
   };
   auto largest_of_all = [&](float v, float* room) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    v = wave_largest(v);
     if constexpr (L > 64) {
       if (lane == 0) room[threadIdx.x >> 6] = v;
       __syncthreads();
@@ -115,7 +114,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
       for (int i = 1; i < kN; ++i) most = fmaxf(most, v[i]);
       if (__builtin_amdgcn_ballot_w64(most > reference + kFollow) != 0) {
         const float next = fmaxf(reference, most), by = exp_of(reference - next);
-        spread = by > 0.f && sum > 0.f ? by * (spread + (next - reference) * sum) : 0.f;     // the distance may be infinite
+        if constexpr (SPREAD) spread = by > 0.f && sum > 0.f ? by * (spread + (next - reference) * sum) : 0.f;     // the distance may be infinite
         sum *= by;
         reference = next;
       }
@@ -127,7 +126,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
       for (int i = 0; i < kN; ++i) {
         const float d = v[i] - reference, e = exp_of(d);
         sum += e;
-        spread -= e > 0.f ? e * d : 0.f;
+        if constexpr (SPREAD) spread -= e > 0.f ? e * d : 0.f;
       }
     };
     if (__builtin_amdgcn_ballot_w64(in_head) != 0) {
@@ -147,7 +146,8 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
         }
       }
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) take(v[k], Number<V>{}, first + k * L + at + 1);
+      for (int k = 0; k < kAhead; ++k)
+        if (first + k * L + (at & ~63u) < vectors) take(v[k], Number<V>{}, first + k * L + at + 1);
     }
     if (__builtin_amdgcn_ballot_w64(in_tail) != 0) {
       const float v = in_tail ? single(tail + at) : -kInfinity;
@@ -284,14 +284,15 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
 }
 
 // A row's parts together, a wave a row: the first part that has the largest logit gives its rest, the others all of their sum.
+constexpr uint32_t kJoinKeys = 4096;
 __global__ __launch_bounds__(64) void log_probs_join(LogProbArgs a) {
+  __shared__ uint64_t near[kJoinKeys];
   const uint32_t lane = threadIdx.x;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const LogPart* const parts = a.parts + row * a.num_parts;
     float largest = -kInfinity;
     for (uint32_t i = lane; i < a.num_parts; i += 64) largest = fmaxf(largest, parts[i].largest);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
+    largest = wave_largest(largest);
     uint32_t owner = ~0u;
     for (uint32_t i = lane; i < a.num_parts; i += 64)
       if (parts[i].largest == largest) { owner = i; break; }
@@ -312,7 +313,13 @@ __global__ __launch_bounds__(64) void log_probs_join(LogProbArgs a) {
     spread = wave_sum(spread);
     const RowEnd end = finish_row(a, row, largest, rest, spread, lane == 0);
     const uint32_t top = a.top, all = a.num_parts * top;
-    const uint64_t* const keys = a.keys + row * all;
+    const uint64_t* keys = a.keys + row * all;
+    if (all <= kJoinKeys) {
+      for (uint32_t c = lane; c < all; c += 64) near[c] = keys[c];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+      __builtin_amdgcn_wave_barrier();
+      keys = near;
+    }
     uint32_t real = 0;
     for (uint32_t c = lane; c < all; c += 64) {
       const uint64_t k = keys[c];
@@ -344,45 +351,60 @@ __global__ __launch_bounds__(64) void log_probs_join(LogProbArgs a) {
 
 // A workgroup takes 8192 neighbouring logits of a row, eight of a thread at a time, from a multiple of eight on.
 constexpr uint32_t kGradientPart = 8192;
-template <typename E, typename Out>
+template <typename E, typename Out, bool ENTROPY>
 __global__ __launch_bounds__(256) void log_probs_gradient(LogProbArgs a) {
   constexpr int kAhead = kGradientPart / (256 * 8);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const int64_t begin = row * a.row_stride, first = begin / 8 * 8 + static_cast<int64_t>(blockIdx.y) * kGradientPart;
-    const int64_t end = begin + a.vocab;
-    const int64_t token = token_of(a, row);
-    const float norm = a.norms[row], by = token >= 0 ? a.dlog_probs[row] : 0.f;
-    const float of_entropy = a.dentropy != nullptr ? a.dentropy[row] : 0.f, entropy = a.dentropy != nullptr ? a.entropy[row] : 0.f;
-    const bool nothing = norm == -kInfinity || (token < 0 && a.dentropy == nullptr);
-    const E* const from = static_cast<const E*>(a.logits);
-    Out* const to = static_cast<Out*>(a.dlogits);
-    auto slope = [&](float l, int64_t i) {
+    // places count from the last multiple of eight at or before the row's first logit
+    const int64_t begin = row * a.row_stride, base = begin / 8 * 8;
+    const uint32_t first = static_cast<uint32_t>(begin - base), end = first + a.vocab;
+    const int64_t found = token_of(a, row);
+    const uint32_t token = found >= 0 ? first + static_cast<uint32_t>(found) : ~0u;
+    const float norm = a.norms[row], by = found >= 0 ? a.dlog_probs[row] : 0.f;
+    const float of_entropy = ENTROPY ? a.dentropy[row] : 0.f, entropy = ENTROPY ? a.entropy[row] : 0.f;
+    const bool nothing = norm == -kInfinity || (found < 0 && !ENTROPY);
+    const E* const from = static_cast<const E*>(a.logits) + base;
+    Out* const to = static_cast<Out*>(a.dlogits) + base;
+    auto slope = [&](float l) {
       const float d = l - norm, p = exp_of(d);
       float v = -by * p;
-      if (i == begin + token && token >= 0) v = by * -expm1f(d);
-      if (a.dentropy != nullptr) v -= p > 0.f || p != p ? of_entropy * p * (d + entropy) : 0.f;
-      return nothing ? 0.f : v;
+      if constexpr (ENTROPY) v -= p > 0.f || p != p ? of_entropy * p * (d + entropy) : 0.f;
+      return v;
     };
+    // 1 - p at the token, also where p is next to 1
+    auto at_token = [&](float l) {
+      const float d = l - norm, p = exp_of(d);
+      float v = by * -expm1f(d);
+      if constexpr (ENTROPY) v -= p > 0.f || p != p ? of_entropy * p * (d + entropy) : 0.f;
+      return v;
+    };
+    const uint32_t start = blockIdx.y * kGradientPart + threadIdx.x * 8;
     float v[kAhead][8];
-    int64_t at[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      at[k] = first + (k * 256 + static_cast<int64_t>(threadIdx.x)) * 8;
-      if (!nothing && at[k] >= begin && at[k] + 8 <= end) Stored<E, 8>::load(from + at[k], v[k]);
+      const uint32_t at = start + k * 256 * 8;
+      if (!nothing && at >= first && at + 8 <= end) Stored<E, 8>::load(from + at, v[k]);
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      if (at[k] >= begin && at[k] + 8 <= end) {
+      const uint32_t at = start + k * 256 * 8;
+      if (at >= first && at + 8 <= end) {
+        float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[k][e] = slope(v[k][e], at[k] + e);
-        Stored<Out, 8>::store(to + at[k], v[k]);
-      } else {
-        for (int e = 0; e < 8; ++e) {
-          const int64_t i = at[k] + e;
-          if (i < begin || i >= end) continue;
+        for (int e = 0; e < 8; ++e) x[e] = nothing ? 0.f : slope(v[k][e]);
+        if (!nothing && token - at < 8) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (token - at == e) x[e] = at_token(v[k][e]);
+        }
+        Stored<Out, 8>::store(to + at, x);
+      } else if (at < end) {
+        for (uint32_t i = at < first ? first : at; i < at + 8 && i < end; ++i) {
           float l = 0.f;
-          if (!nothing) Stored<E, 1>::load(from + i, &l);
-          l = slope(l, i);
+          if (!nothing) {
+            Stored<E, 1>::load(from + i, &l);
+            l = i == token ? at_token(l) : slope(l);
+          }
           Stored<Out, 1>::store(to + i, &l);
         }
       }
@@ -392,24 +414,28 @@ __global__ __launch_bounds__(256) void log_probs_gradient(LogProbArgs a) {
 
 constexpr int64_t kMostGroups = 1 << 20;         // workgroups of a launch along the rows
 
-template <typename E, bool TOP> int launch_part(const LogProbArgs& a, void* stream) {
+template <typename E, bool TOP, bool SPREAD> int launch_part(const LogProbArgs& a, void* stream) {
   auto with = [&](auto threads) {
     constexpr int L = decltype(threads)::value;
     constexpr int64_t kRows = L == 64 ? 4 : 1;
     const dim3 grid(static_cast<uint32_t>(std::min((a.rows + kRows - 1) / kRows, kMostGroups)), a.num_parts);
-    return enqueue(log_probs_part<E, L, TOP>, grid, L < 256 ? 256 : L, 0, stream, a);
+    return enqueue(log_probs_part<E, L, TOP, SPREAD>, grid, L < 256 ? 256 : L, 0, stream, a);
   };
   if (a.part <= 1024) return with(Number<64>{});
-  return a.part <= 16384 ? with(Number<256>{}) : with(Number<1024>{});
+  // candidates are kept for 64 logits a thread; without them a workgroup of 256 threads has fewer sums to join
+  return !TOP || a.part <= 16384 ? with(Number<256>{}) : with(Number<1024>{});
 }
 
 }  // namespace
 
 int launch_log_probs(const LogProbArgs& args, void* stream) {
   const bool top = args.top > 0;
-  int st;
-  if (args.logits_bf16) st = top ? launch_part<uint16_t, true>(args, stream) : launch_part<uint16_t, false>(args, stream);
-  else st = top ? launch_part<float, true>(args, stream) : launch_part<float, false>(args, stream);
+  auto with = [&](auto e) {
+    typedef decltype(e) E;
+    if (args.entropy != nullptr) return top ? launch_part<E, true, true>(args, stream) : launch_part<E, false, true>(args, stream);
+    return top ? launch_part<E, true, false>(args, stream) : launch_part<E, false, false>(args, stream);
+  };
+  const int st = args.logits_bf16 ? with(uint16_t{}) : with(float{});
   if (st != 0 || args.num_parts == 1) return st;
   return enqueue(log_probs_join, dim3(static_cast<uint32_t>(std::min(args.rows, kMostGroups))), 64, 0, stream, args);
 }
@@ -417,11 +443,14 @@ int launch_log_probs(const LogProbArgs& args, void* stream) {
 int launch_log_probs_gradient(const LogProbArgs& args, void* stream) {
   // a row that begins within a vector of eight may need a part more
   const dim3 grid(static_cast<uint32_t>(std::min(args.rows, kMostGroups)), (args.vocab + 7 + kGradientPart - 1) / kGradientPart);
-  if (args.logits_bf16)
-    return args.dlogits_bf16 ? enqueue(log_probs_gradient<uint16_t, uint16_t>, grid, 256, 0, stream, args)
-                             : enqueue(log_probs_gradient<uint16_t, float>, grid, 256, 0, stream, args);
-  return args.dlogits_bf16 ? enqueue(log_probs_gradient<float, uint16_t>, grid, 256, 0, stream, args)
-                           : enqueue(log_probs_gradient<float, float>, grid, 256, 0, stream, args);
+  auto with = [&](auto e, auto out) {
+    typedef decltype(e) E;
+    typedef decltype(out) Out;
+    return args.dentropy != nullptr ? enqueue(log_probs_gradient<E, Out, true>, grid, 256, 0, stream, args)
+                                    : enqueue(log_probs_gradient<E, Out, false>, grid, 256, 0, stream, args);
+  };
+  if (args.logits_bf16) return args.dlogits_bf16 ? with(uint16_t{}, uint16_t{}) : with(uint16_t{}, float{});
+  return args.dlogits_bf16 ? with(float{}, uint16_t{}) : with(float{}, float{});
 }
 
 }  // namespace noloco

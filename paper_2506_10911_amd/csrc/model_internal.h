@@ -69,11 +69,11 @@ struct ProductArgs {
   void* before;               // the same
 };
 
-constexpr double kSmallWork = double(1 << 28);  // multiplications of all workers that make a product a large one
+constexpr double kSmallWork = double(1 << 28);  // multiplications of all workers up to which dz stays in binary32
 
 // How a product goes out, by its sizes and types alone (but for the alignment of its operands).  Offsets are into the workspace.
 struct ProductPlan {
-  int32_t tile;               // 0: product_any, 256, 128, or 32 (32 x 256)
+  int32_t tile;               // 0: product_small, 256, 128, or 32 (32 x 256)
   int32_t f16;                // operands packed to binary16 times powers of two
   int32_t packed[2], parts[2];
   uint32_t splits;            // parts that k is shared out in
@@ -97,13 +97,13 @@ struct DirectArgs {
   int64_t parts_ld;
 };
 
-constexpr int kPackParts = 64;
+constexpr int kPackParts = 256;
 struct PackOperand {
   const void* p;
   void* out;                  // [parts][W][rows][wide rounded up to eight]; null: not packed
   int64_t worker_stride, ld;
   uint32_t rows, wide;
-  int32_t bf16, parts, eights;      // eights: p is at a multiple of 16 bytes
+  int32_t bf16, parts;
 };
 struct PackArgs {
   PackOperand operand[2];

@@ -247,54 +247,76 @@ uint64_t tiles_of(uint64_t v, uint64_t tile) { return (v + tile - 1) / tile; }
 
 uint64_t pack_bytes(int64_t m, int64_t n, int64_t k) {
   auto most = [k](int64_t size) { return static_cast<uint64_t>(std::max(size * ((k + 7) / 8 * 8), k * ((size + 7) / 8 * 8))) * 4; };
-  return whole(most(m)) + whole(most(n)) + 2048;
+  return whole(most(m)) + whole(most(n)) + 4096;
 }
 
+// Estimates of a product's time, us, from which its way is chosen.
+//   small    tiles of 32 x 32 that read their operands from the caches at 8 TB/s together (5 where these are larger,
+//            half where vectors lie across lines): 4 x 512 x
+//            1024 x 1024 bf16 35 us, float 60; and rounds of 1024 k of a workgroup's sixteen waves, 2.5 us each
+//   direct   stages of 64 k: in tiles of 128 0.85 us each with one workgroup on a CU (2048 x 2048 x 2048 33 us), 0.52 with two (2 of
+//            them 39), of 256 1.1, and 1.6 where the chip is full (8 x 4096 x 2048 x 8192 1013 us, in tiles of 128 1237); 32 rows 0.4 us or
+//            what reading the matrix takes; packing and joining by what they move, and 3 us a launch
+// Both sides where they meet: 1024 x 1024 x 1024 bf16 17.5 and 16.2 us, float 30.8 and 33.4; 64 x 4096 x 4096 bf16 24 and 16, float
+// 28 and 110; one token through 4096 x 4096 14.5 and 10.2; 2 x 128 x 1024 x 1024 7.7 and 12.3.
 ProductPlan plan_product(const ProductArgs& args, uint64_t room) {
   ProductPlan plan{};
   plan.parts[0] = plan.parts[1] = 1;
   plan.splits = 1;
   const uint64_t W = args.W, m = args.m, n = args.n, k = args.k;
-  if (k == 0 || m == 0 || n == 0 || double(W) * m * n * k < kSmallWork) return plan;
-  // Padding to 256 may cost a tenth of the products.
-  const uint64_t big = tiles_of(m, 256) * tiles_of(n, 256) * W, small = tiles_of(m, 128) * tiles_of(n, 128) * W;
-  uint64_t tiles, target;
-  if (m <= 32 && args.a.along_k) {
-    plan.tile = 32;
-    tiles = tiles_of(n, 256) * W;
-    target = 256;
-  } else if (big >= 256 && big * 4 <= small + small / 10) {
-    plan.tile = 256;
-    tiles = big;
-    target = 256;
-  } else {
-    plan.tile = 128;
-    tiles = small;
-    target = 512;
-  }
-  if (tiles > kMostGroups || W * m * ((n + 7) / 8) > kMostGroups * 256 * 64) return ProductPlan{};
+  if (k == 0 || m == 0 || n == 0) return plan;
+  const uint64_t part = W * m * (tiles_of(n, 8) * 8) * sizeof(float);
+  auto parts_in = [&](uint64_t bytes) { return std::min(bytes, kPartsRoom) / part; };
+
+  const uint64_t tiles32 = tiles_of(m, 32) * tiles_of(n, 32) * W, rounds = tiles_of(k, 1024);
+  const int element = (args.a.bf16 ? 2 : 4) + (args.b.bf16 ? 2 : 4);
+  ProductPlan small = plan;
+  if (rounds > 2) small.splits = static_cast<uint32_t>(std::max<uint64_t>(1, std::min({rounds, 1024 / tiles32, parts_in(room), uint64_t(32)})));
+  small.bytes = small.splits > 1 ? small.splits * part : 0;
+  double rate = double(W) * k * (m + n) * element < 2e8 ? 8 : 5;
+  if ((args.a.along_k && args.a.ld % 8 != 0) || (args.b.along_k && args.b.ld % 8 != 0)) rate /= 2;
+  const double of_small = 4 + (small.splits > 1 ? 3 : 0) + std::max(2.5 * std::min(k / 1024., double(tiles_of(rounds, small.splits))), tiles32 * 2048e-6 * k * element / 64 / rate);
+
   const int floats = (args.a.bf16 ? 0 : 1) + (args.b.bf16 ? 0 : 1);
   plan.f16 = args.out_bf16 ? floats == 2 : floats > 0;
   uint64_t at = 0;
+  double moved = 0;
   for (int i = 0; i < 2; ++i) {
     const Operand& o = i == 0 ? args.a : args.b;
     const uint64_t size = i == 0 ? m : n, rows = o.along_k ? size : k, wide = tiles_of(o.along_k ? k : size, 8) * 8;
     plan.packed[i] = plan.f16 || !lies_well(o, args.k);
     plan.parts[i] = plan.f16 && !args.out_bf16 && !o.bf16 ? 2 : 1;
     plan.packed_at[i] = at;
-    if (plan.packed[i]) at += whole(W * rows * wide * 2 * plan.parts[i]);
+    if (!plan.packed[i]) continue;
+    at += whole(W * rows * wide * 2 * plan.parts[i]);
+    moved += double(W) * rows * wide * ((o.bf16 ? 2 : 4) * (plan.f16 ? 2 : 1) + 2 * plan.parts[i]);
   }
   plan.largest_at = at;
   at += plan.f16 ? whole(W * 2 * kPackParts * sizeof(float)) : 0;
   plan.exponents_at = at;
   at += plan.f16 ? whole(W * 2 * sizeof(int32_t)) : 0;
   plan.parts_at = at;
-  const uint64_t segments = plan.parts[0] + plan.parts[1] - 1, stages = tiles_of(k, 64) * segments;
-  const uint64_t part = W * m * (tiles_of(n, 8) * 8) * sizeof(float), left = room > at ? std::min(room - at, kPartsRoom) : 0;
-  plan.splits = static_cast<uint32_t>(std::max<uint64_t>(1, std::min({target / std::max<uint64_t>(tiles, 1), stages / 8, left / part, uint64_t(32)})));
-  if (plan.splits > 1) at += plan.splits * part;
-  plan.bytes = at;
-  return plan;
+  const uint64_t segments = plan.parts[0] + plan.parts[1] - 1, stages = tiles_of(k, 64) * segments, left = room > at ? room - at : 0;
+  const double packing = (moved > 0 ? 3 : 0) + (plan.f16 ? 3 : 0) + moved / 3.5e6;
+  double best = of_small;
+  ProductPlan chosen = small;
+  for (int tile : {32, 128, 256}) {
+    if ((tile == 32) != (m <= 32 && args.a.along_k)) continue;
+    const uint64_t tiles = tiles_of(m, tile) * tiles_of(n, tile == 32 ? 256 : tile) * W, target = tile == 128 ? 512 : 256;
+    if (tiles > kMostGroups || W * m * tiles_of(n, 8) > kMostGroups * 256 * 64) continue;
+    plan.tile = tile;
+    plan.splits = static_cast<uint32_t>(std::max<uint64_t>(1, std::min({target / tiles, stages / 8, parts_in(left), uint64_t(32)})));
+    plan.bytes = at + (plan.splits > 1 ? plan.splits * part : 0);
+    const uint64_t each = tiles_of(stages, plan.splits), groups = tiles * plan.splits, on_cu = tiles_of(groups, 256);
+    double us = 5 + packing + (plan.splits > 1 ? 3 + 2 * plan.splits * part / 5e6 : 0);
+    if (tile == 32) us += std::max(0.4 * each * on_cu, 2e-6 * W * n * k / 5.5);
+    else if (tile == 128) us += groups <= 256 ? 0.85 * each + 3 : on_cu * (0.52 * each + 2.5);
+    else us += groups < 200 ? 1.1 * each + 6 : on_cu * (1.6 * each + 6);
+    if (us >= best) continue;
+    best = us;
+    chosen = plan;
+  }
+  return chosen;
 }
 
 }  // namespace noloco

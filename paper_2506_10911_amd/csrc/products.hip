@@ -9,8 +9,8 @@
 //   float result, float operands       a float one as a pair of binary16 (22 bits), a bf16 one as one, times powers of two; the
 //                                      products of two pairs but that of their low halves.  What a pair leaves of a number is
 //                                      2^-22 of it or 2^-40 of the operand's largest.
-// Small products (product_any), which packing would make longer, take any operands through the registers and a float one apart
-// into bf16: two of them, 16 bits, for a bf16 result; three, which together are the number, for a float one, and the products of
+// Small products (product_small), which packing would make longer, take any operands from memory to the registers and a float one
+// apart into bf16: two of them, 16 bits, for a bf16 result; three, which together are the number, for a float one, and the products of
 // parts that reach 2^-16 of the largest.
 #include <type_traits>
 
@@ -55,182 +55,138 @@ template <int N> __device__ __forceinline__ void finish(const ProductArgs& a, in
   store_numbers<N>(a.out, at, a.out_bf16, v);
 }
 
-// Do N neighbouring numbers (four or eight) of everything that the end of a product touches lie at a multiple of their vectors' size?
+// Do N neighbouring numbers (four or eight) of everything that the end of a product touches lie at a multiple of their vectors' size
+// (16 bytes, four bf16 8)?
 template <int N> __device__ __forceinline__ bool ends_in(const ProductArgs& a) {
-  auto fits = [](const void* p, int32_t bf16) { return reinterpret_cast<uintptr_t>(p) % (bf16 ? 2 * N : 16) == 0; };
-  return ((a.out_stride | a.out_ld) & (N - 1)) == 0 && fits(a.out, a.out_bf16) && fits(a.more, a.out_bf16) && fits(a.before, a.out_bf16) &&
-         (a.bias == nullptr || ((a.bias_stride & (N - 1)) == 0 && fits(a.bias, a.bias_bf16)));
+  auto fits = [](const void* p, int32_t bf16, int64_t steps) {
+    return p == nullptr || (reinterpret_cast<uintptr_t>(p) % (bf16 ? 2 * N : 16) == 0 && (steps & (bf16 ? N - 1 : 3)) == 0);
+  };
+  const int64_t steps = a.out_stride | a.out_ld;
+  return fits(a.out, a.out_bf16, steps) && fits(a.more, a.out_bf16, steps) && fits(a.before, a.out_bf16, steps) &&
+         fits(a.bias, a.bias_bf16, a.bias_stride);
 }
 
 // ---------------------------------------------------------------------------
-// Small products, and any operands
+// Small products
 // ---------------------------------------------------------------------------
 
-constexpr int kTile = 128, kDepth = 32;
-constexpr int kPlane = kTile * kDepth * 2;       // bytes of one part of an operand's stage
-
-// Sixteen neighbouring numbers of an operand, as they come from memory; those that are not there are zeros.
-template <typename E> struct Sixteen {
-  E v[16];
-  __device__ __forceinline__ void load(const E* p, int there, bool whole) {
-    if (whole) {
-      constexpr int kVector = 16 / sizeof(E);
-      typedef E vector __attribute__((ext_vector_type(kVector)));
+// Eight neighbouring numbers at any address of their type's alignment, in whole loads.
+template <typename E> struct Eight {
+  typedef E vector __attribute__((ext_vector_type(16 / sizeof(E)), aligned(sizeof(E))));
+  E v[8];
+  __device__ __forceinline__ void along(const E* p) {
+    constexpr int N = 16 / sizeof(E);
 #pragma unroll
-      for (int i = 0; i < 16; i += kVector) {
-        const vector x = *reinterpret_cast<const vector*>(p + i);
+    for (int i = 0; i < 8; i += N) {
+      const vector x = *reinterpret_cast<const vector*>(p + i);
 #pragma unroll
-        for (int k = 0; k < kVector; ++k) v[i + k] = x[k];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = i < there ? p[i] : E(0);
+      for (int k = 0; k < N; ++k) v[i + k] = x[k];
     }
   }
-  // Part `part` of PARTS of numbers first .. first + 7.
-  template <int PARTS> __device__ __forceinline__ ushort8 part(int part, int first) const {
+  __device__ __forceinline__ void across(const E* p, int64_t apart, int there) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < there ? p[i * apart] : E(0);
+  }
+  // Part `part` of PARTS of the numbers.
+  template <int PARTS> __device__ __forceinline__ bf16x8 part(int part) const {
     ushort8 out;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (sizeof(E) == 2) {
-        out[i] = v[first + i];
-      } else if constexpr (PARTS == 1) {
-        out[i] = narrow(v[first + i]);
+        out[i] = v[i];
       } else {
-        // cut, not rounded: each rest is exact, and the third has at most eight bits
-        float x = v[first + i];
+        // cut, not rounded, but for the last: each rest is exact, and a third has at most eight bits
+        float x = v[i];
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           if (k < part) x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
         out[i] = part == PARTS - 1 ? narrow(x) : static_cast<uint16_t>(__float_as_uint(x) >> 16);
       }
     }
-    return out;
+    return __builtin_bit_cast(bf16x8, out);
   }
 };
 
-// 128 x 128 of the result by four waves, each 64 x 64 in blocks of 32 x 32.  Operands come through registers, where they are
-// taken apart, one stage of 32 k ahead of the products.
-//
-// Numbers along k: rows of 64 bytes, 16-byte chunk q of row r at q ^ (r >> 2 & 3), so that 16 lanes meet 16 quarters of the
-// LDS's banks.  Numbers along m: rows of 256 bytes, one k each, chunk q of row k at q ^ (k & 3) << 2, turned by the LDS's
-// transposing reads.
-template <typename TA, typename TB, bool ALONG_A, bool ALONG_B, int PA, int PB>
-__global__ __launch_bounds__(256) void product_any(ProductArgs a) {
-  __shared__ __align__(1024) char lds[(PA + PB) * kPlane];
-  const uint32_t thread = threadIdx.x, lane = thread & 63;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(thread >> 6);
-  const uint32_t wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  const uint32_t tiles_m = (a.m + kTile - 1) / kTile;
-  const uint32_t m0 = blockIdx.x % tiles_m * kTile, n0 = blockIdx.x / tiles_m * kTile;
-  const int64_t w = blockIdx.y;
-  const TA* const pa = static_cast<const TA*>(a.a.p) + w * a.a.worker_stride;
-  const TB* const pb = static_cast<const TB*>(a.b.p) + w * a.b.worker_stride;
+constexpr int kSmallRow = 36;                // floats of a row of a wave's sums in the LDS
+constexpr int kSmallSums = 32 * kSmallRow;
 
-  auto load = [&](auto& into, const auto* p, int64_t ld, auto along, uint32_t first, uint32_t size, uint32_t k0) {
-    typedef typename std::remove_reference<decltype(*p)>::type E;
-    const bool aligned = ((reinterpret_cast<uintptr_t>(p) | static_cast<uint64_t>(ld) * sizeof(E)) & 15) == 0;
-    const uint32_t row = first + (along ? thread >> 1 : (thread & 7) * 16), k = k0 + (along ? (thread & 1) * 16 : thread >> 3);
-    const int64_t there = along ? (row < size ? static_cast<int64_t>(a.k) - k : 0) : (k < a.k ? static_cast<int64_t>(size) - row : 0);
-    const int64_t at = along ? row * ld + k : k * ld + row;
-    into.load(p + (there > 0 ? at : 0), static_cast<int>(there < 0 ? 0 : there < 16 ? there : 16), aligned && there >= 16);
-  };
-  auto put = [&](const auto& from, auto along, auto parts, char* to) {
-    constexpr int P = decltype(parts)::value;
+// 32 x 32 of the result by a workgroup, whose waves take blocks of 64 k in turn and add up their sums in the LDS (and
+// by several, where k is long and tiles are few).  Operands come
+// from memory to the registers as the matrix cores take them, without a barrier: a wave's loads for 64 k are on their way together.
+// What is read of an operand is read by every tile that needs it, which the caches bear in small products.
+template <typename TA, typename TB, bool ALONG_A, bool ALONG_B, int PA, int PB>
+__global__ __launch_bounds__(1024) void product_small(ProductArgs a, float* parts) {
+  extern __shared__ __align__(16) float sums[];
+  constexpr int kSlices = 4;
+  const uint32_t lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tiles_m = (a.m + 31) / 32, m0 = blockIdx.x % tiles_m * 32, n0 = blockIdx.x / tiles_m * 32;
+  const int64_t w = blockIdx.y;
+  // rows behind the last one are the last one: what comes of them is not stored
+  const uint32_t of32 = lane & 31, half = lane >> 5, m = min(m0 + of32, a.m - 1), n = min(n0 + of32, a.n - 1);
+  const TA* const pa = static_cast<const TA*>(a.a.p) + w * a.a.worker_stride + (ALONG_A ? m * a.a.ld : static_cast<int64_t>(m));
+  const TB* const pb = static_cast<const TB*>(a.b.p) + w * a.b.worker_stride + (ALONG_B ? n * a.b.ld : static_cast<int64_t>(n));
+  float16v acc;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t row = along ? thread >> 1 : thread >> 3, q = along ? (thread & 1) * 2 + h : (thread & 7) * 2 + h;
-        const uint32_t at = along ? row * 64 + ((q ^ (row >> 2 & 3)) << 4) : row * 256 + ((q ^ (row & 3) << 2) << 4);
-        *reinterpret_cast<ushort8*>(to + p * kPlane + at) = from.template part<P>(p, h * 8);
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  auto block = [&](uint32_t k0, auto whole) {
+    Eight<TA> fa[kSlices];
+    Eight<TB> fb[kSlices];
+    auto load = [&](auto& f, const auto* p, int64_t ld, auto along, uint32_t k) {
+      if constexpr (whole) {
+        if (along) f.along(p + k); else f.across(p + k * ld, ld, 8);
+      } else {
+        const int there = static_cast<int>(a.k) - static_cast<int>(k);
+        if (along && there >= 8) f.along(p + k); else if (along) f.across(p + k, 1, there); else f.across(p + k * ld, ld, there);
       }
-  };
-  // Fragment: number lane % 32 of a block of 32, eight k from 8 (lane / 32) on.
-  const uint32_t of32 = lane & 31, half = lane >> 5;
-  auto fragment = [&](const char* plane, auto along, uint32_t first, int slice) {
-    if (along) {
-      const uint32_t row = first + of32, q = slice * 2 + half;
-      return *reinterpret_cast<const bf16x8*>(plane + row * 64 + ((q ^ (row >> 2 & 3)) << 4));
-    } else {
-      const uint32_t k = slice * 16 + half * 8 + (lane >> 2 & 3), byte = first * 2 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-      const char* const at = plane + k * 256 + (((byte >> 4) ^ (k & 3) << 2) << 4) + (byte & 15);
-      const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(at));
-      const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_memory short4v*)(at + 4 * 256));
-      return __builtin_bit_cast(bf16x8, static_cast<short8v>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
-    }
-  };
-  typedef typename std::conditional<ALONG_A, Yes, No>::type AlongA;
-  typedef typename std::conditional<ALONG_B, Yes, No>::type AlongB;
-  Sixteen<TA> next_a;
-  Sixteen<TB> next_b;
-  float16v acc[2][2];
+    };
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-  if (a.k > 0) {
-    load(next_a, pa, a.a.ld, AlongA{}, m0, a.m, 0);
-    load(next_b, pb, a.b.ld, AlongB{}, n0, a.n, 0);
-  }
-  for (uint32_t k0 = 0; k0 < a.k; k0 += kDepth) {
-    put(next_a, AlongA{}, Number<PA>{}, lds);
-    put(next_b, AlongB{}, Number<PB>{}, lds + PA * kPlane);
-    __syncthreads();
-    if (k0 + kDepth < a.k) {
-      load(next_a, pa, a.a.ld, AlongA{}, m0, a.m, k0 + kDepth);
-      load(next_b, pb, a.b.ld, AlongB{}, n0, a.n, k0 + kDepth);
+    for (int s = 0; s < kSlices; ++s) {
+      if (!whole && k0 + s * 16 >= a.k) break;
+      const uint32_t k = k0 + s * 16 + half * 8;
+      load(fa[s], pa, a.a.ld, std::integral_constant<bool, ALONG_A>{}, k);
+      load(fb[s], pb, a.b.ld, std::integral_constant<bool, ALONG_B>{}, k);
     }
 #pragma unroll
-    for (int slice = 0; slice < kDepth / 16; ++slice) {
-      bf16x8 fa[PA][2], fb[PB][2];
-#pragma unroll
-      for (int p = 0; p < PA; ++p)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) fa[p][i] = fragment(lds + p * kPlane, AlongA{}, wm + i * 32, slice);
-#pragma unroll
-      for (int p = 0; p < PB; ++p)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) fb[p][j] = fragment(lds + (PA + p) * kPlane, AlongB{}, wn + j * 32, slice);
+    for (int s = 0; s < kSlices; ++s) {
+      if (!whole && k0 + s * 16 >= a.k) break;
       // the small products first
 #pragma unroll
       for (int both = PA > 2 || PB > 2 ? 2 : 1; both >= 0; --both)
 #pragma unroll
         for (int p = 0; p <= both; ++p) {
           if (p >= PA || both - p >= PB) continue;
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[both - p][j], fa[p][i], acc[i][j], 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s].template part<PB>(both - p), fa[s].template part<PA>(p), acc, 0, 0, 0);
         }
     }
-    __syncthreads();
+  };
+  for (uint32_t k0 = (blockIdx.z * waves + wave) * 64; k0 < a.k; k0 += gridDim.z * waves * 64) {
+    if (k0 + 64 <= a.k) block(k0, Yes{}); else block(k0, No{});
   }
-
-  // Block (i, j), element e of a lane: m = 32 i + of32, n = 32 j + 8 (e / 4) + 4 half + e % 4.
+  // element e of a lane: m = lane % 32, n = 8 (e / 4) + 4 (lane / 32) + e % 4
+#pragma unroll
+  for (int e = 0; e < 16; e += 4)
+    *reinterpret_cast<float4v*>(sums + wave * kSmallSums + of32 * kSmallRow + e * 2 + half * 4) = float4v{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+  __syncthreads();
   const bool fours = ends_in<4>(a);
+  for (uint32_t v4 = threadIdx.x; v4 < 256; v4 += blockDim.x) {
+    const uint32_t row = v4 >> 3, col = (v4 & 7) * 4;
+    if (m0 + row >= a.m || n0 + col >= a.n) continue;
+    float4v sum = *reinterpret_cast<const float4v*>(sums + row * kSmallRow + col);
+    for (uint32_t i = 1; i < waves; ++i) sum += *reinterpret_cast<const float4v*>(sums + i * kSmallSums + row * kSmallRow + col);
+    if (parts != nullptr) {
+      *reinterpret_cast<float4v*>(parts + ((blockIdx.z * static_cast<uint64_t>(a.W) + w) * a.m + m0 + row) * ((a.n + 7) / 8 * 8) + n0 + col) = sum;
+      continue;
+    }
+    float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    if (n0 + col + 4 <= a.n && fours) {
+      finish<4>(a, w, m0 + row, n0 + col, v);
+    } else {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const uint32_t m = m0 + wm + i * 32 + of32, n = n0 + wn + j * 32 + e * 2 + half * 4;
-        if (m >= a.m || n >= a.n) continue;
-        float v[4] = {acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
-        if (fours && n + 4 <= a.n) {
-          finish<4>(a, w, m, n, v);
-        } else {
-#pragma unroll 1
-          for (uint32_t c = 0; c < 4 && n + c < a.n; ++c) {
-            float one = c == 0 ? v[0] : (c == 1 ? v[1] : (c == 2 ? v[2] : v[3]));
-            finish<1>(a, w, m, n + c, &one);
-          }
-        }
-      }
+      for (uint32_t c = 0; c < 4; ++c)
+        if (n0 + col + c < a.n) finish<1>(a, w, m0 + row, n0 + col + c, v + c);
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -460,7 +416,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
 
   // Results go through the LDS, 32 rows of every wave at a time, and from there in whole lines.  Block (i, j), element e of a lane:
   // m = 32 i + lane % 32, n = 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4.
-  const bool eights = ends_in<8>(a);
+  const bool eights = ends_in<8>(a), fours = ends_in<4>(a);
   const uint32_t of32 = lane & 31, half = lane >> 5;
 #pragma unroll
   for (int i = 0; i < MB; ++i) {
@@ -473,7 +429,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
         *reinterpret_cast<float4v*>(mine + j * 128 + e * 8) = float4v{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
     __syncthreads();
     auto row_of = [&](uint32_t row) { return m0 + row / 32 * (TM / WM) + i * 32 + row % 32; };
-    if (d.parts != nullptr || eights) {
+    if (d.parts != nullptr || fours) {
       for (uint32_t v = thread; v < kImageRows * (TN / 8); v += kThreads) {
         const uint32_t row = v / (TN / 8), col = v % (TN / 8) * 8, m = row_of(row), n = n0 + col;
         if (m >= a.m || n >= a.n) continue;
@@ -486,12 +442,19 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
           continue;
         }
         float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        if (n + 8 <= a.n) {
+        if (eights && n + 8 <= a.n) {
           finish<8>(a, w, m, n, x);
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (n + e < a.n) finish<1>(a, w, m, n + e, x + e);
+          for (int h = 0; h < 8; h += 4) {
+            if (n + h + 4 <= a.n) {
+              finish<4>(a, w, m, n + h, x + h);
+            } else {
+#pragma unroll
+              for (int e = h; e < h + 4; ++e)
+                if (n + e < a.n) finish<1>(a, w, m, n + e, x + e);
+            }
+          }
         }
       }
     } else {
@@ -534,32 +497,36 @@ __global__ __launch_bounds__(256) void product_join(ProductArgs a, DirectArgs d)
 // Operands as large products take them
 // ---------------------------------------------------------------------------
 
-// The largest finite number of an operand, or of what one of kPackParts workgroups takes of it.
+// Eight numbers of a row from column `col` on as floats; zeros behind its end.
+__device__ __forceinline__ void load_eight(const PackOperand& o, int64_t row_at, uint32_t col, float* x) {
+  auto load = [&](auto element) {
+    typedef decltype(element) E;
+    const E* const p = static_cast<const E*>(o.p) + row_at + col;
+    Eight<E> eight;
+    if (col + 8 <= o.wide) eight.along(p); else eight.across(p, 1, static_cast<int>(o.wide - col));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (sizeof(E) == 2) x[e] = widen(eight.v[e]); else x[e] = eight.v[e];
+    }
+  };
+  if (o.bf16) load(uint16_t{}); else load(float{});
+}
+
+// The largest finite number of what one of kPackParts workgroups takes of an operand.
 __global__ __launch_bounds__(256) void product_largest(PackArgs p) {
   const PackOperand& o = p.operand[blockIdx.z];
   if (o.out == nullptr) return;
-  const int64_t w = blockIdx.y, numbers = static_cast<int64_t>(o.rows) * o.wide;
+  const int64_t w = blockIdx.y;
+  const uint32_t vectors = (o.wide + 7) / 8, all = o.rows * vectors;
   float most = 0.f;
-  auto take = [&](float v) {
-    v = fabsf(v);
-    most = v < __builtin_inff() ? fmaxf(most, v) : most;
-  };
-  const int64_t at = w * o.worker_stride;
-  const bool vectors = o.eights && ((o.worker_stride | o.ld | o.wide) & 7) == 0;
-  if (vectors) {
-    for (int64_t v = blockIdx.x * 256 + threadIdx.x; v < numbers / 8; v += kPackParts * 256) {
-      const int64_t row = v * 8 / o.wide, col = v * 8 - row * o.wide;
-      float x[8];
-      load_numbers<8>(o.p, at + row * o.ld + col, o.bf16, x);
+  for (uint32_t v = blockIdx.x * 256 + threadIdx.x; v < all; v += kPackParts * 256) {
+    const uint32_t row = v / vectors;
+    float x[8];
+    load_eight(o, w * o.worker_stride + row * o.ld, (v - row * vectors) * 8, x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) take(x[e]);
-    }
-  } else {
-    for (int64_t v = blockIdx.x * 256 + threadIdx.x; v < numbers; v += kPackParts * 256) {
-      const int64_t row = v / o.wide, col = v - row * o.wide;
-      float x;
-      load_numbers<1>(o.p, at + row * o.ld + col, o.bf16, &x);
-      take(x);
+    for (int e = 0; e < 8; ++e) {
+      const float size = fabsf(x[e]);
+      most = size < __builtin_inff() ? fmaxf(most, size) : most;
     }
   }
 #pragma unroll
@@ -579,8 +546,9 @@ __global__ __launch_bounds__(256) void product_pack(PackArgs p) {
   const int64_t w = blockIdx.y;
   int by = 0;
   if (p.f16) {
-    static_assert(kPackParts == 64, "a lane each");
-    float most = p.largest[(w * 2 + blockIdx.z) * kPackParts + (threadIdx.x & 63)];
+    static_assert(kPackParts == 256, "four of a lane");
+    const float4v four = *reinterpret_cast<const float4v*>(p.largest + (w * 2 + blockIdx.z) * kPackParts + (threadIdx.x & 63) * 4);
+    float most = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
     if (most > 0.f) {
@@ -590,24 +558,12 @@ __global__ __launch_bounds__(256) void product_pack(PackArgs p) {
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) p.exponents[w * 2 + blockIdx.z] = by;
   }
-  const uint32_t vectors = static_cast<uint32_t>((o.wide + 7) / 8);
-  const int64_t all = static_cast<int64_t>(o.rows) * vectors;
-  const bool whole = o.eights && ((o.worker_stride | o.ld | o.wide) & 7) == 0;
-  for (int64_t v = blockIdx.x * 256 + threadIdx.x; v < all; v += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t row = v / vectors;
-    const uint32_t col = static_cast<uint32_t>(v - row * vectors) * 8;
-    const int64_t from = w * o.worker_stride + row * o.ld + col;
+  const uint32_t vectors = (o.wide + 7) / 8, all = o.rows * vectors;
+  uint16_t* const out = static_cast<uint16_t*>(o.out) + w * (all * 8ll);
+  for (uint32_t v = blockIdx.x * 256 + threadIdx.x; v < all; v += gridDim.x * 256) {
+    const uint32_t row = v / vectors;
     float x[8];
-    if (whole) {
-      load_numbers<8>(o.p, from, o.bf16, x);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = 0.f;
-        if (col + e < o.wide) load_numbers<1>(o.p, from + e, o.bf16, x + e);
-      }
-    }
-    uint16_t* const to = static_cast<uint16_t*>(o.out) + (w * o.rows + row) * (vectors * 8ll) + col;
+    load_eight(o, w * o.worker_stride + row * o.ld, (v - row * vectors) * 8, x);
     ushort8 first, second;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -620,8 +576,8 @@ __global__ __launch_bounds__(256) void product_pack(PackArgs p) {
         first[e] = narrow(x[e]);
       }
     }
-    *reinterpret_cast<ushort8*>(to) = first;
-    if (o.parts == 2) *reinterpret_cast<ushort8*>(to + static_cast<int64_t>(p.W) * o.rows * (vectors * 8ll)) = second;
+    *reinterpret_cast<ushort8*>(out + v * 8ll) = first;
+    if (o.parts == 2) *reinterpret_cast<ushort8*>(out + p.W * (all * 8ll) + v * 8ll) = second;
   }
 }
 
@@ -629,17 +585,19 @@ __global__ __launch_bounds__(256) void product_pack(PackArgs p) {
 
 namespace {
 
-int launch_any(const ProductArgs& args, void* stream) {
-  const dim3 grid((args.m + kTile - 1) / kTile * ((args.n + kTile - 1) / kTile), args.W);
+int launch_small(const ProductArgs& args, uint32_t splits, float* parts, void* stream) {
+  // blocks of 64 k that a wave takes: one, where a workgroup has as many waves
+  const uint32_t blocks = (args.k + 63) / 64, waves = blocks <= 2 ? std::max(blocks, 1u) : (blocks <= 4 ? 4 : (blocks <= 8 ? 8 : 16));
+  const dim3 grid((args.m + 31) / 32 * ((args.n + 31) / 32), args.W, splits);
   auto with_layout = [&](auto ta, auto tb, auto pa, auto pb) {
     typedef decltype(ta) TA;
     typedef decltype(tb) TB;
     constexpr int PA = decltype(pa)::value, PB = decltype(pb)::value;
     if (args.a.along_k) {
-      return args.b.along_k ? enqueue(product_any<TA, TB, true, true, PA, PB>, grid, 256, 0, stream, args)
-                            : enqueue(product_any<TA, TB, true, false, PA, PB>, grid, 256, 0, stream, args);
+      return args.b.along_k ? enqueue(product_small<TA, TB, true, true, PA, PB>, grid, waves * 64, waves * kSmallSums * 4, stream, args, parts)
+                            : enqueue(product_small<TA, TB, true, false, PA, PB>, grid, waves * 64, waves * kSmallSums * 4, stream, args, parts);
     }
-    return enqueue(product_any<TA, TB, false, false, PA, PB>, grid, 256, 0, stream, args);
+    return enqueue(product_small<TA, TB, false, false, PA, PB>, grid, waves * 64, waves * kSmallSums * 4, stream, args, parts);
   };
   const uint16_t half = 0;
   const float whole = 0.f;
@@ -658,8 +616,16 @@ int launch_any(const ProductArgs& args, void* stream) {
 
 int launch_product(const ProductArgs& args, const ProductPlan& plan, char* room, void* stream) {
   if (args.m == 0 || args.n == 0) return 0;
-  if (plan.tile == 0) return launch_any(args, stream);
   DirectArgs d{};
+  d.splits = plan.splits;
+  d.parts = plan.splits > 1 ? reinterpret_cast<float*>(room + plan.parts_at) : nullptr;
+  d.parts_ld = (args.n + 7) / 8 * 8;
+  auto join = [&](int st) {
+    if (st != 0 || d.splits == 1) return st;
+    const uint64_t vectors = static_cast<uint64_t>(args.W) * args.m * ((args.n + 7) / 8);
+    return enqueue(product_join, dim3(static_cast<uint32_t>((vectors + 255) / 256)), 256, 0, stream, args, d);
+  };
+  if (plan.tile == 0) return join(launch_small(args, plan.splits, d.parts, stream));
   PackArgs pack{};
   pack.f16 = plan.f16;
   pack.W = args.W;
@@ -673,8 +639,7 @@ int launch_product(const ProductArgs& args, const ProductPlan& plan, char* room,
     int64_t worker = o.worker_stride, ld = o.ld, part = 0;
     if (plan.packed[i]) {
       PackOperand& to = pack.operand[i];
-      to = {o.p, room + plan.packed_at[i], o.worker_stride, o.ld, o.along_k ? size : args.k, o.along_k ? args.k : size, o.bf16, plan.parts[i],
-            reinterpret_cast<uintptr_t>(o.p) % 16 == 0};
+      to = {o.p, room + plan.packed_at[i], o.worker_stride, o.ld, o.along_k ? size : args.k, o.along_k ? args.k : size, o.bf16, plan.parts[i]};
       p = to.out;
       ld = (to.wide + 7ll) / 8 * 8;
       worker = to.rows * ld;
@@ -703,9 +668,6 @@ int launch_product(const ProductArgs& args, const ProductPlan& plan, char* room,
     (plan.parts[0] == 2 ? d.a_parts : d.b_parts) = 1;
   }
   d.exponents = pack.exponents;
-  d.splits = plan.splits;
-  d.parts = plan.splits > 1 ? reinterpret_cast<float*>(room + plan.parts_at) : nullptr;
-  d.parts_ld = (args.n + 7) / 8 * 8;
   auto tiles = [&](uint32_t tm, uint32_t tn, uint32_t run) {
     d.tiles_m = (args.m + tm - 1) / tm;
     d.tiles_n = (args.n + tn - 1) / tn;
@@ -728,9 +690,7 @@ int launch_product(const ProductArgs& args, const ProductPlan& plan, char* room,
     st = ab ? NOLOCO_PRODUCT(32, 256, 1, 4, 4, true, true) : NOLOCO_PRODUCT(32, 256, 1, 4, 4, true, false);
   }
 #undef NOLOCO_PRODUCT
-  if (st != 0 || d.splits == 1) return st;
-  const uint64_t vectors = static_cast<uint64_t>(args.W) * args.m * ((args.n + 7) / 8);
-  return enqueue(product_join, dim3(static_cast<uint32_t>((vectors + 255) / 256)), 256, 0, stream, args, d);
+  return join(st);
 }
 
 }  // namespace noloco
