@@ -68,7 +68,7 @@ def check(logits, tokens, vocab, top):
     again = forward(logits, tokens, vocab, top, max_tokens=logits.shape[1] + 500, max_top=32)
     assert all(torch.equal(got[k].nan_to_num(7.0), again[k].nan_to_num(7.0)) for k in got if k != "norms") and same_bits(got["norms"], again["norms"])
     few = forward(logits, tokens, vocab, 0, entropy=False, norms=False)
-    assert same_bits(few["log_probs"], got["log_probs"])
+    within(few["log_probs"], *want["log_probs"])           # another workgroup size may sum in another order
 
 
 SIZES = [  # W, T, vocab, row_stride
