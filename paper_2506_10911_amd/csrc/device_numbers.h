@@ -30,14 +30,20 @@ template <typename E, int N> struct Stored {
   static constexpr int kVector = N == 1 ? 1 : (sizeof(E) == 2 && N % 8 == 0 ? 8 : 4);
   static_assert(N % kVector == 0, "vectors");
   typedef E vector __attribute__((ext_vector_type(kVector)));
-  __device__ __forceinline__ static void load(const E* p, float* v) {
+  __device__ __forceinline__ static void load(const E* p, float* v) { load<false>(p, v); }
+  __device__ __forceinline__ static void store(E* p, const float* v) { store<false>(p, v); }
+  // What nobody reads again soon: past the caches that others fill.
+  __device__ __forceinline__ static void load_once(const E* p, float* v) { load<true>(p, v); }
+  __device__ __forceinline__ static void store_once(E* p, const float* v) { store<true>(p, v); }
+  template <bool ONCE> __device__ __forceinline__ static void load(const E* p, float* v) {
 #pragma unroll
     for (int i = 0; i < N; i += kVector) {
       E raw[kVector];
       if constexpr (kVector == 1) {
         raw[0] = *p;
       } else {
-        const vector x = *reinterpret_cast<const vector*>(p + i);
+        const vector* const from = reinterpret_cast<const vector*>(p + i);
+        const vector x = ONCE ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
         for (int k = 0; k < kVector; ++k) raw[k] = x[k];
       }
@@ -47,7 +53,7 @@ template <typename E, int N> struct Stored {
       }
     }
   }
-  __device__ __forceinline__ static void store(E* p, const float* v) {
+  template <bool ONCE> __device__ __forceinline__ static void store(E* p, const float* v) {
 #pragma unroll
     for (int i = 0; i < N; i += kVector) {
       E raw[kVector];
@@ -61,7 +67,8 @@ template <typename E, int N> struct Stored {
         vector x;
 #pragma unroll
         for (int k = 0; k < kVector; ++k) x[k] = raw[k];
-        *reinterpret_cast<vector*>(p + i) = x;
+        vector* const to = reinterpret_cast<vector*>(p + i);
+        if constexpr (ONCE) __builtin_nontemporal_store(x, to); else *to = x;
       }
     }
   }

@@ -44,14 +44,11 @@ struct RowEnd {
   float largest, log_total;        // log(1 + rest)
   __device__ __forceinline__ float log_prob(float logit) const { return largest == -kInfinity ? largest : (logit - largest) - log_total; }
 };
-__device__ __forceinline__ RowEnd finish_row(const LogProbArgs& a, int64_t row, float largest, float rest, float spread, bool writes) {
+__device__ __forceinline__ RowEnd finish_row(const LogProbArgs& a, int64_t row, int64_t token, float logit, float largest, float rest, float spread, bool writes) {
   RowEnd end{largest, log1pf(rest)};
   const bool nan = rest != rest, nothing = !nan && largest == -kInfinity;
   if (nan) end.largest = rest;
   if (writes) {
-    const int64_t token = token_of(a, row);
-    float logit = 0.f;
-    if (token >= 0) load_numbers<1>(a.logits, row * a.row_stride + token, a.logits_bf16, &logit);
     a.log_probs[row] = token >= 0 ? end.log_prob(logit) : 0.f;
     if (a.norms != nullptr) a.norms[row] = end.largest + end.log_total;
     if (a.entropy != nullptr) a.entropy[row] = nothing ? 0.f : end.log_total + spread / (1.f + rest);
@@ -184,7 +181,10 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
     }
     RowEnd row_end{};
     if (a.num_parts == 1) {
-      row_end = finish_row(a, row, largest, rest, spread, at == 0);
+      const int64_t token = token_of(a, row);
+      float logit = 0.f;
+      if (at == 0 && token >= 0) load_numbers<1>(a.logits, row * a.row_stride + token, a.logits_bf16, &logit);
+      row_end = finish_row(a, row, token, logit, largest, rest, spread, at == 0);
     } else if (at == 0) {
       a.parts[row * a.num_parts + blockIdx.y] = LogPart{largest, rest, spread, 0.f};
     }
@@ -283,12 +283,20 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
   }
 }
 
-// A row's parts together, a wave a row: the first part that has the largest logit gives its rest, the others all of their sum.
-constexpr uint32_t kJoinKeys = 4096;
-__global__ __launch_bounds__(64) void log_probs_join(LogProbArgs a) {
+// A row's parts together, a workgroup a row: the first part that has the largest logit gives its rest, the others all of their sum.
+constexpr uint32_t kJoinKeys = 1024;
+__global__ __launch_bounds__(256) void log_probs_join(LogProbArgs a) {
   __shared__ uint64_t near[kJoinKeys];
-  const uint32_t lane = threadIdx.x;
+  const uint32_t lane = threadIdx.x & 63;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    // every wave for itself up to the alternatives, whose keys come meanwhile
+    const int64_t token = token_of(a, row);
+    float logit = 0.f;
+    if (token >= 0) load_numbers<1>(a.logits, row * a.row_stride + token, a.logits_bf16, &logit);
+    const uint32_t top = a.top, all = a.num_parts * top;
+    const uint64_t* const keys = a.keys + row * all;
+    if (all <= kJoinKeys)
+      for (uint32_t c = threadIdx.x; c < all; c += 256) near[c] = keys[c];
     const LogPart* const parts = a.parts + row * a.num_parts;
     float largest = -kInfinity;
     for (uint32_t i = lane; i < a.num_parts; i += 64) largest = fmaxf(largest, parts[i].largest);
@@ -311,41 +319,37 @@ __global__ __launch_bounds__(64) void log_probs_join(LogProbArgs a) {
     }
     rest = wave_sum(rest);
     spread = wave_sum(spread);
-    const RowEnd end = finish_row(a, row, largest, rest, spread, lane == 0);
-    const uint32_t top = a.top, all = a.num_parts * top;
-    const uint64_t* keys = a.keys + row * all;
-    if (all <= kJoinKeys) {
-      for (uint32_t c = lane; c < all; c += 64) near[c] = keys[c];
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-      __builtin_amdgcn_wave_barrier();
-      keys = near;
-    }
-    uint32_t real = 0;
-    for (uint32_t c = lane; c < all; c += 64) {
+    const RowEnd end = finish_row(a, row, token, logit, largest, rest, spread, threadIdx.x == 0);
+    if (top == 0) continue;
+    __syncthreads();
+    // A key's place is the number of larger ones: counted while there are few, searched in the sorted lists where there are many.
+    for (uint32_t c = threadIdx.x; c < all; c += 256) {
       const uint64_t k = keys[c];
       if (k == 0) continue;
-      ++real;
-      const uint32_t mine = c / top;
-      uint32_t larger = c - mine * top;      // lists are sorted: those before it in its own
-      for (uint32_t i = 0; i < a.num_parts && larger < top; ++i) {
-        if (i == mine) continue;
-        uint32_t lo = 0, hi = top;
-        while (lo < hi) {
-          const uint32_t mid = (lo + hi) / 2;
-          if (keys[i * top + mid] > k) lo = mid + 1; else hi = mid;
+      uint32_t larger = 0;
+      if (all <= kJoinKeys) {
+#pragma unroll 8
+        for (uint32_t i = 0; i < all; ++i) larger += near[i] > k ? 1 : 0;
+      } else {
+        for (uint32_t i = 0; i < a.num_parts && larger < top; ++i) {
+          uint32_t lo = 0, hi = top;
+          while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (keys[i * top + mid] > k) lo = mid + 1; else hi = mid;
+          }
+          larger += lo;
         }
-        larger += lo;
       }
       if (larger >= top) continue;
       a.top_tokens[row * top + larger] = static_cast<int32_t>(~static_cast<uint32_t>(k));
       a.top_log_probs[row * top + larger] = end.log_prob(logit_of(k));
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) real += static_cast<uint32_t>(__shfl_xor(static_cast<int>(real), d));
-    for (uint32_t c = real + lane; c < top; c += 64) {
+    // a vocabulary has as many keys as tokens, or `top` of each of its parts: only one that is smaller leaves places
+    for (uint32_t c = a.vocab + threadIdx.x; c < top; c += 256) {
       a.top_tokens[row * top + c] = -1;
       a.top_log_probs[row * top + c] = -kInfinity;
     }
+    __syncthreads();
   }
 }
 
@@ -383,7 +387,7 @@ __global__ __launch_bounds__(256) void log_probs_gradient(LogProbArgs a) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const uint32_t at = start + k * 256 * 8;
-      if (!nothing && at >= first && at + 8 <= end) Stored<E, 8>::load(from + at, v[k]);
+      if (!nothing && at >= first && at + 8 <= end) Stored<E, 8>::load_once(from + at, v[k]);
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(256) void log_probs_gradient(LogProbArgs a) {
           for (int e = 0; e < 8; ++e)
             if (token - at == e) x[e] = at_token(v[k][e]);
         }
-        Stored<Out, 8>::store(to + at, x);
+        Stored<Out, 8>::store_once(to + at, x);
       } else if (at < end) {
         for (uint32_t i = at < first ? first : at; i < at + 8 && i < end; ++i) {
           float l = 0.f;
@@ -437,7 +441,7 @@ int launch_log_probs(const LogProbArgs& args, void* stream) {
   };
   const int st = args.logits_bf16 ? with(uint16_t{}) : with(float{});
   if (st != 0 || args.num_parts == 1) return st;
-  return enqueue(log_probs_join, dim3(static_cast<uint32_t>(std::min(args.rows, kMostGroups))), 64, 0, stream, args);
+  return enqueue(log_probs_join, dim3(static_cast<uint32_t>(std::min(args.rows, kMostGroups))), 256, 0, stream, args);
 }
 
 int launch_log_probs_gradient(const LogProbArgs& args, void* stream) {

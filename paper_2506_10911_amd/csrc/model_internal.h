@@ -18,7 +18,7 @@ constexpr int64_t kNormRows = 4;            // rows that a workgroup works on at
 
 // Workgroups of a worker: each takes every `groups`th set of rows and leaves one sum of the weights' gradients.
 inline uint32_t norm_groups(int64_t tokens, int64_t W, int64_t width) {
-  const int64_t most = std::max<int64_t>(1, (width > kNormGradientHeld ? 64 : 1024) / W);
+  const int64_t most = std::max<int64_t>(1, (width > kNormGradientHeld ? 64 : 768) / W);
   return static_cast<uint32_t>(std::max<int64_t>(1, std::min((tokens + kNormRows - 1) / kNormRows, most)));
 }
 
@@ -118,8 +118,8 @@ struct SlopeArgs {
   const void* dout;           // [W][tokens][outputs]
   const void* before;         // null: dz is dout, and only the sums are made
   void* dz;
-  float* partial;             // [W][groups][outputs]; null: no sums
-  void* grad;                 // worker 0's first bias
+  float* partial;             // [W][groups][outputs]
+  void* grad;                 // worker 0's first bias; null: no sums
   int64_t stride;             // between workers' rows of grad
   int64_t tokens;
   uint32_t outputs, groups;
@@ -127,9 +127,11 @@ struct SlopeArgs {
   int32_t dout_bf16, dz_bf16, grad_bf16, accumulate;
 };
 
-constexpr int64_t kSlopeRows = 64;           // tokens of a workgroup, at least
+// Groups of tokens, each a workgroup's: 64 of 64 tokens and more; up to 256 tokens are one group, which leaves its sums in the
+// gradient itself.
+constexpr int64_t kSlopeRows = 64;
 inline uint32_t slope_groups(int64_t tokens) {
-  return static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>((tokens + kSlopeRows - 1) / kSlopeRows, 64)));
+  return tokens <= 4 * kSlopeRows ? 1 : static_cast<uint32_t>(std::min<int64_t>((tokens + kSlopeRows - 1) / kSlopeRows, 64));
 }
 int launch_slope(const SlopeArgs& args, void* stream);
 

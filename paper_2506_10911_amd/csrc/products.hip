@@ -42,10 +42,7 @@ template <int N> __device__ __forceinline__ void finish(const ProductArgs& a, in
     for (int i = 0; i < N; ++i) v[i] += bias[i];
   }
   if (a.before != nullptr) store_numbers<N>(a.before, at, a.out_bf16, v);
-  if (a.activation != NOLOCO_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = activate(a.activation, v[i]);
-  }
+  activate<N>(a.activation, v);
   if (a.more != nullptr || a.accumulate) {
     float more[N];
     load_numbers<N>(a.accumulate ? a.out : a.more, at, a.out_bf16, more);
