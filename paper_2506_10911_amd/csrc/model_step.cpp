@@ -303,7 +303,7 @@ ProductPlan plan_product(const ProductArgs& args, uint64_t room) {
   for (int tile : {32, 128, 256}) {
     if ((tile == 32) != (m <= 32 && args.a.along_k)) continue;
     const uint64_t tiles = tiles_of(m, tile) * tiles_of(n, tile == 32 ? 256 : tile) * W, target = tile == 128 ? 512 : 256;
-    if (tiles > kMostGroups || W * m * tiles_of(n, 8) > kMostGroups * 256 * 64) continue;
+    if (tiles > kMostGroups) continue;
     plan.tile = tile;
     plan.splits = static_cast<uint32_t>(std::max<uint64_t>(1, std::min({target / tiles, stages / 8, parts_in(left), uint64_t(32)})));
     plan.bytes = at + (plan.splits > 1 ? plan.splits * part : 0);

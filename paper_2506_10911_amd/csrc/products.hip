@@ -364,12 +364,11 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
   if (stages >= STAGES) {
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) ask();
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * kLoads) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * kLoads) : "memory");
   } else {
     for (uint32_t i = 0; i < stages; ++i) ask();
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   }
-  __builtin_amdgcn_s_barrier();
   Fragments even, odd;
   read(0, 0, even);
   // The stages behind the last one that is asked for by themselves, so that nothing in the loop is conditional.
@@ -381,10 +380,9 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
       if (slice + 1 < kSlices) {
         read(s, slice + 1, next);
       } else {
-        // the next stage has come, those behind it may be on their way
-        if constexpr (ask_more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * kLoads) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
+        // the next stage has come, those behind it may be on their way; wait and barrier in one, so that no read comes between them
+        if constexpr (ask_more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if constexpr (read_next) read(s + 1, 0, next);
         if constexpr (ask_more) ask();
       }

@@ -1,6 +1,7 @@
 """What layer norm, matrices and log probabilities refuse before they touch a GPU, and their host code under AddressSanitizer and
 UBSan against stand-ins for the HIP runtime and the kernel launchers."""
 import os
+import re
 import subprocess
 
 import pytest
@@ -84,3 +85,28 @@ def test_host_code_is_clean_under_asan_and_ubsan(tmp_path):
                          capture_output=True, text=True, timeout=300)
     assert run.returncode == 0, run.stdout + run.stderr
     assert "model host driver: ok" in run.stdout
+
+
+def test_only_the_loads_to_the_lds_use_m0(tmp_path):
+    """They write it in inline assembly, which cannot say so: m0 is reserved. So nothing else in these kernels may count on what it holds."""
+    with open(nl.library_path(), "rb") as f:
+        data = f.read()
+    kernels, at = 0, data.find(b"\x7fELF", 4)
+    objdump = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "llvm-objdump")
+    while at >= 0:
+        if int.from_bytes(data[at + 18:at + 20], "little") == 224:                  # AMDGPU
+            table, entry, count = (int.from_bytes(data[at + a:at + b], "little") for a, b in ((40, 48), (58, 60), (60, 62)))
+            if b"product_direct" in data[at:at + table]:
+                image = tmp_path / "gfx950.elf"
+                image.write_bytes(data[at:at + table + entry * count])
+                text = subprocess.run([objdump, "-d", "--no-show-raw-insn", str(image)], check=True, capture_output=True, text=True).stdout
+                for body in re.findall(r"<[^>]*product_direct[^>]*>:\n(.*?)\n\n", text + "\n\n", re.S):
+                    lines = [line.split("//")[0].strip() for line in body.splitlines()]
+                    kernels += 1
+                    for i, line in enumerate(lines):
+                        if re.search(r"\bm0\b", line):
+                            assert re.match(r"s_mov_b32 m0, s\d+$", line) and lines[i + 1] == "s_nop 0" and lines[i + 2].endswith("offen lds")
+                        elif line.endswith(" lds"):
+                            assert lines[i - 2].startswith("s_mov_b32 m0")
+        at = data.find(b"\x7fELF", at + 4)
+    assert kernels == 2 * (3 + 3 + 2)                  # formats; layouts of the operands in tiles of 256, 128, 32 x 256
