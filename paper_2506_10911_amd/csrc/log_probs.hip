@@ -66,6 +66,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
   constexpr uint32_t kMost = (NOLOCO_MAX_TOP * (L == 64 ? 16 : 64)) + 64;
   __shared__ float shared[4][2 * kWaves];
   __shared__ uint64_t keys[TOP ? kRows : 1][TOP ? L : 1], found[TOP ? kRows : 1][TOP ? kMost : 1];
+  __shared__ uint64_t groups[TOP ? kRows : 1][64];
   __shared__ uint32_t found_count[kRows];
   __shared__ uint64_t bound_of[kRows];
   const uint32_t sub = threadIdx.x / L, at = threadIdx.x % L, lane = threadIdx.x & 63;
@@ -215,13 +216,12 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
         uint64_t group = keys[sub][lane];
 #pragma unroll
         for (uint32_t i = 1; i < kWaves; ++i) group = max(group, keys[sub][i * 64 + lane]);
+        groups[sub][lane] = group;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
         uint32_t larger = 0;
-#pragma unroll 1
-        for (int j = 0; j < 64; ++j) {
-          const uint64_t other = static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<int>(group >> 32), j)) << 32 |
-                                 static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(group), j));
-          larger += other > group ? 1 : 0;
-        }
+#pragma unroll 16
+        for (int j = 0; j < 64; ++j) larger += groups[sub][j] > group ? 1 : 0;
         if (lane == 0) bound_of[sub] = 1;
         if (larger == top - 1 && group != 0) bound_of[sub] = group;
       }
@@ -261,6 +261,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
       for (uint32_t c = at; c < candidates; c += L) {
         const uint64_t k = found[sub][c];
         uint32_t larger = 0;
+#pragma unroll 8
         for (uint32_t j = 0; j < candidates; ++j) larger += found[sub][j] > k ? 1 : 0;
         if (larger >= top) continue;
         if (a.num_parts == 1) {

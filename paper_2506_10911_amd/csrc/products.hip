@@ -32,6 +32,12 @@ typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 #define lds_memory __attribute__((address_space(3)))
 
+// What the end of a product adds to N neighbouring numbers of a row: the residual, or what is there.
+template <int N> __device__ __forceinline__ void load_more(const ProductArgs& a, int64_t w, uint32_t m, uint32_t n, float* more) {
+  if (a.more != nullptr || a.accumulate)
+    load_numbers<N>(a.accumulate ? a.out : a.more, w * a.out_stride + m * a.out_ld + n, a.out_bf16, more);
+}
+
 // The end of a product for N neighbouring numbers of a row.
 template <int N> __device__ __forceinline__ void finish(const ProductArgs& a, int64_t w, uint32_t m, uint32_t n, float* v) {
   const int64_t at = w * a.out_stride + m * a.out_ld + n;
@@ -45,7 +51,7 @@ template <int N> __device__ __forceinline__ void finish(const ProductArgs& a, in
   activate<N>(a.activation, v);
   if (a.more != nullptr || a.accumulate) {
     float more[N];
-    load_numbers<N>(a.accumulate ? a.out : a.more, at, a.out_bf16, more);
+    load_more<N>(a, w, m, n, more);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += more[i];
   }
@@ -412,9 +418,23 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
   // Results go through the LDS, 32 rows of every wave at a time, and from there in whole lines.  Block (i, j), element e of a lane:
   // m = 32 i + lane % 32, n = 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4.
   const bool eights = ends_in<8>(a), fours = ends_in<4>(a);
+  const bool adds = d.parts == nullptr && eights && a.activation == NOLOCO_ACT_NONE && a.before == nullptr && a.bias == nullptr && a.n % 8 == 0 &&
+                    (a.more != nullptr || a.accumulate);
   const uint32_t of32 = lane & 31, half = lane >> 5;
+  constexpr int kVectors = kImageRows * (TN / 8) / kThreads;      // of eight numbers that a thread writes at a time
 #pragma unroll
   for (int i = 0; i < MB; ++i) {
+    auto row_of = [&](uint32_t row) { return m0 + row / 32 * (TM / WM) + i * 32 + row % 32; };
+    // Where something is added and nothing else is done it is asked for before the barriers, all of it at once (one by one, each
+    // behind the last one's store, 8 products of 768 x 2048 x 2304 added to float gradients took 84 us).
+    float more[kVectors][8];
+    if (adds) {
+#pragma unroll
+      for (int u = 0; u < kVectors; ++u) {
+        const uint32_t v = thread + u * kThreads, m = row_of(v / (TN / 8)), n = n0 + v % (TN / 8) * 8;
+        if (m < a.m && n + 8 <= a.n) load_more<8>(a, w, m, n, more[u]);
+      }
+    }
     __syncthreads();
     char* const mine = lds + (wm * 32 + of32) * kImageRow + (wn * (TN / WN) + half * 4) * 4;
 #pragma unroll
@@ -423,8 +443,17 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
       for (int e = 0; e < 16; e += 4)
         *reinterpret_cast<float4v*>(mine + j * 128 + e * 8) = float4v{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
     __syncthreads();
-    auto row_of = [&](uint32_t row) { return m0 + row / 32 * (TM / WM) + i * 32 + row % 32; };
-    if (d.parts != nullptr || fours) {
+    if (adds) {
+#pragma unroll
+      for (int u = 0; u < kVectors; ++u) {
+        const uint32_t v = thread + u * kThreads, row = v / (TN / 8), col = v % (TN / 8) * 8, m = row_of(row), n = n0 + col;
+        if (m >= a.m || n >= a.n) continue;
+        const float4v* const from = reinterpret_cast<const float4v*>(lds + row * kImageRow + col * 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) more[u][e] += from[e / 4][e % 4];
+        store_numbers<8>(a.out, w * a.out_stride + m * a.out_ld + n, a.out_bf16, more[u]);
+      }
+    } else if (d.parts != nullptr || fours) {
       for (uint32_t v = thread; v < kImageRows * (TN / 8); v += kThreads) {
         const uint32_t row = v / (TN / 8), col = v % (TN / 8) * 8, m = row_of(row), n = n0 + col;
         if (m >= a.m || n >= a.n) continue;
