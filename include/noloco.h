@@ -473,7 +473,7 @@ typedef struct noloco_norm {
 
 /*
  * Plan for the layer norms of an arena's rows, with the workspace of noloco_layer_norm_gradient (one hipMalloc: sums of the
- * weights' gradients, 8 bytes for each element of the widest norm and up to 1024 groups of tokens, W workers).
+ * weights' gradients, 8 bytes for each element of the widest norm and each of up to 768 groups of tokens, one a worker at least).
  * Errors: NOLOCO_ERR_SEGMENT_OVERLAP (weight and bias of a norm share an element, or one leaves the row),
  * NOLOCO_ERR_INVALID_ARG, NOLOCO_ERR_ALIGNMENT, NOLOCO_ERR_UNSUPPORTED (width above 2^20, max_tokens above 2^27,
  * W * max_tokens above 2^31 - 1), NOLOCO_ERR_DEVICE.  On error *out is null.
@@ -526,10 +526,12 @@ typedef enum noloco_activation {
 } noloco_activation;
 
 /*
- * Plan for the matrices of an arena's rows, with a workspace (one hipMalloc) for gradients before the activation and for
- * sums that are taken in parts.  A gradient goes through the workers in batches that fit it.
- *   workspace_bytes  most bytes for the workspace; 0: 4 GiB.  Never more than all workers need at once, and never less than
- *                    one worker needs by itself (4 bytes for each of the largest layer's max_tokens x outputs, and less)
+ * Plan for the matrices of an arena's rows, with a workspace (one hipMalloc) for gradients before the activation, for operands
+ * that the matrix cores cannot take as they lie, and for sums that are taken in parts.  Calls go through the workers in batches
+ * that fit it.
+ *   workspace_bytes  most bytes for the workspace; 0: 1 GiB.  Never more than all workers need at once, and never less than
+ *                    one worker needs by itself (about 4 bytes for each number of the largest layer's dz, x and matrix); and up to
+ *                    64 MiB beside it for sums that are taken in parts
  * Errors: NOLOCO_ERR_SEGMENT_OVERLAP (a matrix and its own bias share an element, or one leaves the row),
  * NOLOCO_ERR_INVALID_ARG, NOLOCO_ERR_ALIGNMENT, NOLOCO_ERR_UNSUPPORTED (a side above 2^22; max_tokens above 2^24; matrix,
  * x or out of one worker of more than 2^30 numbers, row_stride counted), NOLOCO_ERR_DEVICE.  On error *out is null.
@@ -543,9 +545,11 @@ noloco_status noloco_linear_plan_destroy(noloco_linear_plan* plan);
  * z = x M + bias;  out = act(z) + residual
  *   residual   of out's type, [W][num_tokens][outputs], may be null (nothing is added) and may be out itself
  *   before     of out's type, [W][num_tokens][outputs]: z, which the gradient takes; may be null
- * How products take their operands goes by the result: for a bf16 result float operands are rounded to bf16; for a float
- * result they keep their 24 bits (three bf16 each, and the products of these that binary32 can tell).  Sums are binary32.
- * A NaN or an infinity in x or M makes NaN or infinite what depends on it.
+ * How products take their operands goes by the result and the sizes; sums are binary32.
+ *   bf16 result    beside a bf16 operand a float one is rounded to bf16, as the result is; two float ones to binary16 (11 bits) times
+ *                  a power of two of each worker.  In small products (some 10^9 multiplications and less) both keep 16 bits
+ *   float result   float operands keep 22 bits, or 2^-40 of the worker's largest number; in small products 24.  bf16 ones are whole
+ * A NaN or an infinity in x or M makes NaN or infinite what depends on it, and nothing else.
  */
 noloco_status noloco_linear(const noloco_linear_plan* plan, int32_t layer, const void* x, int32_t x_dtype, const void* theta,
                             int32_t theta_dtype, int64_t num_tokens, int32_t activation, const void* residual, void* before,
@@ -556,7 +560,8 @@ noloco_status noloco_linear(const noloco_linear_plan* plan, int32_t layer, const
  *   before     of dout's type, [W][num_tokens][outputs]: what noloco_linear left; may be null for NOLOCO_ACT_NONE
  *   add        of dx's type, [W][num_tokens][inputs], may be null (nothing is added) and may be dx itself
  *   dx, grad   either may be null: not computed.  x may be null where grad is
- * Products take their operands by the result's type as above; dz is rounded to bf16 only where a bf16 result takes it.
+ * Products take their operands as above, dz as a float one if there is an activation: a bf16 result of bf16 arrays alone takes
+ * it rounded to bf16.
  */
 noloco_status noloco_linear_gradient(const noloco_linear_plan* plan, int32_t layer, const void* dout, int32_t dout_dtype,
                                      const void* x, int32_t x_dtype, const void* theta, int32_t theta_dtype, int64_t num_tokens,

@@ -3,7 +3,8 @@
 //   n = log sum exp(l),  log_prob = l[token] - n,  entropy = -sum p log p with p = exp(l - n)
 //   dl[v] = dlog_prob ([v = token] - p[v]) - dentropy p[v] (log p[v] + entropy)
 //
-// Bound by memory: logits are read once each way.  A row is read in one pass with sums relative to a reference that
+// Bound by memory: logits are read once each way (8 x 1024 rows of 50257 bf16 151 us, 5.5 TB/s; their gradient, which is read and
+// written past the caches, 308, 5.3 TB/s; through them 327).  A row is read in one pass with sums relative to a reference that
 // follows the largest logit at a distance of at most 16 (exp of that times a row's length is far from binary32's range),
 // so that a new largest one hardly ever costs a correction.  Where one logit has most of the probability the sum is 1 and a rest,
 // and log(1 + rest) needs the rest's own digits: such a row is read a second time, from the caches, and only its rest is summed.
@@ -56,7 +57,9 @@ __device__ __forceinline__ RowEnd finish_row(const LogProbArgs& a, int64_t row, 
   return end;
 }
 
-// L threads take a part of a row; where that is a wave, four waves take four rows.  SPREAD: the entropy is asked for.
+// L threads take a part of a row; where that is a wave, four waves take four rows.  SPREAD: the entropy is asked for.  256 threads and
+// several rows on a CU rather than 1024 and two: a row's barriers then cost others nothing (319 us, so 151).  Few rows are cut
+// into parts of 4096 logits and more: four rows of 50257 with eight alternatives 7 us, and 5 for the join.
 template <typename E, int L, bool TOP, bool SPREAD>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs a) {
   constexpr int V = 16 / sizeof(E);          // logits of a load

@@ -116,7 +116,8 @@ constexpr int kSmallSums = 32 * kSmallRow;
 // 32 x 32 of the result by a workgroup, whose waves take blocks of 64 k in turn and add up their sums in the LDS (and
 // by several, where k is long and tiles are few).  Operands come
 // from memory to the registers as the matrix cores take them, without a barrier: a wave's loads for 64 k are on their way together.
-// What is read of an operand is read by every tile that needs it, which the caches bear in small products.
+// What is read of an operand is read by every tile that needs it, which the caches bear in small products: 4 x 256 x 96 x 192 float
+// 5.1 us, which is a launch's (through the LDS, a stage of 32 k after the other, 17.6); 1024 x 1024 x 1024 bf16 17, 126 TFLOP/s.
 template <typename TA, typename TB, bool ALONG_A, bool ALONG_B, int PA, int PB>
 __global__ __launch_bounds__(1024) void product_small(ProductArgs a, float* parts) {
   extern __shared__ __align__(16) float sums[];
@@ -308,6 +309,13 @@ template <bool F16> __device__ __forceinline__ float16v multiply(short8v a, shor
 // TM x TN of the result by WM x WN waves, each (TM / WM) x (TN / WN) in blocks of 32 x 32.  Operands come to the LDS past the registers,
 // STAGES stages of 64 k deep.  Fragments are read one slice of 16 k ahead of the products that use them, across the stage's end too:
 // the barrier in front of the last slice's products tells that the next stage has come and that this one's buffer is free.
+//
+// Tiles of 256 x 256 (eight waves, a CU to themselves) 1200 to 1300 TFLOP/s where they fill the chip several times (8192 x 8192 x
+// 8192 850 us; a large library product 1400 to 1460), of 128 x 128 (four, two workgroups a CU) 1040: what bounds them is the clock, which
+// falls to 1.76 to 1.92 of 2.4 GHz, and the stages' way to the LDS; the matrix cores are busy 60 % of its cycles.  (Reads held in front of
+// the slice's products by force, and four stages for a workgroup with a CU to itself, changed nothing.)  The end of a tile is not
+// hidden: 8 x 4096 x 2048 x 8192 takes 1013 us, with the activation and what stands before it 1180.  32 x 256 reads a matrix for a few tokens
+// as it streams, four stages deep: 2 x 16384 x 4096 44 us, 6.1 TB/s.
 template <int TM, int TN, int WM, int WN, bool ALONG_A, bool ALONG_B, bool F16, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, DirectArgs d) {
   constexpr int kWaves = WM * WN, kThreads = kWaves * 64, MB = TM / WM / 32, NB = TN / WN / 32, kSlices = 4;
