@@ -500,27 +500,34 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
   }
 }
 
-// The parts of a product whose k is shared out, in their order, and its end: a thread takes eight neighbouring numbers.
-__global__ __launch_bounds__(256) void product_join(ProductArgs a, DirectArgs d) {
-  const uint32_t wide = (a.n + 7) / 8;
-  const uint64_t v = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x, rows = static_cast<uint64_t>(a.W) * a.m;
+// Results of fewer vectors of eight are joined a number to a thread, others a vector. Few numbers want many waves, as their loads wait for each
+// other: whole products 3 x 119 x 7665 x 405 31.0 us against 33.8 in vectors, 100 x 5000 x 1001 22.4 and 25.1, 512 x 8192 x 2048 (131072
+// vectors) 36.8 and 37.3. Many want wide loads: 1024 x 8192 x 4096 (524288) 85.5 us against 81.4 in vectors.
+constexpr uint64_t kJoinVectors = 1 << 18;
+
+// The parts of a product whose k is shared out, in their order, and its end: a thread takes N neighbouring numbers.
+template <int N> __global__ __launch_bounds__(256) void product_join(ProductArgs a, DirectArgs d) {
+  const uint32_t wide = (a.n + N - 1) / N;
+  const uint64_t v = static_cast<uint64_t>(blockIdx.x) * blockDim.x + threadIdx.x, rows = static_cast<uint64_t>(a.W) * a.m;
   if (v >= rows * wide) return;
   const uint64_t row = v / wide, w = row / a.m;
-  const uint32_t n = static_cast<uint32_t>(v - row * wide) * 8, m = static_cast<uint32_t>(row - w * a.m);
-  float x[8] = {};
+  const uint32_t n = static_cast<uint32_t>(v - row * wide) * N, m = static_cast<uint32_t>(row - w * a.m);
+  float x[N] = {};
   const float* const from = d.parts + row * d.parts_ld + n;
 #pragma unroll 4
   for (uint32_t s = 0; s < d.splits; ++s) {
-    float part[8];
-    Stored<float, 8>::load(from + s * rows * d.parts_ld, part);
+    float part[N];
+    Stored<float, N>::load(from + s * rows * d.parts_ld, part);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] += part[e];
+    for (int e = 0; e < N; ++e) x[e] += part[e];
   }
-  if (n + 8 <= a.n && ends_in<8>(a)) {
-    finish<8>(a, w, m, n, x);
+  if constexpr (N == 1) {
+    finish<1>(a, w, m, n, x);
+  } else if (n + N <= a.n && ends_in<N>(a)) {
+    finish<N>(a, w, m, n, x);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < N; ++e)
       if (n + e < a.n) finish<1>(a, w, m, n + e, x + e);
   }
 }
@@ -654,8 +661,9 @@ int launch_product(const ProductArgs& args, const ProductPlan& plan, char* room,
   d.parts_ld = (args.n + 7) / 8 * 8;
   auto join = [&](int st) {
     if (st != 0 || d.splits == 1) return st;
-    const uint64_t vectors = static_cast<uint64_t>(args.W) * args.m * ((args.n + 7) / 8);
-    return enqueue(product_join, dim3(static_cast<uint32_t>((vectors + 255) / 256)), 256, 0, stream, args, d);
+    const uint64_t rows = static_cast<uint64_t>(args.W) * args.m, vectors = rows * ((args.n + 7) / 8);
+    if (vectors < kJoinVectors) return enqueue(product_join<1>, dim3(static_cast<uint32_t>((rows * args.n + 63) / 64)), 64, 0, stream, args, d);
+    return enqueue(product_join<8>, dim3(static_cast<uint32_t>((vectors + 255) / 256)), 256, 0, stream, args, d);
   };
   if (plan.tile == 0) return join(launch_small(args, plan.splits, d.parts, stream));
   PackArgs pack{};

@@ -228,6 +228,13 @@ def test_large_gradient(size, types):
     check_gradient(size, types, "none" if size[1] % 2 else "silu", with_add=size[1] % 2 == 0, accumulate=size[2] % 2 == 0)
 
 
+@pytest.mark.parametrize("types", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f32", "bf16", "bf16")], ids=str)
+@pytest.mark.parametrize("size", [(1, 1024, 4096, 2048, {}), (1, 1030, 4104, 2051, dict(gap=1))], ids=str)
+def test_large_linear_joined_in_vectors(size, types):
+    """Results of 2^18 vectors and more whose k is shared out, with and without rows that end within a vector."""
+    check_forward(size, types, "silu", with_residual=True)
+
+
 @pytest.mark.parametrize("types", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f32", "f32", "bf16")], ids=str)
 def test_large_products_keep_bad_numbers_to_their_row_and_column(types):
     layer = Layer(2, 712, 776)
