@@ -456,7 +456,7 @@ noloco_status noloco_embed_gradient(const noloco_embedding_plan* plan, const voi
  *   activations   device, float or bf16, 16-byte-aligned
  *   num_tokens    0 <= num_tokens <= max_tokens
  *   accumulate    0: gradients of weights are written, 1: added to what is there
- * Arithmetic is binary32, results are rounded once to their type.  Arrays that a call writes must not overlap any other one
+ * Arithmetic is binary32, results are rounded once to their type; operands of matrix products, see there.  Arrays that a call writes must not overlap any other one
  * of the call (NOLOCO_ERR_INVALID_ARG), but for those that an entry point names.  Calls are enqueued on hip_stream, not
  * synchronised, allocate and copy nothing and may be captured into a HIP graph.  A plan owns its workspace: calls that share
  * one must not overlap in time, replays of graphs among them.  Results are bit-identical from run to run.  The current
@@ -530,7 +530,7 @@ typedef enum noloco_activation {
  * that the matrix cores cannot take as they lie, and for sums that are taken in parts.  Calls go through the workers in batches
  * that fit it.
  *   workspace_bytes  most bytes for the workspace; 0: 1 GiB.  Never more than all workers need at once, and never less than
- *                    one worker needs by itself (about 4 bytes for each number of the largest layer's dz, x and matrix); and up to
+ *                    one worker needs by itself (4 bytes for each number of the largest layer's dz, and about 6 of dz, x and matrix); and up to
  *                    64 MiB beside it for sums that are taken in parts
  * Errors: NOLOCO_ERR_SEGMENT_OVERLAP (a matrix and its own bias share an element, or one leaves the row),
  * NOLOCO_ERR_INVALID_ARG, NOLOCO_ERR_ALIGNMENT, NOLOCO_ERR_UNSUPPORTED (a side above 2^22; max_tokens above 2^24; matrix,
@@ -545,10 +545,13 @@ noloco_status noloco_linear_plan_destroy(noloco_linear_plan* plan);
  * z = x M + bias;  out = act(z) + residual
  *   residual   of out's type, [W][num_tokens][outputs], may be null (nothing is added) and may be out itself
  *   before     of out's type, [W][num_tokens][outputs]: z, which the gradient takes; may be null
- * How products take their operands goes by the result and the sizes; sums are binary32.
- *   bf16 result    beside a bf16 operand a float one is rounded to bf16, as the result is; two float ones to binary16 (11 bits) times
- *                  a power of two of each worker.  In small products (some 10^9 multiplications and less) both keep 16 bits
- *   float result   float operands keep 22 bits, or 2^-40 of the worker's largest number; in small products 24.  bf16 ones are whole
+ * Sums are binary32.  What products keep of their operands goes by the types; which of two ways they go, and so whether it is more, by
+ * sizes, alignment and the workspace as well:
+ *   bf16 result    bf16 operands are whole.  A float one beside a bf16 one is rounded to bf16, as the result is; two float ones keep 11
+ *                  bits.  At best both cases keep 16
+ *   float result   float operands keep 22 bits, at best 24, bf16 ones are whole
+ * but for at most 2^-22 of the largest number among the 512 or fewer neighbours in its row that a number is packed with.  No other row
+ * costs a number digits, whatever it holds.
  * A NaN or an infinity in x or M makes NaN or infinite what depends on it, and nothing else.
  */
 noloco_status noloco_linear(const noloco_linear_plan* plan, int32_t layer, const void* x, int32_t x_dtype, const void* theta,
@@ -560,8 +563,7 @@ noloco_status noloco_linear(const noloco_linear_plan* plan, int32_t layer, const
  *   before     of dout's type, [W][num_tokens][outputs]: what noloco_linear left; may be null for NOLOCO_ACT_NONE
  *   add        of dx's type, [W][num_tokens][inputs], may be null (nothing is added) and may be dx itself
  *   dx, grad   either may be null: not computed.  x may be null where grad is
- * Products take their operands as above, dz as a float one if there is an activation: a bf16 result of bf16 arrays alone takes
- * it rounded to bf16.
+ * Products take their operands as above, dz as a float one if there is an activation.
  */
 noloco_status noloco_linear_gradient(const noloco_linear_plan* plan, int32_t layer, const void* dout, int32_t dout_dtype,
                                      const void* x, int32_t x_dtype, const void* theta, int32_t theta_dtype, int64_t num_tokens,

@@ -75,8 +75,8 @@ constexpr double kSmallWork = double(1 << 28);  // multiplications of all worker
 // How a product goes out, by its sizes and types alone (but for the alignment of its operands).  Offsets are into the workspace.
 struct ProductPlan {
   int32_t tile;               // 0: product_small, 256, 128, or 32 (32 x 256)
-  int32_t f16;                // operands packed to binary16 times powers of two
-  int32_t packed[2], parts[2];
+  int32_t f16;                // operands packed to binary16 times powers of two, or to bf16 parts where a worker's rows are too far apart
+  int32_t packed[2], parts[2];        // parts: that there is room for, as many bf16 as the result needs of the operand
   uint32_t splits;            // parts that k is shared out in
   uint64_t packed_at[2], largest_at, exponents_at, parts_at, bytes;      // bytes: of the workspace
 };
@@ -90,15 +90,20 @@ constexpr uint64_t kPartsRoom = 64 << 20;      // and for sums in parts, for all
 struct DirectArgs {
   const void *a, *b;          // 16-bit numbers, part 0 of worker 0
   int64_t a_worker, a_ld, a_part, b_worker, b_ld, b_part;
-  uint32_t a_parts, b_parts;  // two bits a segment: which part it takes
-  uint32_t segments, splits;
+  // [0]: of bf16 operands as they lie, or of binary16; [1]: of workers in bf16 parts
+  uint32_t a_parts[2], b_parts[2];    // two bits a segment: which part it takes
+  uint32_t segments[2], splits;
   uint32_t tiles_m, tiles_n, run;
-  const int32_t* exponents;   // [W][2]
+  const int32_t* exponents;   // [W][4]: of the two operands, and 1 where the worker is in bf16 parts
   float* parts;               // [splits][W][m][parts_ld], or null
   int64_t parts_ld;
 };
 
 constexpr int kPackParts = 256;
+// Of an operand packed to binary16 the largest number of every piece of a row, 512 numbers or what a row has left, is at least 2^-17 of the
+// worker's largest: then what binary16 leaves, 2^-39 of the latter, is 2^-22 of the piece's largest.
+constexpr uint32_t kPackPiece = 512;
+constexpr float kPackRange = 0x1p-17f;
 struct PackOperand {
   const void* p;
   void* out;                  // [parts][W][rows][wide rounded up to eight]; null: not packed
@@ -108,7 +113,7 @@ struct PackOperand {
 };
 struct PackArgs {
   PackOperand operand[2];
-  float* largest;             // [W][2][kPackParts]
+  float* largest;             // [W][2][2][kPackParts]: largest numbers, and the least of the rows' largest
   int32_t* exponents;
   int32_t f16, W;
 };

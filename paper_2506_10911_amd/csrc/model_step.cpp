@@ -246,8 +246,8 @@ uint64_t tiles_of(uint64_t v, uint64_t tile) { return (v + tile - 1) / tile; }
 }  // namespace
 
 uint64_t pack_bytes(int64_t m, int64_t n, int64_t k) {
-  auto most = [k](int64_t size) { return static_cast<uint64_t>(std::max(size * ((k + 7) / 8 * 8), k * ((size + 7) / 8 * 8))) * 4; };
-  return whole(most(m)) + whole(most(n)) + 4096;
+  auto most = [k](int64_t size) { return static_cast<uint64_t>(std::max(size * ((k + 7) / 8 * 8), k * ((size + 7) / 8 * 8))) * 6; };
+  return whole(most(m)) + whole(most(n)) + 2 * 2 * kPackParts * sizeof(float) + 1024;
 }
 
 // Estimates of a product's time, us, from which its way is chosen.
@@ -285,18 +285,19 @@ ProductPlan plan_product(const ProductArgs& args, uint64_t room) {
     const Operand& o = i == 0 ? args.a : args.b;
     const uint64_t size = i == 0 ? m : n, rows = o.along_k ? size : k, wide = tiles_of(o.along_k ? k : size, 8) * 8;
     plan.packed[i] = plan.f16 || !lies_well(o, args.k);
-    plan.parts[i] = plan.f16 && !args.out_bf16 && !o.bf16 ? 2 : 1;
+    plan.parts[i] = plan.f16 && !o.bf16 ? (args.out_bf16 ? 2 : 3) : 1;
     plan.packed_at[i] = at;
     if (!plan.packed[i]) continue;
     at += whole(W * rows * wide * 2 * plan.parts[i]);
-    moved += double(W) * rows * wide * ((o.bf16 ? 2 : 4) * (plan.f16 ? 2 : 1) + 2 * plan.parts[i]);
+    moved += double(W) * rows * wide * ((o.bf16 ? 2 : 4) * (plan.f16 ? 2 : 1) + (plan.parts[i] == 3 ? 4 : 2));
   }
   plan.largest_at = at;
-  at += plan.f16 ? whole(W * 2 * kPackParts * sizeof(float)) : 0;
+  at += plan.f16 ? whole(W * 2 * 2 * kPackParts * sizeof(float)) : 0;
   plan.exponents_at = at;
-  at += plan.f16 ? whole(W * 2 * sizeof(int32_t)) : 0;
+  at += plan.f16 ? whole(W * 4 * sizeof(int32_t)) : 0;
   plan.parts_at = at;
-  const uint64_t segments = plan.parts[0] + plan.parts[1] - 1, stages = tiles_of(k, 64) * segments, left = room > at ? room - at : 0;
+  // of binary16, which workers are nearly always in
+  const uint64_t segments = 1 + (plan.parts[0] == 3) + (plan.parts[1] == 3), stages = tiles_of(k, 64) * segments, left = room > at ? room - at : 0;
   const double packing = (moved > 0 ? 3 : 0) + (plan.f16 ? 3 : 0) + moved / 3.5e6;
   double best = of_small;
   ProductPlan chosen = small;

@@ -4,11 +4,16 @@
 //
 // Large products (product_direct) load bf16 operands past the registers to the LDS as they lie.  Others are packed first, to
 // rows that begin at multiples of 16 bytes:
-//   bf16 result, one float operand     that one rounded to bf16, which costs as much as the result's own rounding
+//   bf16 result, one float operand     that one rounded to bf16, which costs as much as the result's own rounding (0.0023 of the result's norm
+//                                      together, 0.0017 with the operand in two parts; but these are twice the products: dx of 8 x 2048 x
+//                                      768 x 2304 and its matrix's gradient 237 us in place of 179, of 2 x 4096 x 4096 x 16384 4098 of 2014)
 //   bf16 result, two float operands    both rounded to binary16 (11 bits), each times a power of two of its worker
 //   float result, float operands       a float one as a pair of binary16 (22 bits), a bf16 one as one, times powers of two; the
-//                                      products of two pairs but that of their low halves.  What a pair leaves of a number is
-//                                      2^-22 of it or 2^-40 of the operand's largest.
+//                                      products of two pairs but that of their low halves
+// What binary16 leaves of a number is 2^-39 of the operand's largest or less.  Where a piece of a row is so small that this is more than
+// 2^-22 of the piece's largest number (another row may hold anything, as padding does) the worker's operands are packed to bf16 parts
+// instead, whose range is binary32's: two for a bf16 result (16 bits), three for a float one (24), and the products of parts that
+// reach 2^-16 of the largest: 4 x 2048 x 2048 x 2048 float 400 us in place of 241, with a bf16 result 226 in place of 120.
 // Small products (product_small), which packing would make longer, take any operands from memory to the registers and a float one
 // apart into bf16: two of them, 16 bits, for a bf16 result; three, which together are the number, for a float one, and the products of
 // parts that reach 2^-16 of the largest.
@@ -336,7 +341,10 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
   const uint32_t high = d.tiles_m - group * 4 < 4 ? d.tiles_m - group * 4 : 4;
   const uint32_t m0 = (group * 4 + in % high) * TM, n0 = in / high * TN;
 
-  const uint32_t deep = (a.k + 63) / 64, all = deep * d.segments;
+  // the same in the whole workgroup: is the worker in bf16 parts?
+  const bool in_parts = F16 && uniform(static_cast<uint32_t>(d.exponents[4 * w + 2])) != 0;
+  const uint32_t a_parts = in_parts ? d.a_parts[1] : d.a_parts[0], b_parts = in_parts ? d.b_parts[1] : d.b_parts[0];
+  const uint32_t deep = (a.k + 63) / 64, all = deep * (in_parts ? d.segments[1] : d.segments[0]);
   const uint32_t s0 = static_cast<uint32_t>(static_cast<uint64_t>(all) * blockIdx.y / d.splits);
   const uint32_t stages = static_cast<uint32_t>(static_cast<uint64_t>(all) * (blockIdx.y + 1) / d.splits) - s0;
   A of_a;
@@ -347,8 +355,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
   const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_memory char*)lds));
   auto ask = [&] {
     const uint32_t to = lds_at + (asked & (STAGES - 1)) * kStage, k_left = a.k - stage_k * 64;
-    of_a.ask(d.a_parts >> segment * 2 & 3, stage_k, k_left, to, wave);
-    of_b.ask(d.b_parts >> segment * 2 & 3, stage_k, k_left, to + A::kBytes, wave);
+    of_a.ask(a_parts >> segment * 2 & 3, stage_k, k_left, to, wave);
+    of_b.ask(b_parts >> segment * 2 & 3, stage_k, k_left, to + A::kBytes, wave);
     ++asked;
     if (++stage_k == deep) {
       stage_k = 0;
@@ -386,7 +394,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
   Fragments even, odd;
   read(0, 0, even);
   // The stages behind the last one that is asked for by themselves, so that nothing in the loop is conditional.
-  auto stage = [&](uint32_t s, auto ask_more, auto read_next) {
+  auto stage = [&](uint32_t s, auto half, auto ask_more, auto read_next) {
 #pragma unroll
     for (int slice = 0; slice < kSlices; ++slice) {
       Fragments& now = slice & 1 ? odd : even;
@@ -403,18 +411,21 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
 #pragma unroll
       for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = multiply<F16>(now.b[j], now.a[i], acc[i][j]);
+        for (int j = 0; j < NB; ++j) acc[i][j] = multiply<decltype(half)::value>(now.b[j], now.a[i], acc[i][j]);
       // the products of a slice stay behind its reads, which the compiler would put in front of the next barrier
       if constexpr (TM == 256) __builtin_amdgcn_sched_barrier(0);
     }
   };
-  uint32_t s = 0;
-  for (; s + STAGES < stages; ++s) stage(s, Yes{}, Yes{});
-  for (; s + 1 < stages; ++s) stage(s, No{}, Yes{});
-  stage(s, No{}, No{});
+  auto all_stages = [&](auto half) {
+    uint32_t s = 0;
+    for (; s + STAGES < stages; ++s) stage(s, half, Yes{}, Yes{});
+    for (; s + 1 < stages; ++s) stage(s, half, No{}, Yes{});
+    stage(s, half, No{}, No{});
+  };
+  if (F16 && !in_parts) all_stages(std::bool_constant<F16>{}); else all_stages(std::false_type{});
 
-  if constexpr (F16) {
-    const int by = -(d.exponents[2 * w] + d.exponents[2 * w + 1]);
+  if (F16 && !in_parts) {
+    const int by = -(d.exponents[4 * w] + d.exponents[4 * w + 1]);
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -551,51 +562,100 @@ __device__ __forceinline__ void load_eight(const PackOperand& o, int64_t row_at,
   if (o.bf16) load(uint16_t{}); else load(float{});
 }
 
-// The largest finite number of what one of kPackParts workgroups takes of an operand.
+// The largest finite number of what one of kPackParts workgroups takes of an operand, and the least of its pieces' largest but those of zeros
+// alone: a wave takes a piece, a vector of eight a lane, or several short rows.  Four at a time, whose numbers are on their way together
+// (one by one 8192 x 512 x 2048 float took 6 us more).
 __global__ __launch_bounds__(256) void product_largest(PackArgs p) {
+  constexpr int kAhead = 4;
+  static_assert(kPackPiece == 64 * 8, "a vector of a lane");
   const PackOperand& o = p.operand[blockIdx.z];
-  if (o.out == nullptr) return;
   const int64_t w = blockIdx.y;
-  const uint32_t vectors = (o.wide + 7) / 8, all = o.rows * vectors;
-  float most = 0.f;
-  for (uint32_t v = blockIdx.x * 256 + threadIdx.x; v < all; v += kPackParts * 256) {
-    const uint32_t row = v / vectors;
-    float x[8];
-    load_eight(o, w * o.worker_stride + row * o.ld, (v - row * vectors) * 8, x);
+  const uint32_t vectors = (o.wide + 7) / 8, pieces = (vectors + 63) / 64, all = o.rows * pieces;
+  uint32_t lanes = 1;
+  while (lanes < 64 && lanes < vectors) lanes *= 2;
+  const uint32_t lane = threadIdx.x & (lanes - 1), at_once = 256 / lanes, apart = kPackParts * at_once;
+  const uint32_t rows_apart = apart / pieces, rest_apart = apart - rows_apart * pieces;
+  float most = 0.f, least = __builtin_inff();
+  uint32_t piece = blockIdx.x * at_once + threadIdx.x / lanes, row = piece / pieces, of_row = piece - row * pieces;
+  while (piece < all) {
+    float x[kAhead][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float size = fabsf(x[e]);
-      most = size < __builtin_inff() ? fmaxf(most, size) : most;
+    for (int i = 0; i < kAhead; ++i) {
+      const uint32_t v = of_row * 64 + lane;
+      if (piece < all && v < vectors) {
+        load_eight(o, w * o.worker_stride + row * o.ld, v * 8, x[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+      }
+      piece += apart;
+      row += rows_apart;
+      of_row += rest_apart;
+      if (of_row >= pieces) {
+        of_row -= pieces;
+        ++row;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      float here = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float size = fabsf(x[i][e]);
+        here = size < __builtin_inff() ? fmaxf(here, size) : here;
+      }
+      if (lanes == 64) {
+        here = wave_largest(here);
+      } else {
+        for (uint32_t k = 1; k < lanes; k *= 2) here = fmaxf(here, __shfl_xor(here, k));
+      }
+      most = fmaxf(most, here);
+      least = here > 0.f ? fminf(least, here) : least;
     }
   }
-#pragma unroll
-  for (int k = 32; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
-  __shared__ float waves[4];
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
+  most = wave_largest(most);
+  least = -wave_largest(-least);
+  __shared__ float waves[2][4];
+  if ((threadIdx.x & 63) == 0) {
+    waves[0][threadIdx.x >> 6] = most;
+    waves[1][threadIdx.x >> 6] = least;
+  }
   __syncthreads();
-  if (threadIdx.x == 0)
-    p.largest[(w * 2 + blockIdx.z) * kPackParts + blockIdx.x] = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+  if (threadIdx.x == 0) {
+    float* const to = p.largest + (w * 2 + blockIdx.z) * 2 * kPackParts + blockIdx.x;
+    to[0] = fmaxf(fmaxf(waves[0][0], waves[0][1]), fmaxf(waves[0][2], waves[0][3]));
+    to[kPackParts] = fminf(fminf(waves[1][0], waves[1][1]), fminf(waves[1][2], waves[1][3]));
+  }
 }
 
 // Rows of `wide` numbers to rows of a multiple of eight, zeros behind their ends: bf16, or one or two binary16 of the numbers times a power
-// of two that takes the largest of the worker's operand to between 2^14 and 2^15.
+// of two that takes the largest of the worker's operand to between 2^14 and 2^15, or `parts` bf16 where that leaves too little of a row.
 __global__ __launch_bounds__(256) void product_pack(PackArgs p) {
   const PackOperand& o = p.operand[blockIdx.z];
   if (o.out == nullptr) return;
   const int64_t w = blockIdx.y;
   int by = 0;
+  bool halves = p.f16;
   if (p.f16) {
     static_assert(kPackParts == 256, "four of a lane");
-    const float4v four = *reinterpret_cast<const float4v*>(p.largest + (w * 2 + blockIdx.z) * kPackParts + (threadIdx.x & 63) * 4);
-    float most = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
 #pragma unroll
-    for (int k = 32; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
-    if (most > 0.f) {
-      int power;
-      (void)frexpf(most, &power);      // most = 0.5 to 1 times 2^power
-      by = 15 - power;
+    for (int i = 0; i < 2; ++i) {
+      const float* const from = p.largest + (w * 2 + i) * 2 * kPackParts + (threadIdx.x & 63) * 4;
+      const float4v four = *reinterpret_cast<const float4v*>(from), rows = *reinterpret_cast<const float4v*>(from + kPackParts);
+      float most = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3])), least = fminf(fminf(rows[0], rows[1]), fminf(rows[2], rows[3]));
+      most = wave_largest(most);
+      least = -wave_largest(-least);
+      halves = halves && !(least < most * kPackRange);
+      if (i == blockIdx.z && most > 0.f) {
+        int power;
+        (void)frexpf(most, &power);      // most = 0.5 to 1 times 2^power
+        by = 15 - power;
+      }
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.exponents[w * 2 + blockIdx.z] = by;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      p.exponents[w * 4 + blockIdx.z] = by;
+      if (blockIdx.z == 0) p.exponents[w * 4 + 2] = halves ? 0 : 1;
+    }
   }
   const uint32_t vectors = (o.wide + 7) / 8, all = o.rows * vectors;
   uint16_t* const out = static_cast<uint16_t*>(o.out) + w * (all * 8ll);
@@ -603,20 +663,34 @@ __global__ __launch_bounds__(256) void product_pack(PackArgs p) {
     const uint32_t row = v / vectors;
     float x[8];
     load_eight(o, w * o.worker_stride + row * o.ld, (v - row * vectors) * 8, x);
+    auto store = [&](int part, const ushort8& eight) { *reinterpret_cast<ushort8*>(out + part * (p.W * (all * 8ll)) + v * 8ll) = eight; };
     ushort8 first, second;
+    if (halves) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (p.f16) {
+      for (int e = 0; e < 8; ++e) {
         const float y = ldexpf(x[e], by);
         const _Float16 high = static_cast<_Float16>(y);
         first[e] = __builtin_bit_cast(uint16_t, high);
         second[e] = __builtin_bit_cast(uint16_t, static_cast<_Float16>(y - static_cast<float>(high)));
-      } else {
-        first[e] = narrow(x[e]);
+      }
+      store(0, first);
+      if (o.parts == 3) store(1, second);
+    } else if (o.parts == 1) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) first[e] = narrow(x[e]);
+      store(0, first);
+    } else {
+      for (int part = 0; part < o.parts; ++part) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          // cut where the nearest bf16 is infinity: what is left is exact either way
+          first[e] = narrow(x[e]);
+          if ((first[e] & 0x7fff) == 0x7f80) first[e] = static_cast<uint16_t>(__float_as_uint(x[e]) >> 16);
+          x[e] -= widen(first[e]);
+        }
+        store(part, first);
       }
     }
-    *reinterpret_cast<ushort8*>(out + v * 8ll) = first;
-    if (o.parts == 2) *reinterpret_cast<ushort8*>(out + p.W * (all * 8ll) + v * 8ll) = second;
   }
 }
 
@@ -697,15 +771,18 @@ int launch_product(const ProductArgs& args, const ProductPlan& plan, char* room,
     if (st == 0) st = enqueue(product_pack, dim3(static_cast<uint32_t>(std::min<uint64_t>((most + 255) / 256, 4096)), args.W, 2), 256, 0, stream, pack);
     if (st != 0) return st;
   }
-  // the small products first: low high, high low, high high
-  d.segments = 1;
-  if (plan.parts[0] == 2 && plan.parts[1] == 2) {
-    d.segments = 3;
-    d.a_parts = 1;
-    d.b_parts = 1 << 2;
-  } else if (plan.parts[0] == 2 || plan.parts[1] == 2) {
-    d.segments = 2;
-    (plan.parts[0] == 2 ? d.a_parts : d.b_parts) = 1;
+  // the small products first: of the low halves, of the high ones; of bf16 parts, by what they reach
+  auto segment = [&](int way, uint32_t part_a, uint32_t part_b) {
+    d.a_parts[way] |= part_a << 2 * d.segments[way];
+    d.b_parts[way] |= part_b << 2 * d.segments[way]++;
+  };
+  if (plan.parts[0] == 3) segment(0, 1, 0);
+  if (plan.parts[1] == 3) segment(0, 0, 1);
+  segment(0, 0, 0);
+  if (plan.f16) {
+    for (int both = std::max(plan.parts[0], plan.parts[1]) - 1; both >= 0; --both)
+      for (int of_a = 0; of_a <= both; ++of_a)
+        if (of_a < plan.parts[0] && both - of_a < plan.parts[1]) segment(1, of_a, both - of_a);
   }
   d.exponents = pack.exponents;
   auto tiles = [&](uint32_t tm, uint32_t tn, uint32_t run) {

@@ -1,0 +1,30 @@
+"""The GPU tests of large products take the kernels that they are for: the host code that decides it is asked for their shapes."""
+import pytest
+
+import product_shapes as shapes
+from product_plans import plans
+
+
+def call(gradient, size, types, act=0, accumulate=False, more=False, room=0):
+    """As test_gpu_linear.Layer places a matrix."""
+    W, T, inputs, outputs, at = size
+    transposed, gap, cols = at.get("transposed", False), at.get("gap", 0), inputs if at.get("transposed") else outputs
+    row_stride = cols + at.get("apart", 0)
+    end = gap + (outputs if transposed else inputs) * row_stride
+    layer = (gap, inputs, outputs, end + (gap & 1) if at.get("bias", True) else -1, transposed, row_stride)
+    return dict(gradient=gradient, W=W, T=T, layer=layer, stride=-(-(end + outputs + 3) // 64) * 64, act=act, types=types, accumulate=accumulate,
+                more=more, room=room)
+
+
+@pytest.mark.parametrize("types", shapes.RANGE_TYPES, ids=str)
+def test_rows_far_apart_are_packed(types):
+    (_, products), = plans([call(False, shapes.RANGE, types)])
+    floats = types.count("f32") - (types[2] == "f32")
+    assert len(products) == 1 and products[0]["f16"] == 1 and products[0]["tile"] > 0
+    assert products[0]["parts"] == tuple((3 if types[2] == "f32" else 2) if t == "f32" else 1 for t in types[:2]) and floats >= 1
+
+
+@pytest.mark.parametrize("act", [0, 1])
+def test_padding_in_a_gradient_is_packed(act):
+    (_, products), = plans([call(True, shapes.RANGE, ("f32",) * 5, act)])
+    assert len(products) == 2 and all(p["f16"] == 1 and p["parts"] == (3, 3) and p["tile"] > 0 for p in products)
