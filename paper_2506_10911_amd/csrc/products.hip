@@ -675,15 +675,11 @@ __global__ __launch_bounds__(256) void product_pack(PackArgs p) {
       }
       store(0, first);
       if (o.parts == 3) store(1, second);
-    } else if (o.parts == 1) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) first[e] = narrow(x[e]);
-      store(0, first);
     } else {
       for (int part = 0; part < o.parts; ++part) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          // cut where the nearest bf16 is infinity: what is left is exact either way
+          // cut where the nearest bf16 is infinity, which a zero would make NaN: what is left is exact either way
           first[e] = narrow(x[e]);
           if ((first[e] & 0x7fff) == 0x7f80) first[e] = static_cast<uint16_t>(__float_as_uint(x[e]) >> 16);
           x[e] -= widen(first[e]);

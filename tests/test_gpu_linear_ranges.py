@@ -92,3 +92,22 @@ def test_bad_numbers_beside_rows_far_apart(types):
     assert not got[bad].isfinite().any() and got[~bad].isfinite().all()
     exact = (x[0, 60].double() @ layer.matrix(a)[0].double())
     assert ((got[0, 60].double() - exact).abs() <= 2 * plain.STORED[out] * exact.abs() + 2.0 ** -15 * exact.abs() * (out == torch.bfloat16) + 16 * plain.U * exact.abs()).all()
+
+
+def test_lowest_numbers_that_meet_zeros():
+    """A float operand beside a bf16 one, rounded to bf16: binary32's lowest number, nearest to -infinity, has to stay finite."""
+    W, T, inputs, outputs, more = shapes.RANGE
+    layer = Layer(W, inputs, outputs, **more)
+    lowest = torch.finfo(torch.float32).min
+    a, x, dout = layer.array(torch.bfloat16, std=0.3), randn((W, T, inputs), 2), randn((W, T, outputs), 3, torch.bfloat16)
+    x[0, 5::50] = lowest
+    dout[0, 5::50] = 0
+    _, grad = backward(layer, layer.plan(T), dout, x, a, "none", None, None, torch.bfloat16, a, False)
+    exact, bound = plain.product(x.mT, dout, torch.bfloat16)
+    within(layer.matrix(grad), exact, bound + plain.STORED[torch.bfloat16] * exact.abs())
+    a, x = layer.array(torch.float32, std=0.3), randn((W, T, inputs), 2, torch.bfloat16)
+    layer.matrix(a)[0, 11] = lowest
+    x[0, :, 11] = 0
+    got, _ = forward(layer, layer.plan(T), x, a, "none", None, torch.bfloat16, before=False)
+    exact, bound = plain.product(x, layer.matrix(a), torch.bfloat16)
+    within(got, exact, bound + plain.STORED[torch.bfloat16] * exact.abs())

@@ -28,3 +28,9 @@ def test_rows_far_apart_are_packed(types):
 def test_padding_in_a_gradient_is_packed(act):
     (_, products), = plans([call(True, shapes.RANGE, ("f32",) * 5, act)])
     assert len(products) == 2 and all(p["f16"] == 1 and p["parts"] == (3, 3) and p["tile"] > 0 for p in products)
+
+
+def test_lowest_numbers_are_rounded_to_bf16():
+    (_, of_gradient), (_, of_forward) = plans([call(True, shapes.RANGE, ("bf16", "f32", "bf16", "bf16", "bf16")), call(False, shapes.RANGE, ("bf16", "f32", "bf16"))])
+    for p, which in ((of_gradient[1], 0), (of_forward[0], 1)):
+        assert p["tile"] > 0 and p["f16"] == 0 and p["packed"][which] == 1 and p["parts"] == (1, 1)
