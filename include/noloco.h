@@ -552,7 +552,7 @@ noloco_status noloco_linear_plan_destroy(noloco_linear_plan* plan);
  *   float result   float operands keep 22 bits, at best 24, bf16 ones are whole
  * but for at most 2^-22 of the largest number among the 512 or fewer neighbours in its row that a number is packed with.  No other row
  * costs a number digits, whatever it holds.
- * A NaN or an infinity in x or M makes NaN or infinite what depends on it, and nothing else.
+ * A NaN or an infinity in x or M makes NaN or infinite the z that it enters, and no other.  act and act' of an infinite z are their limits.
  */
 noloco_status noloco_linear(const noloco_linear_plan* plan, int32_t layer, const void* x, int32_t x_dtype, const void* theta,
                             int32_t theta_dtype, int64_t num_tokens, int32_t activation, const void* residual, void* before,
