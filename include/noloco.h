@@ -575,7 +575,9 @@ noloco_status noloco_linear_gradient(const noloco_linear_plan* plan, int32_t lay
 
 /*
  * Plan for logits [W][max_tokens][row_stride], of which the first `vocab` of a row count (the rest is neither read nor
- * written), with the workspace of noloco_token_log_probs (one hipMalloc, a few MB).
+ * written), with the workspace of noloco_token_log_probs: one hipMalloc of 16 + 8 max_top bytes for each of 512 parts of rows at most,
+ * or, of a vocabulary above 65536, for each 65536 logits of all W * max_tokens rows where that is more (18 MB for 32768 rows of 128256 and
+ * 32 alternatives).
  *   max_top  most alternatives that a call asks for, up to NOLOCO_MAX_TOP (NOLOCO_ERR_UNSUPPORTED beyond)
  * Errors: NOLOCO_ERR_INVALID_ARG (row_stride < vocab among them), NOLOCO_ERR_UNSUPPORTED (vocab above 2^24, W * max_tokens
  * above 2^31 - 1, or W * max_tokens * row_stride above 2^60), NOLOCO_ERR_DEVICE.  On error *out is null.
@@ -612,6 +614,8 @@ noloco_status noloco_token_log_probs(const noloco_log_prob_plan* plan, const voi
  *   dlogits          device, [W][num_tokens][row_stride] float or bf16, 16-byte-aligned; may be logits itself where the types
  *                    agree.  Elements behind vocab are left as they are
  * A row whose norm is -infinity has a gradient of zeros, and so has padding where dentropy is null.
+ * p is exp(l - n) with the n that is given: its rounding to binary32, up to |n| 2^-24, is an error of all of the row's p.  Of a row of finite
+ * logits around -1e9, or of the type's lowest number alone, that leaves nothing right; -infinity masks without it.
  */
 noloco_status noloco_token_log_probs_gradient(const noloco_log_prob_plan* plan, const void* logits, int32_t logits_dtype,
                                               const void* tokens, int32_t token_type, int64_t num_tokens, const float* norms,

@@ -288,6 +288,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void log_probs_part(LogProbArgs 
 }
 
 // A row's parts together, a workgroup a row: the first part that has the largest logit gives its rest, the others all of their sum.
+// Rows in parts have more logits than there are alternatives, so that each place is some key's.
 constexpr uint32_t kJoinKeys = 1024;
 __global__ __launch_bounds__(256) void log_probs_join(LogProbArgs a) {
   __shared__ uint64_t near[kJoinKeys];
@@ -347,11 +348,6 @@ __global__ __launch_bounds__(256) void log_probs_join(LogProbArgs a) {
       if (larger >= top) continue;
       a.top_tokens[row * top + larger] = static_cast<int32_t>(~static_cast<uint32_t>(k));
       a.top_log_probs[row * top + larger] = end.log_prob(logit_of(k));
-    }
-    // a vocabulary has as many keys as tokens, or `top` of each of its parts: only one that is smaller leaves places
-    for (uint32_t c = a.vocab + threadIdx.x; c < top; c += 256) {
-      a.top_tokens[row * top + c] = -1;
-      a.top_log_probs[row * top + c] = -kInfinity;
     }
     __syncthreads();
   }
