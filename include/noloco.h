@@ -530,8 +530,8 @@ typedef enum noloco_activation {
  * that the matrix cores cannot take as they lie, and for sums that are taken in parts.  Calls go through the workers in batches
  * that fit it.
  *   workspace_bytes  most bytes for the workspace; 0: 1 GiB.  Never more than all workers need at once, and never less than
- *                    one worker needs by itself (4 bytes for each number of the largest layer's dz, and about 6 of dz, x and matrix); and up to
- *                    64 MiB beside it for sums that are taken in parts
+ *                    one worker needs by itself (4 bytes for each number of the largest layer's dz, and about 6 of dz, x and matrix); beside it up to
+ *                    64 MiB for sums that are taken in parts, where max_tokens and the layers ask for any
  * Errors: NOLOCO_ERR_SEGMENT_OVERLAP (a matrix and its own bias share an element, or one leaves the row),
  * NOLOCO_ERR_INVALID_ARG, NOLOCO_ERR_ALIGNMENT, NOLOCO_ERR_UNSUPPORTED (a side above 2^22; max_tokens above 2^24; matrix,
  * x or out of one worker of more than 2^30 numbers, row_stride counted), NOLOCO_ERR_DEVICE.  On error *out is null.

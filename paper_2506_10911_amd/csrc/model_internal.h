@@ -85,7 +85,9 @@ struct ProductPlan {
 ProductPlan plan_product(const ProductArgs& args, uint64_t room);
 // Most bytes that packing a product takes for each worker, whatever its types.
 uint64_t pack_bytes(int64_t m, int64_t n, int64_t k);
-constexpr uint64_t kPartsRoom = 64 << 20;      // and for sums in parts, for all workers
+// And for sums in parts, for all workers, whatever the types and for any fewer workers and smaller sizes; never more than kPartsRoom.
+uint64_t parts_bytes(int64_t W, int64_t m, int64_t n, int64_t k);
+constexpr uint64_t kPartsRoom = 64 << 20;
 
 struct DirectArgs {
   const void *a, *b;          // 16-bit numbers, part 0 of worker 0

@@ -250,6 +250,13 @@ uint64_t pack_bytes(int64_t m, int64_t n, int64_t k) {
   return whole(most(m)) + whole(most(n)) + 2 * 2 * kPackParts * sizeof(float) + 1024;
 }
 
+uint64_t parts_bytes(int64_t W, int64_t m, int64_t n, int64_t k) {
+  const uint64_t part = static_cast<uint64_t>(W) * m * (tiles_of(n, 8) * 8) * sizeof(float), rounds = tiles_of(k, 1024);
+  // as plan_product shares k out: small products in up to 1024 workgroups' tiles, others eight stages each of up to three segments
+  const uint64_t small = rounds > 2 ? std::min<uint64_t>(rounds, 32) : 0, direct = std::min<uint64_t>(tiles_of(k, 64) * 3 / 8, 32);
+  return std::max(std::min<uint64_t>(small * part, 1024 * 32 * 32 * sizeof(float)), direct > 1 ? std::min(direct * part, kPartsRoom) : 0);
+}
+
 // Estimates of a product's time, us, from which its way is chosen.
 //   small    tiles of 32 x 32 that read their operands from the caches at 8 TB/s together (5 where these are larger,
 //            half where vectors lie across lines): 4 x 512 x
@@ -370,8 +377,9 @@ extern "C" noloco_status noloco_linear_plan_create(const noloco_linear_layer* la
     st = check_layer(l, worker_stride, max_tokens);
     if (st != NOLOCO_OK) return st;
     one = std::max(one, dz_bytes(l, max_tokens) + sums_bytes(l, max_tokens) + packed_bytes(l, max_tokens));
-    const double numbers = double(W) * std::max({double(max_tokens) * l.inputs, double(max_tokens) * l.outputs, double(l.inputs) * l.outputs});
-    parts = std::max(parts, static_cast<uint64_t>(std::min(numbers * 32 * sizeof(float), double(noloco::kPartsRoom))));
+    const int64_t sides[2] = {l.inputs, l.outputs};
+    for (int i = 0; i < 2; ++i)
+      parts = std::max({parts, noloco::parts_bytes(W, max_tokens, sides[i], sides[1 - i]), noloco::parts_bytes(W, sides[i], sides[1 - i], max_tokens)});
   }
   try {
     std::unique_ptr<noloco_linear_plan> plan(new noloco_linear_plan);
