@@ -59,3 +59,48 @@ def test_room_for_parts_that_calls_make():
     size = (2, 1, 16384, 4096, {})
     (room, products), = plans([call(False, size, ("bf16",) * 3)])
     assert products[0]["splits"] >= 8 and room <= _without_parts(*size[:4]) + 32 * 2 * 16384 * 4
+
+
+def _ways(calls):
+    return [p for _, products in plans(calls) for p in products]
+
+
+def test_large_shapes_take_every_kernel():
+    forward = _ways([call(False, *case) for case in shapes.FORWARD])
+    gradient = _ways([call(True, size, types) for size in shapes.GRADIENT_SIZES for types in shapes.GRADIENT_TYPES])
+    gradient += _ways([call(True, shapes.GRADIENT_SIZES[0], shapes.MIXED)])
+    ways = forward + gradient
+    assert all(p["tile"] > 0 for p in ways)
+    taken = {(p["tile"], p["along"], p["f16"]) for p in ways}
+    layouts = [(tile, along) for tile in (128, 256) for along in ((1, 0), (1, 1), (0, 0))] + [(32, (1, 0)), (32, (1, 1))]
+    assert taken == {(*layout, f16) for layout in layouts for f16 in (0, 1)}
+    # more stages of 64 than are under way at first, in every part of k; shared out and not
+    assert all(-(-p["k"] // 64) / p["splits"] > (4 if p["tile"] == 32 else 2) for p in ways)
+    assert {(p["tile"], p["splits"] > 1) for p in ways} == {(tile, shared) for tile in (32, 128, 256) for shared in (False, True)}
+    assert {p["parts"] for p in ways if p["f16"]} == {(3, 3), (3, 1), (1, 3), (2, 2)}
+    assert any(p["tile"] == 256 and p["W"] > 1 for p in ways)
+    assert {(p["tile"], p["end"]) for p in ways if p["splits"] == 1} >= {(128, 8), (128, 4), (128, 1), (256, 8), (256, 1), (32, 8)}
+    # operands that are packed beside ones that are read as they lie
+    assert {p["packed"] for p in ways if not p["f16"]} == {(0, 0), (0, 1), (1, 0), (1, 1)}
+
+
+def test_added_gradients_take_the_end_that_adds():
+    ways = _ways([call(True, size, types, accumulate=True, more=True) for size in shapes.GRADIENT_SIZES for types in shapes.GRADIENT_TYPES])
+    assert {(p["tile"], p["f16"]) for p in ways if p["adds"]} >= {(256, 0), (256, 1), (128, 0)}
+    assert {p["end"] for p in ways if not p["adds"] and p["splits"] == 1} == {1, 4, 8}
+    # parts joined a number to a thread and in vectors
+    vectors = {p["W"] * p["m"] * -(-p["n"] // 8) >= 1 << 18 for p in ways if p["splits"] > 1}
+    assert vectors == {False, True}
+
+
+@pytest.mark.parametrize("room", shapes.BATCH_ROOMS)
+@pytest.mark.parametrize("types", shapes.BATCH_TYPES, ids=str)
+def test_batches_of_workers_share_the_workspace(types, room):
+    ways = _ways([call(True, shapes.BATCHES, types, act=4, room=room)])
+    assert len(ways) > 2 and max(p["W"] for p in ways) < shapes.BATCHES[0] and all(p["tile"] > 0 and p["f16"] == 1 for p in ways)
+
+
+@pytest.mark.parametrize("types", [shapes.WHOLE, shapes.FLOAT, shapes.SINGLE], ids=str)
+def test_bad_numbers_are_packed_as_floats(types):
+    p, = _ways([call(False, shapes.RANGE, types)])
+    assert p["tile"] > 0 and p["f16"] == (types != shapes.WHOLE)
