@@ -102,7 +102,7 @@ struct DirectArgs {
 };
 
 constexpr int kPackParts = 256;
-// Of an operand packed to binary16 the largest number of every piece of a row, 512 numbers or what a row has left, is at least 2^-17 of the
+// Of an operand packed to binary16 the largest number of every 512 neighbours of a row, or of a whole shorter one, is at least 2^-17 of the
 // worker's largest: then what binary16 leaves, 2^-39 of the latter, is 2^-22 of the piece's largest.
 constexpr uint32_t kPackPiece = 512;
 constexpr float kPackRange = 0x1p-17f;

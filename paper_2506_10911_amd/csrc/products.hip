@@ -564,7 +564,7 @@ __device__ __forceinline__ void load_eight(const PackOperand& o, int64_t row_at,
 
 // The largest finite number of what one of kPackParts workgroups takes of an operand, and the least of its pieces' largest but those of zeros
 // alone: a wave takes a piece, a vector of eight a lane, or several short rows.  Four at a time, whose numbers are on their way together
-// (one by one 8192 x 512 x 2048 float took 6 us more).
+// (one by one 8192 x 512 x 2048 float took 6 us more).  A row's last piece begins within the one before it: a number by itself may well be small.
 __global__ __launch_bounds__(256) void product_largest(PackArgs p) {
   constexpr int kAhead = 4;
   static_assert(kPackPiece == 64 * 8, "a vector of a lane");
@@ -581,7 +581,7 @@ __global__ __launch_bounds__(256) void product_largest(PackArgs p) {
     float x[kAhead][8];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const uint32_t v = of_row * 64 + lane;
+      const uint32_t v = min(of_row * 64, vectors - min(vectors, 64u)) + lane;
       if (piece < all && v < vectors) {
         load_eight(o, w * o.worker_stride + row * o.ld, v * 8, x[i]);
       } else {
