@@ -20,7 +20,7 @@ __device__ __forceinline__ void put_bias(const SlopeArgs& a, int64_t w, uint32_t
 
 // A workgroup takes 64 N columns of a group of tokens; its waves (four, or sixteen where there is one group) take the tokens in turn, a
 // few at a time whose numbers are on their way together.  Bound by memory, with an activation nearly as much by its slope's instructions: 2 x 4096 x 16384 through the
-// normal distribution's 181 us (4.5 TB/s).
+// normal distribution's 167 us (4.8 TB/s).
 template <typename E, typename Z, int N, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void linear_slope(SlopeArgs a) {
   constexpr int kAhead = N == 8 ? 2 : 4;

@@ -17,7 +17,8 @@ constexpr int64_t kNormGradientHeld = 8192; // and in the gradient, with as many
 constexpr int64_t kNormRows = 4;            // rows that a workgroup works on at once, at most
 
 // Workgroups of a worker: each takes every `groups`th set of rows and leaves one sum of the weights' gradients.  768 in all: the
-// gradient's registers let three share a CU, and with 1024 the last of them ran alone (2 x 8192 rows of 4096 97 us, so 91).
+// gradient's registers let three share a CU, and with 1024 the last of them ran alone (2 x 8192 rows of 4096 97 us, so 91).  Rows that
+// no workgroup holds: 64, so that the sums of the widest take 512 MB at most, with a quarter of the chip at work.
 inline uint32_t norm_groups(int64_t tokens, int64_t W, int64_t width) {
   const int64_t most = std::max<int64_t>(1, (width > kNormGradientHeld ? 64 : 768) / W);
   return static_cast<uint32_t>(std::max<int64_t>(1, std::min((tokens + kNormRows - 1) / kNormRows, most)));

@@ -264,8 +264,9 @@ uint64_t parts_bytes(int64_t W, int64_t m, int64_t n, int64_t k) {
 //   direct   stages of 64 k: in tiles of 128 0.85 us each with one workgroup on a CU (2048 x 2048 x 2048 33 us), 0.52 with two (2 of
 //            them 39), of 256 1.1, and 1.6 where the chip is full (8 x 4096 x 2048 x 8192 1013 us, in tiles of 128 1237); 32 rows 0.4 us or
 //            what reading the matrix takes; packing and joining by what they move, and 3 us a launch
-// Both sides where they meet: 1024 x 1024 x 1024 bf16 17.5 and 16.2 us, float 30.8 and 33.4; 64 x 4096 x 4096 bf16 24 and 16, float
-// 28 and 110; one token through 4096 x 4096 14.5 and 10.2; 2 x 128 x 1024 x 1024 7.7 and 12.3.
+// Both sides where they meet, small and direct: 64 x 4096 x 4096 bf16 31 and 16 us, float 36 and 65; one token through 4096 x 4096 16
+// and 10, float 18 and 60; 2 x 128 x 1024 x 1024 7.3 and 12.3, float 9.6 and 29.5; 1024 x 1024 x 1024 float 30 and 32.  In bf16 the
+// estimates take the slower one there, 20.6 and 18.4, and for 2 x 2456 x 6912 x 32, 26 and 20: the rate of the caches is cruder than it is.
 ProductPlan plan_product(const ProductArgs& args, uint64_t room) {
   ProductPlan plan{};
   plan.parts[0] = plan.parts[1] = 1;

@@ -315,12 +315,12 @@ template <bool F16> __device__ __forceinline__ float16v multiply(short8v a, shor
 // STAGES stages of 64 k deep.  Fragments are read one slice of 16 k ahead of the products that use them, across the stage's end too:
 // the barrier in front of the last slice's products tells that the next stage has come and that this one's buffer is free.
 //
-// Tiles of 256 x 256 (eight waves, a CU to themselves) 1200 to 1300 TFLOP/s where they fill the chip several times (8192 x 8192 x
-// 8192 850 us; a large library product 1400 to 1460), of 128 x 128 (four, two workgroups a CU) 1040: what bounds them is the clock, which
-// falls to 1.76 to 1.92 of 2.4 GHz, and the stages' way to the LDS; the matrix cores are busy 60 % of its cycles.  (Reads held in front of
-// the slice's products by force, and four stages for a workgroup with a CU to itself, changed nothing.)  The end of a tile is not
-// hidden: 8 x 4096 x 2048 x 8192 takes 1013 us, with the activation and what stands before it 1180.  32 x 256 reads a matrix for a few tokens
-// as it streams, four stages deep: 2 x 16384 x 4096 44 us, 6.1 TB/s.
+// Tiles of 256 x 256 (eight waves, a CU to themselves) 1070 to 1280 TFLOP/s where they fill the chip several times (8192 x 8192 x
+// 8192 859 us; a large library product 1400 to 1460), of 128 x 128 (four, two workgroups a CU) 1040.  The matrix cores are busy 60 % of
+// the cycles at 1.75 to 1.87 of 2.4 GHz, the LDS 25 %: a wave waits for its stage and the barrier for 30 to 41 % of its cycles, which nothing else
+// on the CU covers.  (Reads held in front of the slice's products by force, and four stages for a workgroup with a CU to itself, changed
+// nothing.)  The end of a tile is not hidden either: 8 x 4096 x 2048 x 8192 takes 1027 us, with the activation and what stands before
+// it 1175.  32 x 256 reads a matrix for a few tokens as it streams, four stages deep: 2 x 16384 x 4096 44 us, 6.1 TB/s.
 template <int TM, int TN, int WM, int WN, bool ALONG_A, bool ALONG_B, bool F16, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, DirectArgs d) {
   constexpr int kWaves = WM * WN, kThreads = kWaves * 64, MB = TM / WM / 32, NB = TN / WN / 32, kSlices = 4;

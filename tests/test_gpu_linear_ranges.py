@@ -5,7 +5,7 @@ import torch
 
 import model_plain as plain
 import product_shapes as shapes
-from test_gpu_linear import DTYPES, Layer, backward, forward, randn, within
+from test_gpu_linear import DTYPES, Layer, backward, code, forward, nl, randn, same_bits, within
 
 pytestmark = pytest.mark.gpu
 
@@ -111,3 +111,33 @@ def test_lowest_numbers_that_meet_zeros():
     got, _ = forward(layer, layer.plan(T), x, a, "none", None, torch.bfloat16, before=False)
     exact, bound = plain.product(x, layer.matrix(a), torch.bfloat16)
     within(got, exact, bound + plain.STORED[torch.bfloat16] * exact.abs())
+
+
+@pytest.mark.parametrize("types", shapes.RANGE_TYPES[::3], ids=str)
+def test_captured_and_replayed_with_rows_near_and_far(types):
+    """One graph, whose operands' rows lie near each other and far apart in turn, eager calls between."""
+    W, T, inputs, outputs, more = shapes.RANGE
+    layer = Layer(W, inputs, outputs, **more)
+    x_type, theta_type, out_type = (DTYPES[t] for t in types)
+    a = layer.array(theta_type, std=0.3)
+    plan, theta, x = layer.plan(T), a.cuda(), randn((W, T, inputs), 2, x_type).cuda()
+    out = torch.empty((W, T, outputs), dtype=out_type, device="cuda")
+    step = lambda: nl.linear(plan, 1, x, code(x), theta, code(theta), T, out, code(out))  # noqa: E731
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for replay, how in enumerate(("", "one huge", "", "falling")):
+        host = rows_apart(randn((W, T, inputs), 10 + replay), how).to(x_type)
+        x.copy_(host)
+        step()
+        torch.cuda.synchronize()
+        want = out.clone()
+        for _ in range(2):
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert same_bits(out, want)
+        if how:
+            check_product(out.cpu(), host, layer.matrix(a), out_type)
