@@ -341,16 +341,17 @@ __global__ __launch_bounds__(WM * WN * 64) void product_direct(ProductArgs a, Di
   const uint32_t high = d.tiles_m - group * 4 < 4 ? d.tiles_m - group * 4 : 4;
   const uint32_t m0 = (group * 4 + in % high) * TM, n0 = in / high * TN;
 
-  // the same in the whole workgroup: is the worker in bf16 parts?
-  const bool in_parts = F16 && uniform(static_cast<uint32_t>(d.exponents[4 * w + 2])) != 0;
-  const uint32_t a_parts = in_parts ? d.a_parts[1] : d.a_parts[0], b_parts = in_parts ? d.b_parts[1] : d.b_parts[0];
-  const uint32_t deep = (a.k + 63) / 64, all = deep * (in_parts ? d.segments[1] : d.segments[0]);
-  const uint32_t s0 = static_cast<uint32_t>(static_cast<uint64_t>(all) * blockIdx.y / d.splits);
-  const uint32_t stages = static_cast<uint32_t>(static_cast<uint64_t>(all) * (blockIdx.y + 1) / d.splits) - s0;
+  // is the worker in bf16 parts?  Asked for before the operands' places are made
+  const int32_t parts_flag = F16 ? d.exponents[4 * w + 2] : 0;
   A of_a;
   B of_b;
   of_a.open(d.a, w * d.a_worker, d.a_ld, d.a_part, m0, a.m, lane, wave);
   of_b.open(d.b, w * d.b_worker, d.b_ld, d.b_part, n0, a.n, lane, wave);
+  const bool in_parts = F16 && uniform(static_cast<uint32_t>(parts_flag)) != 0;
+  const uint32_t a_parts = in_parts ? d.a_parts[1] : d.a_parts[0], b_parts = in_parts ? d.b_parts[1] : d.b_parts[0];
+  const uint32_t deep = (a.k + 63) / 64, all = deep * (in_parts ? d.segments[1] : d.segments[0]);
+  const uint32_t s0 = static_cast<uint32_t>(static_cast<uint64_t>(all) * blockIdx.y / d.splits);
+  const uint32_t stages = static_cast<uint32_t>(static_cast<uint64_t>(all) * (blockIdx.y + 1) / d.splits) - s0;
   uint32_t segment = s0 / deep, stage_k = s0 - segment * deep, asked = 0;
   const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_memory char*)lds));
   auto ask = [&] {
@@ -562,69 +563,113 @@ __device__ __forceinline__ void load_eight(const PackOperand& o, int64_t row_at,
   if (o.bf16) load(uint16_t{}); else load(float{});
 }
 
+// The largest size among eight numbers, as the bits of a float: sizes are in the order of their bits, above all of them infinities and NaN, which
+// count as zeros.
+template <typename E> __device__ __forceinline__ uint32_t largest_of(const Eight<E>& eight) {
+  constexpr uint32_t kInfinite = 0x7f800000u;
+  uint32_t most = 0;
+  if constexpr (sizeof(E) == 2) {
+    ushort8 sizes;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sizes[e] = eight.v[e] & 0x7fff;
+    const auto four = __builtin_elementwise_max(sizes.lo, sizes.hi);
+    const auto two = __builtin_elementwise_max(four.lo, four.hi);
+    most = static_cast<uint32_t>(max(two[0], two[1])) << 16;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(eight.v[e]) & 0x7fffffffu);
+  }
+  if (most >= kInfinite) {
+    most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t size = (sizeof(E) == 2 ? static_cast<uint32_t>(eight.v[e]) << 16 : __builtin_bit_cast(uint32_t, static_cast<float>(eight.v[e]))) & 0x7fffffffu;
+      most = size < kInfinite ? max(most, size) : most;
+    }
+  }
+  return most;
+}
+template <int CONTROL> __device__ __forceinline__ uint32_t larger(uint32_t v) {
+  return max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CONTROL, 15, 15, true)));
+}
+__device__ __forceinline__ uint32_t lane_bits(uint32_t v, int lane) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), lane)); }
+// Over the wave, in scalar registers from the sixteens on.
+__device__ __forceinline__ uint32_t wave_largest_bits(uint32_t v) {
+  v = larger<0x140>(larger<0x141>(larger<0x4E>(larger<0xB1>(v))));
+  return max(max(lane_bits(v, 0), lane_bits(v, 16)), max(lane_bits(v, 32), lane_bits(v, 48)));
+}
+
 // The largest finite number of what one of kPackParts workgroups takes of an operand, and the least of its pieces' largest but those of zeros
-// alone: a wave takes a piece, a vector of eight a lane, or several short rows.  Four at a time, whose numbers are on their way together
-// (one by one 8192 x 512 x 2048 float took 6 us more).  A row's last piece begins within the one before it: a number by itself may well be small.
+// alone: a wave takes a piece, a vector of eight a lane, or several short rows.  Who has no piece or vector of its own takes the last one again,
+// and a row's last vector and last piece begin within the ones before them (a number by itself may well be small), so that loads depend on
+// nothing; four of them are on their way together.  Bound by instructions, of which small operands' waves have few to share: the two of 8
+// products, 1038 x 332 and 1842 x 332 float, take 7 us (with loads under conditions and sizes compared as floats 15).
 __global__ __launch_bounds__(256) void product_largest(PackArgs p) {
-  constexpr int kAhead = 4;
+  constexpr uint32_t kAhead = 4;
   static_assert(kPackPiece == 64 * 8, "a vector of a lane");
   const PackOperand& o = p.operand[blockIdx.z];
   const int64_t w = blockIdx.y;
-  const uint32_t vectors = (o.wide + 7) / 8, pieces = (vectors + 63) / 64, all = o.rows * pieces;
-  uint32_t lanes = 1;
-  while (lanes < 64 && lanes < vectors) lanes *= 2;
-  const uint32_t lane = threadIdx.x & (lanes - 1), at_once = 256 / lanes, apart = kPackParts * at_once;
-  const uint32_t rows_apart = apart / pieces, rest_apart = apart - rows_apart * pieces;
-  float most = 0.f, least = __builtin_inff();
-  uint32_t piece = blockIdx.x * at_once + threadIdx.x / lanes, row = piece / pieces, of_row = piece - row * pieces;
-  while (piece < all) {
-    float x[kAhead][8];
+  const uint32_t vectors = (o.wide + 7) / 8, wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  uint32_t most = 0, least = ~0u;              // least: less one, so that zeros are the largest
+  auto find = [&](auto element) {
+    typedef decltype(element) E;
+    const E* const from = static_cast<const E*>(o.p) + w * o.worker_stride;
+    const uint32_t last = o.wide - 8;
+    if (vectors > 32) {
+      const uint32_t pieces = (vectors + 63) / 64, all = o.rows * pieces, begin = vectors - min(vectors, 64u);
+      for (uint32_t first = blockIdx.x * 4 + wave; first < all; first += kAhead * kPackParts * 4) {
+        Eight<E> eight[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const uint32_t v = min(of_row * 64, vectors - min(vectors, 64u)) + lane;
-      if (piece < all && v < vectors) {
-        load_eight(o, w * o.worker_stride + row * o.ld, v * 8, x[i]);
-      } else {
+        for (uint32_t i = 0; i < kAhead; ++i) {
+          const uint32_t piece = min(first + i * kPackParts * 4, all - 1), row = pieces == 1 ? piece : uniform(piece / pieces);
+          eight[i].along(from + row * o.ld + min((min((piece - row * pieces) * 64, begin) + lane) * 8, last));
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+        for (uint32_t i = 0; i < kAhead; ++i) {
+          const uint32_t here = wave_largest_bits(largest_of(eight[i]));
+          most = max(most, here);
+          least = min(least, here - 1);
+        }
       }
-      piece += apart;
-      row += rows_apart;
-      of_row += rest_apart;
-      if (of_row >= pieces) {
-        of_row -= pieces;
-        ++row;
+      return;
+    }
+    uint32_t lanes = 1;
+    while (lanes < vectors) lanes *= 2;
+    const uint32_t at_once = 256 / lanes, col = min((lane & (lanes - 1)) * 8, last);
+    for (uint32_t first = blockIdx.x * at_once; first < o.rows; first += kAhead * kPackParts * at_once) {
+      Eight<E> eight[kAhead];
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i) {
+        const E* const at = from + min(first + i * kPackParts * at_once + threadIdx.x / lanes, o.rows - 1) * o.ld;
+        if (o.wide >= 8) eight[i].along(at + col); else eight[i].across(at, 1, static_cast<int>(o.wide));
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i) {
+        uint32_t here = largest_of(eight[i]);
+        if (lanes > 1) here = larger<0xB1>(here);
+        if (lanes > 2) here = larger<0x4E>(here);
+        if (lanes > 4) here = larger<0x141>(here);
+        if (lanes > 8) here = larger<0x140>(here);
+        if (lanes > 16) here = max(here, static_cast<uint32_t>(__shfl_xor(static_cast<int>(here), 16)));
+        most = max(most, here);
+        least = min(least, here - 1);
       }
     }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      float here = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float size = fabsf(x[i][e]);
-        here = size < __builtin_inff() ? fmaxf(here, size) : here;
-      }
-      if (lanes == 64) {
-        here = wave_largest(here);
-      } else {
-        for (uint32_t k = 1; k < lanes; k *= 2) here = fmaxf(here, __shfl_xor(here, k));
-      }
-      most = fmaxf(most, here);
-      least = here > 0.f ? fminf(least, here) : least;
-    }
-  }
-  most = wave_largest(most);
-  least = -wave_largest(-least);
-  __shared__ float waves[2][4];
-  if ((threadIdx.x & 63) == 0) {
-    waves[0][threadIdx.x >> 6] = most;
-    waves[1][threadIdx.x >> 6] = least;
+    most = wave_largest_bits(most);
+    least = ~wave_largest_bits(~least);
+  };
+  if (o.bf16) find(uint16_t{}); else find(float{});
+  __shared__ uint32_t waves[2][4];
+  if (lane == 0) {
+    waves[0][wave] = most;
+    waves[1][wave] = least;
   }
   __syncthreads();
   if (threadIdx.x == 0) {
     float* const to = p.largest + (w * 2 + blockIdx.z) * 2 * kPackParts + blockIdx.x;
-    to[0] = fmaxf(fmaxf(waves[0][0], waves[0][1]), fmaxf(waves[0][2], waves[0][3]));
-    to[kPackParts] = fminf(fminf(waves[1][0], waves[1][1]), fminf(waves[1][2], waves[1][3]));
+    to[0] = __uint_as_float(max(max(waves[0][0], waves[0][1]), max(waves[0][2], waves[0][3])));
+    least = min(min(waves[1][0], waves[1][1]), min(waves[1][2], waves[1][3]));
+    to[kPackParts] = least == ~0u ? __builtin_inff() : __uint_as_float(least + 1);
   }
 }
 
@@ -640,11 +685,11 @@ __global__ __launch_bounds__(256) void product_pack(PackArgs p) {
     static_assert(kPackParts == 256, "four of a lane");
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float* const from = p.largest + (w * 2 + i) * 2 * kPackParts + (threadIdx.x & 63) * 4;
-      const float4v four = *reinterpret_cast<const float4v*>(from), rows = *reinterpret_cast<const float4v*>(from + kPackParts);
-      float most = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3])), least = fminf(fminf(rows[0], rows[1]), fminf(rows[2], rows[3]));
-      most = wave_largest(most);
-      least = -wave_largest(-least);
+      const uint32_t* const from = reinterpret_cast<const uint32_t*>(p.largest) + (w * 2 + i) * 2 * kPackParts + (threadIdx.x & 63) * 4;
+      const uint4v four = *reinterpret_cast<const uint4v*>(from), rows = *reinterpret_cast<const uint4v*>(from + kPackParts);
+      // floats of at least zero, in the order of their bits
+      const float most = __uint_as_float(wave_largest_bits(max(max(four[0], four[1]), max(four[2], four[3]))));
+      const float least = __uint_as_float(~wave_largest_bits(~min(min(rows[0], rows[1]), min(rows[2], rows[3]))));
       halves = halves && !(least < most * kPackRange);
       if (i == blockIdx.z && most > 0.f) {
         int power;
