@@ -3,6 +3,8 @@ go: (W, T, inputs, outputs, more of test_gpu_linear.Layer)."""
 
 # Rows of very different sizes: operands that are packed to binary16, or to bf16 parts.
 RANGE = (2, 1500, 712, 1544, dict(bias=False))
+# The same with rows that several of a wave's lanes take: 4, 8 and 16.
+NARROW = [(2, 3000, 20, 5000, dict(bias=False)), (2, 2040, 64, 4090, dict(bias=False)), (2, 1000, 100, 3000, dict(bias=False))]
 RANGE_TYPES = [("f32", "f32", "f32"), ("bf16", "f32", "f32"), ("f32", "bf16", "f32"), ("f32", "f32", "bf16")]
 
 # Every kernel of large products: tiles of 256, 128 and 32 x 256, operands along k or across it, bf16 or binary16; odd edges of tiles, stages and

@@ -45,6 +45,16 @@ def test_rows_of_activations(types, how):
     check_product(got, x, layer.matrix(a), out)
 
 
+@pytest.mark.parametrize("how", ["one huge", "one tiny", "falling"])
+@pytest.mark.parametrize("size", shapes.NARROW, ids=str)
+def test_short_rows(size, how):
+    W, T, inputs, outputs, more = size
+    layer = Layer(W, inputs, outputs, **more)
+    a, x = layer.array(torch.float32, std=0.3), rows_apart(randn((W, T, inputs), 2), how)
+    got, _ = forward(layer, layer.plan(T), x, a, "none", None, torch.float32, before=False)
+    check_product(got, x, layer.matrix(a), torch.float32)
+
+
 @pytest.mark.parametrize("types", shapes.RANGE_TYPES, ids=str)
 def test_rows_of_the_matrix(types):
     """One that belongs to an input that is zero everywhere."""

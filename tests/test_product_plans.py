@@ -24,6 +24,12 @@ def test_rows_far_apart_are_packed(types):
     assert products[0]["parts"] == tuple((3 if types[2] == "f32" else 2) if t == "f32" else 1 for t in types[:2]) and floats >= 1
 
 
+@pytest.mark.parametrize("size", shapes.NARROW, ids=str)
+def test_short_rows_are_packed(size):
+    (_, products), = plans([call(False, size, ("f32",) * 3)])
+    assert products[0]["f16"] == 1 and products[0]["tile"] > 0 and products[0]["packed"] == (1, 1)
+
+
 @pytest.mark.parametrize("act", [0, 1])
 def test_padding_in_a_gradient_is_packed(act):
     (_, products), = plans([call(True, shapes.RANGE, ("f32",) * 5, act)])
